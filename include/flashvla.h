@@ -419,6 +419,187 @@ fv_status fv_debug_forward(fv_handle h, const float *buffer, const float *t,
  */
 fv_status fv_debug_stage(fv_handle h, int32_t stage, int32_t layer, int32_t reps, void *stream);
 
+/*
+ * ---------------------------------------------------------------------------
+ * The observation context: operators that make, keep and read the keys and
+ * values which fv_set_prefix installs and a vision-language model attends to.
+ *
+ * They take no handle.  The caller owns every tensor, the cache's bookkeeping
+ * included; the operators keep nothing between calls and allocate nothing, so
+ * each may be captured into a HIP graph and replayed.  Pointers are dev memory
+ * of the stream's GPU (the current one for the NULL stream) unless written
+ * otherwise, 16-byte aligned (int32 arrays: 4-byte).  What the host can see is
+ * checked before anything is enqueued (FV_ERR_INVALID_ARG); indexes in device
+ * memory are checked by the kernels, which never read or write outside the
+ * stated tensors whatever the indexes hold.  Calls that write the same tensors
+ * are ordered by their stream; on several streams, the caller orders them.
+ * fv_context_error() describes the calling thread's last failure.
+ *
+ * head_dim is 64, 128, 192 or 256; dtype FV_BF16 or FV_FP32; n_q_heads a
+ * multiple of n_kv_heads, query head h reading kv head h / (n_q_heads /
+ * n_kv_heads); at most 1024 query heads.  A leading dimension (ld*) counts the
+ * elements from one token's row to the next: at least the row, a multiple of
+ * 16 bytes, at most 2^20; the heads of a row lie side by side.
+ * ---------------------------------------------------------------------------
+ */
+
+/*
+ * A paged cache of max_seqs sequences in n_layers layers.
+ *  k, v   [n_layers][n_pages][n_kv_heads][page_len][head_dim] of the dtype
+ *  table  int32 [max_seqs][max_pages]: position p of sequence s is row
+ *         p % page_len of page table[s][p / page_len] (in every layer)
+ *  len    int32 [max_seqs]: tokens of each sequence
+ *  refs   int32 [n_pages]: how many sequences hold a page; 0 is a free page
+ * The first ceil(len / page_len) entries of a table row are in use; the others
+ * are ignored.  A fresh cache has len and refs zero.
+ * Requirements: page_len a multiple of 16, at most 256; n_layers <= 1024;
+ * n_kv_heads <= 1024; n_pages <= 2^20; max_seqs, max_pages <= 65536.
+ */
+typedef struct {
+  int32_t dtype, n_layers, n_kv_heads, head_dim, page_len, n_pages, max_seqs, max_pages;
+  void *k, *v;
+  int32_t *table, *len, *refs;
+} fv_pages;
+
+/*
+ * fv_rope_append -- rotary positions of several axes on new queries and keys,
+ * and the new keys and values into the pages of one layer.
+ * Pair i of a head, the elements i and i + head_dim/2, turns by the angle
+ * pos[a][token] * theta^(-2i/head_dim), where a is the axis whose section holds
+ * i: axis 0 has the first sections[0] pairs, axis 1 the next sections[1], and so
+ * on (time, height and width of an image or video token; one axis is the usual
+ * rotary embedding).  Angles are formed in 64 bits and reduced exactly to one
+ * turn, so far positions lose nothing; products are fp32, rounded once.
+ *  q         [n][n_q_heads][head_dim], ldq    k, v   [n][n_kv_heads][head_dim], ldk, ldv
+ *  q_out     as q, ldq_out: rotated queries    k_out  as k, ldk_out: rotated keys, or NULL
+ *  pos       int32 [n_axes][n], n_axes 1..4; the sections add up to head_dim/2
+ *  seqs, at  int32 [n]: the token becomes position at of sequence seqs of the
+ *            cache.  A token whose place does not exist (seqs or at out of range,
+ *            a table entry that is no page) is rotated and not stored: a padded
+ *            batch passes seqs = -1.  Two tokens of one place: either is stored.
+ *  cache     the pages, or NULL: rotate only (then seqs, at and v are not read)
+ * len is neither read nor changed; fv_pages_grow makes room beforehand.
+ * q_out may be q and k_out may be k (same leading dimension); otherwise outputs
+ * and inputs must not overlap.  n = 0 does nothing.
+ * Errors: FV_ERR_INVALID_ARG, FV_ERR_HIP.
+ */
+typedef struct {
+  const void *q, *k, *v;
+  void *q_out, *k_out;
+  int32_t ldq, ldk, ldv, ldq_out, ldk_out;
+  const int32_t *pos, *seqs, *at;
+  int32_t n, n_q_heads, n_kv_heads, head_dim, dtype, layer;
+  int32_t n_axes, sections[4];
+  float theta;
+} fv_rope_args;
+fv_status fv_rope_append(const fv_rope_args *args, const fv_pages *cache, void *stream);
+
+/*
+ * fv_prompt_attention -- attention over whole prompts, packed one after another.
+ *  q, out  [n_q][n_q_heads][head_dim], ldq, ldo     k, v  [n_k][n_kv_heads][head_dim], ldk, ldv
+ *  cu_q, cu_k  int32 [n_seqs + 1], ascending from 0: prompt s has the query rows
+ *              cu_q[s] .. cu_q[s+1] and the keys cu_k[s] .. cu_k[s+1]
+ *  causal  1: the queries are the last ones of their keys, query i of nq seeing
+ *             the keys j <= nk - nq + i; 0: every query sees its prompt's keys
+ *  scale   of the scores, positive and finite (1/sqrt(head_dim) is usual)
+ * A query that sees no key (nk = 0; the first rows of a causal prompt with nq >
+ * nk) gives zeros.  Rows past cu_q[n_seqs] are left as they were.  What a query
+ * does not see has no influence on its result, also where it is infinite or NaN.
+ * Scores, softmax and sums are fp32; in bf16 the probabilities are rounded to
+ * bf16 before they meet the values.  out must not overlap q, k or v.
+ * Errors: FV_ERR_INVALID_ARG (a size below 0, n_seqs > 65536, strides,
+ * pointers), FV_ERR_HIP.
+ */
+typedef struct {
+  const void *q, *k, *v;
+  void *out;
+  int32_t ldq, ldk, ldv, ldo;
+  const int32_t *cu_q, *cu_k;
+  int32_t n_seqs, n_q, n_k, n_q_heads, n_kv_heads, head_dim, dtype, causal;
+  float scale;
+} fv_prompt_args;
+fv_status fv_prompt_attention(const fv_prompt_args *args, void *stream);
+
+/*
+ * fv_paged_attention -- attention of one new token a sequence over one layer of
+ * the cache (the token's own key and value are in the cache already).
+ *  q, out   [n][n_q_heads][head_dim], ldq, ldo
+ *  seqs     int32 [n]: row i reads the first len[seqs[i]] positions of that
+ *           sequence.  A row whose seqs is out of range is left as it was (a
+ *           padded batch passes -1); an empty sequence gives zeros.  Table
+ *           entries that are no page hold no keys.
+ *  max_len  a bound of the lengths that only plans the work: sequences may be
+ *           longer at some cost in time.  0: what a table row can hold.
+ *  scale    as above
+ *  work     fv_paged_attention_workspace bytes, overwritten (calls that may run
+ *           at the same time need one each); NULL where that is 0
+ * Rounding as in fv_prompt_attention; the result does not depend on the other
+ * rows' lengths.  out must not overlap q.
+ * Errors: FV_ERR_INVALID_ARG, FV_ERR_HIP.
+ */
+typedef struct {
+  const void *q;
+  void *out;
+  int32_t ldq, ldo;
+  const int32_t *seqs;
+  int32_t n, n_q_heads, layer, max_len;
+  float scale;
+  void *work;
+  size_t work_bytes;
+} fv_paged_args;
+fv_status fv_paged_attention_workspace(const fv_paged_args *args, const fv_pages *cache,
+                                       size_t *bytes);
+fv_status fv_paged_attention(const fv_paged_args *args, const fv_pages *cache, void *stream);
+
+/*
+ * The cache's upkeep.  Each call takes effect as a whole or, where it writes a
+ * status other than FV_PAGES_OK, not at all.  Lists are int32 [n] in device
+ * memory, n <= max_seqs (n = 0: nothing but the status); pages are taken lowest
+ * number first, in the list's order.  `status` is one int32 in device memory,
+ * written on the stream.  `work` is fv_pages_workspace bytes, overwritten (calls
+ * that may run at the same time need one each).
+ *
+ *  fv_pages_grow     sequence seqs[i] gets add[i] >= 0 more positions, with pages
+ *                    for them.  FV_PAGES_BAD: a sequence out of range or listed
+ *                    twice, add[i] < 0, more than max_pages pages, or a part-filled
+ *                    last page that another sequence holds too.
+ *  fv_pages_fork     children[i], an empty sequence, becomes a copy of parents[i]:
+ *                    full pages are shared, the rows in use of a part-filled last
+ *                    page are copied to a page of its own in every layer (its other
+ *                    rows are left as they were).  A parent may occur several times.
+ *                    FV_PAGES_BAD: out of range, a child listed twice, not empty or
+ *                    a parent too, a parent's entry in use that is no page.
+ *  fv_pages_free     the sequences are emptied: one holder fewer for each page, the
+ *                    whole table row -1, len 0.  FV_PAGES_BAD: out of range, twice.
+ *  fv_pages_compact  the pages in use move to the front: with u of them in use, the
+ *                    i-th lowest page in use from u on moves to the i-th lowest free
+ *                    page below u, contents, holders and table entries.  Writes u to
+ *                    `used` (int32 in device memory).  Moved-from pages keep their
+ *                    contents.
+ *  fv_pages_gather   copies sequences out, dense, as fv_set_prefix takes them:
+ *                    k_out, v_out [n_layers][n][ld][n_kv_heads][head_dim]; row r of
+ *                    entry i is position r of seqs[i], for r < min(len, ld); other
+ *                    rows, and those on table entries that are no page, are left as
+ *                    they were.  A sequence may occur several times; n <= 65536.
+ * FV_PAGES_FULL: fewer free pages than the call needs.
+ * Errors: FV_ERR_INVALID_ARG, FV_ERR_HIP.
+ */
+enum { FV_PAGES_OK = 0, FV_PAGES_BAD = 1, FV_PAGES_FULL = 2 };
+fv_status fv_pages_workspace(const fv_pages *cache, size_t *bytes);
+fv_status fv_pages_grow(const fv_pages *cache, const int32_t *seqs, const int32_t *add, int32_t n,
+                        int32_t *status, void *work, void *stream);
+fv_status fv_pages_fork(const fv_pages *cache, const int32_t *parents, const int32_t *children,
+                        int32_t n, int32_t *status, void *work, void *stream);
+fv_status fv_pages_free(const fv_pages *cache, const int32_t *seqs, int32_t n, int32_t *status,
+                        void *stream);
+fv_status fv_pages_compact(const fv_pages *cache, int32_t *used, void *work, void *stream);
+fv_status fv_pages_gather(const fv_pages *cache, const int32_t *seqs, int32_t n, int32_t ld,
+                          void *k_out, void *v_out, void *stream);
+
+/* Message of the calling thread's last failed call of the observation context
+ * ("" if its last one succeeded), valid until the thread's next one. */
+const char *fv_context_error(void);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,45 @@
+// Internal declarations of the observation context's operators (rotary append,
+// prompt attention, paged attention, the cache's upkeep).
+#pragma once
+
+#include "fv_internal.h"
+
+namespace fv {
+
+// First of the `group` kv heads' rows: the pools are [layer][page][kv head][row][dh].
+__host__ __device__ __forceinline__ size_t page_row(int page, int n_kv, int head, int page_len) {
+  return ((size_t)page * n_kv + head) * page_len;
+}
+
+// The launches take validated arguments.
+template <typename T>
+void launch_rope_append(const fv_rope_args& a, const fv_pages* c, hipStream_t s);
+template <typename T>
+void launch_prompt(const fv_prompt_args& a, hipStream_t s);
+
+// How a paged attention is laid out: chunks of `chunk` keys, at most n_chunks
+// a sequence, each with one workgroup per kv head and tile of 16 query heads.
+struct PagedPlan {
+  int chunk, n_chunks;
+  size_t work_bytes;  // partial outputs and softmax statistics; 0 with one chunk
+};
+PagedPlan plan_paged(int n, int n_q_heads, int n_kv_heads, int head_dim, int max_keys, bool bf16);
+template <typename T>
+void launch_paged(const fv_paged_args& a, const fv_pages& c, const PagedPlan& p, hipStream_t s);
+
+// int32 values of the upkeep's workspace: a header, then three lists.
+constexpr int kPagesHeader = 64;
+inline size_t pages_list(const fv_pages& c) {
+  return (size_t)(c.n_pages > c.max_seqs ? c.n_pages : c.max_seqs);
+}
+inline size_t pages_work_ints(const fv_pages& c) { return kPagesHeader + 3 * pages_list(c); }
+void launch_pages_grow(const fv_pages& c, const int* seqs, const int* add, int n, int* status,
+                       int* work, hipStream_t s);
+void launch_pages_fork(const fv_pages& c, const int* parents, const int* children, int n,
+                       int* status, int* work, hipStream_t s);
+void launch_pages_free(const fv_pages& c, const int* seqs, int n, int* status, hipStream_t s);
+void launch_pages_compact(const fv_pages& c, int* used, int* work, hipStream_t s);
+void launch_pages_gather(const fv_pages& c, const int* seqs, int n, int ld, void* k_out,
+                         void* v_out, hipStream_t s);
+
+}  // namespace fv

@@ -1,0 +1,413 @@
+// Attention of one new token a sequence over the pages of a cache.
+//
+// Every key and value is read once and used for the few query heads that share
+// its kv head, so memory bounds it: the kernel is built around many wide loads
+// in flight.  A sequence's keys are split into chunks, one workgroup each (per
+// kv head and tile of 16 query heads), and a chunk's tiles among four waves that
+// do not wait for each other: every wave runs its own softmax (running maximum
+// and sum) over its own tiles, from memory straight into registers.  The waves
+// join in LDS at the end, the chunks in a second kernel, both in a fixed order.
+//
+// Per tile S^T = K Q^T by MFMA (the queries are the columns, 16 of them, padded),
+// so a lane holds scores of one query head for four consecutive keys of each 16,
+// which is, without data movement, the operand that O^T += V^T P^T wants.  V^T
+// needs keys along a lane: a lane loads 16 bytes (8 bf16 elements) of each of
+// its own 8 keys, one 256-byte row per 16 lanes, and turns the 8x8 block over in
+// registers (32 byte permutes, nothing beside the loads); which element of the
+// head a matrix row stands for is free, and chosen so that this works out.
+#include "fv_context.h"
+
+namespace fv {
+namespace {
+
+constexpr int kPagedWaves = 4;
+constexpr float kLog2e = 1.4426950408889634f;
+
+// Largest of the lanes l, l ^ 16, l ^ 32, l ^ 48.
+__device__ __forceinline__ float max_xor16_32(float x) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  const float y = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(y), __float_as_uint(y), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+struct PagedCall {
+  const void *q, *k, *v;  // the pools of the layer
+  void* out;
+  const int *seqs, *table, *len;
+  float* part;  // [n][n_chunks][heads][DH] sums, then [n][n_chunks][heads][2] maximum and sum
+  float* stat;
+  int ldq, ldo, n, heads, n_kv, group, q_tiles, page_len, n_pages, max_seqs, max_pages;
+  int chunk, n_chunks;
+  float scale;  // of the scores, in log2 units
+};
+
+// Chunks of a sequence that hold keys.  The last workgroup takes what lies past
+// the planned bound, should a sequence be longer.
+__device__ __forceinline__ int chunks_of(int len, int chunk, int n_chunks) {
+  const int c = (len + chunk - 1) / chunk;
+  return c < n_chunks ? c : n_chunks;
+}
+__device__ __forceinline__ int length_of(const PagedCall& a, int s) {
+  return min(max(a.len[s], 0), a.max_pages * a.page_len);
+}
+
+// A V tile in registers, and its matrix operands.  bf16: 32 keys, 8 a lane
+// (4g .. 4g+3 of either half); the head's 128-element blocks 8 elements a lane,
+// a last block of 64 four.  fp32: 16 keys, 4 a lane, blocks of 64, 4 elements.
+template <typename T, int DH> struct VTile;
+
+template <int DH> struct VTile<bf16_t, DH> {
+  static constexpr int B8 = DH / 128, B4 = (DH % 128) / 64;
+  u32x4 w[B8 > 0 ? B8 : 1][8];
+  u32x2 n[8];
+  __device__ __forceinline__ void load(const bf16_t* const (&row)[2], int l16, int lg) {
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      const bf16_t* p = row[x >> 2] + (size_t)(4 * lg + (x & 3)) * DH;
+#pragma unroll
+      for (int b = 0; b < B8; ++b) w[b][x] = *reinterpret_cast<const u32x4*>(p + 128 * b + 8 * l16);
+      if (B4) n[x] = *reinterpret_cast<const u32x2*>(p + 128 * B8 + 4 * l16);
+    }
+  }
+  __device__ __forceinline__ void drop(int x) {  // key x of the lane is not there
+#pragma unroll
+    for (int b = 0; b < B8; ++b) w[b][x] = u32x4{0, 0, 0, 0};
+    if (B4) n[x] = u32x2{0, 0};
+  }
+  // operand of tile t: element t % 8 of the lane's in block t / 8 (t % 4 of the last 64)
+  __device__ __forceinline__ u32x4 operand(int t) const {
+    const int b = t / 8, j = b < B8 ? t % 8 : t - 8 * B8;
+    const uint32_t sel = j & 1 ? 0x07060302u : 0x05040100u;
+    u32x4 r;
+#pragma unroll
+    for (int y = 0; y < 4; ++y)
+      r[y] = b < B8 ? __builtin_amdgcn_perm(w[b < B8 ? b : 0][2 * y + 1][j >> 1],
+                                            w[b < B8 ? b : 0][2 * y][j >> 1], sel)
+                    : __builtin_amdgcn_perm(n[2 * y + 1][(j >> 1) & 1], n[2 * y][(j >> 1) & 1], sel);
+    return r;
+  }
+};
+
+template <int DH> struct VTile<float, DH> {
+  u32x4 w[DH / 64][4];
+  __device__ __forceinline__ void load(const float* const (&row)[1], int l16, int lg) {
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+      for (int b = 0; b < DH / 64; ++b)
+        w[b][x] = *reinterpret_cast<const u32x4*>(row[0] + (size_t)(4 * lg + x) * DH + 64 * b + 4 * l16);
+  }
+  __device__ __forceinline__ void drop(int x) {
+#pragma unroll
+    for (int b = 0; b < DH / 64; ++b) w[b][x] = u32x4{0, 0, 0, 0};
+  }
+  __device__ __forceinline__ u32x4 operand(int t) const {
+    return u32x4{w[t / 4][0][t % 4], w[t / 4][1][t % 4], w[t / 4][2][t % 4], w[t / 4][3][t % 4]};
+  }
+};
+
+// Head element of matrix row i of tile t.
+template <typename T, int DH> __device__ __forceinline__ int element_of(int t, int i) {
+  if (sizeof(T) == 4) return 64 * (t / 4) + 4 * i + t % 4;
+  constexpr int B8 = DH / 128;
+  return t / 8 < B8 ? 128 * (t / 8) + 8 * i + t % 8 : 128 * B8 + 4 * i + (t - 8 * B8);
+}
+
+template <typename T, int DH>
+__global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_kernel(PagedCall a) {
+  constexpr int NH = sizeof(T) == 2 ? 2 : 1;       // 16-key halves of a tile
+  constexpr int KT = 16 * NH;                      // keys of a tile
+  constexpr int KB = DH * (int)sizeof(T) / 64;     // 64-byte blocks of a head
+  constexpr int EB = 64 / (int)sizeof(T);          // elements of one
+  constexpr int NT = DH / 16;                      // tiles of O^T
+  __shared__ float sm[kPagedWaves][16], sl[kPagedWaves][16];
+  __shared__ __attribute__((aligned(16))) float so[kPagedWaves][16][DH + 4];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int l16 = lane & 15, lg = lane >> 4;
+  int id = blockIdx.x;
+  const int qt = id % a.q_tiles;
+  id /= a.q_tiles;
+  const int kh = id % a.n_kv;
+  id /= a.n_kv;
+  const int ch = id % a.n_chunks, row = id / a.n_chunks;
+  const int s = a.seqs[row];
+  if (s < 0 || s >= a.max_seqs) return;
+  const int len = length_of(a, s);
+  const int chunks = chunks_of(len, a.chunk, a.n_chunks);
+  if (ch >= chunks && ch > 0) return;
+  const int k0 = ch * a.chunk, k1 = ch == a.n_chunks - 1 ? len : min(len, k0 + a.chunk);
+  const int* table = a.table + (size_t)s * a.max_pages;
+
+  // queries: the head of column l16, zeros past the group
+  const int head = qt * 16 + l16;
+  u32x4 qf[KB];
+  {
+    const T* q = static_cast<const T*>(a.q) + (size_t)row * a.ldq + (kh * a.group + head) * DH;
+#pragma unroll
+    for (int b = 0; b < KB; ++b)
+      qf[b] = head < a.group
+                  ? *reinterpret_cast<const u32x4*>(q + EB * b + (EB / 4) * lg)
+                  : u32x4{0, 0, 0, 0};
+  }
+
+  f32x4 o[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;  // of the lane's query; l over the lane's keys only
+  bool any = false;              // a key was seen
+
+  const T* kp = static_cast<const T*>(a.k);
+  const T* vp = static_cast<const T*>(a.v);
+  const int tiles = (k1 - k0 + KT - 1) / KT;
+  // Page numbers 64 halves at a time: lane i holds half i % NH of the wave's tile base + i / NH.
+  constexpr int GO = 64 / NH;
+  for (int base = wave; base < tiles; base += kPagedWaves * GO) {
+    const int myKey = k0 + (base + kPagedWaves * (lane / NH)) * KT + 16 * (lane % NH);
+    int page = -1;
+    if (myKey < k1) {
+      page = table[myKey / a.page_len];
+      if (page < 0 || page >= a.n_pages) page = -1;
+    }
+    const int off = page >= 0 ? myKey % a.page_len : 0;
+    const int here = min(GO, (tiles - base + kPagedWaves - 1) / kPagedWaves);
+    for (int it = 0; it < here; ++it) {
+      const int key0 = k0 + (base + kPagedWaves * it) * KT;
+      const T* krow[NH];
+      const T* vrow[NH];
+      int left[NH];  // keys of the half that are there
+#pragma unroll
+      for (int h = 0; h < NH; ++h) {
+        const int pg = __builtin_amdgcn_readlane(page, it * NH + h);
+        const int of = __builtin_amdgcn_readlane(off, it * NH + h);
+        left[h] = pg < 0 ? 0 : min(16, k1 - (key0 + 16 * h));
+        const size_t at = (page_row(pg < 0 ? 0 : pg, a.n_kv, kh, a.page_len) + of) * DH;
+        krow[h] = kp + at;
+        vrow[h] = vp + at;
+      }
+      u32x4 kf[NH][KB];
+#pragma unroll
+      for (int h = 0; h < NH; ++h)
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+          kf[h][b] = *reinterpret_cast<const u32x4*>(krow[h] + (size_t)l16 * DH + EB * b + (EB / 4) * lg);
+      VTile<T, DH> vt;
+      vt.load(vrow, l16, lg);
+
+      f32x4 sc[NH];
+#pragma unroll
+      for (int h = 0; h < NH; ++h) {
+        sc[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int b = 0; b < KB; ++b) sc[h] = mma64(kf[h][b], qf[b], sc[h], T{});
+      }
+      bool whole = true;
+#pragma unroll
+      for (int h = 0; h < NH; ++h) {
+        whole = whole && left[h] == 16;
+        any = any || left[h] > 0;
+      }
+      if (!whole) {  // keys that are not there: no weight, and values that hold nothing
+#pragma unroll
+        for (int h = 0; h < NH; ++h)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (4 * lg + r >= left[h]) {
+              sc[h][r] = -INFINITY;
+              vt.drop(4 * h + r);
+            }
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int h = 0; h < NH; ++h)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          sc[h][r] *= a.scale;
+          top = fmaxf(top, sc[h][r]);
+        }
+      top = max_xor16_32(top);
+      if (__any(top > m)) {
+        const float now = fmaxf(m, top);
+        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - now);
+        m = now;
+        l *= f;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) o[t] *= f;
+      }
+      const float ref = m == -INFINITY ? 0.f : m;
+      u32x4 pf;
+      if constexpr (sizeof(T) == 2) {
+        u16x8 pb;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float p = __builtin_amdgcn_exp2f(sc[h][r] - ref);
+            l += p;
+            pb[4 * h + r] = f32_to_bf16(p);
+          }
+        pf = __builtin_bit_cast(u32x4, pb);
+      } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float p = __builtin_amdgcn_exp2f(sc[0][r] - ref);
+          l += p;
+          pf[r] = __float_as_uint(p);
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t) o[t] = mma64(vt.operand(t), pf, o[t], T{});
+    }
+  }
+
+  // join the waves
+  l = sum_xor16_32(l);
+  if (lg == 0) {
+    sm[wave][l16] = m;
+    // a sequence of keys that all score -inf has no softmax: NaN, as 0/0
+    sl[wave][l16] = any && m == -INFINITY ? 0.f : l;
+  }
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) so[wave][l16][element_of<T, DH>(t, 4 * lg + r)] = o[t][r];
+  __shared__ int seen[kPagedWaves];
+  if (lane == 0) seen[wave] = any;
+  __syncthreads();
+  const int tid = threadIdx.x;
+  const int heads_here = min(16, a.group - qt * 16);
+  bool some = false;
+#pragma unroll
+  for (int w = 0; w < kPagedWaves; ++w) some = some || seen[w];
+  for (int idx = tid; idx < heads_here * (DH / 4); idx += 64 * kPagedWaves) {
+    const int hd = idx / (DH / 4), d = 4 * (idx % (DH / 4));
+    float mm = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kPagedWaves; ++w) mm = fmaxf(mm, sm[w][hd]);
+    const float ref = mm == -INFINITY ? 0.f : mm;
+    float ll = 0.f;
+    f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kPagedWaves; ++w) {
+      const float f = __builtin_amdgcn_exp2f(sm[w][hd] - ref);
+      ll += f * sl[w][hd];
+      acc += f * *reinterpret_cast<const f32x4*>(&so[w][hd][d]);
+    }
+    const int qh = kh * a.group + qt * 16 + hd;
+    if (a.n_chunks == 1) {
+      const float inv = some ? 1.0f / ll : 0.f;
+      store4(static_cast<T*>(a.out) + (size_t)row * a.ldo + qh * DH + d, acc[0] * inv, acc[1] * inv,
+             acc[2] * inv, acc[3] * inv);
+    } else {
+      const size_t at = ((size_t)row * a.n_chunks + ch) * a.heads + qh;
+      *reinterpret_cast<f32x4*>(a.part + at * DH + d) = acc;
+      if (d == 0) {
+        a.stat[2 * at] = some ? mm : -INFINITY;
+        // no key at all: a sum of -1, which no other chunk has
+        a.stat[2 * at + 1] = some ? ll : -1.f;
+      }
+    }
+  }
+}
+
+// Joins a row's chunks: block (row, head), DH/4 threads.
+template <typename T, int DH>
+__global__ __launch_bounds__(64) void paged_join_kernel(PagedCall a) {
+  const int row = blockIdx.x / a.heads, qh = blockIdx.x - row * a.heads;
+  const int s = a.seqs[row];
+  if (s < 0 || s >= a.max_seqs) return;
+  const int chunks = max(1, chunks_of(length_of(a, s), a.chunk, a.n_chunks));
+  const int d = 4 * threadIdx.x;
+  float m = -INFINITY, l = 0.f;
+  bool some = false;
+  for (int ch = 0; ch < chunks; ++ch)
+    m = fmaxf(m, a.stat[2 * (((size_t)row * a.n_chunks + ch) * a.heads + qh)]);
+  const float ref = m == -INFINITY ? 0.f : m;
+  f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int ch = 0; ch < chunks; ++ch) {
+    const size_t at = ((size_t)row * a.n_chunks + ch) * a.heads + qh;
+    const float lc = a.stat[2 * at + 1];
+    if (lc == -1.f) continue;
+    some = true;
+    const float f = __builtin_amdgcn_exp2f(a.stat[2 * at] - ref);
+    l += f * lc;
+    if (d < DH) acc += f * *reinterpret_cast<const f32x4*>(a.part + at * DH + d);
+  }
+  if (d >= DH) return;
+  const float inv = some ? 1.0f / l : 0.f;
+  store4(static_cast<T*>(a.out) + (size_t)row * a.ldo + qh * DH + d, acc[0] * inv, acc[1] * inv,
+         acc[2] * inv, acc[3] * inv);
+}
+
+template <typename T, int DH>
+void paged_at(const PagedCall& a, hipStream_t s) {
+  const int blocks = a.n * a.n_chunks * a.n_kv * a.q_tiles;
+  hipLaunchKernelGGL((paged_kernel<T, DH>), dim3(blocks), dim3(64 * kPagedWaves), 0, s, a);
+  if (a.n_chunks > 1)
+    hipLaunchKernelGGL((paged_join_kernel<T, DH>), dim3(a.n * a.heads), dim3(64), 0, s, a);
+}
+
+}  // namespace
+
+PagedPlan plan_paged(int n, int n_q_heads, int n_kv_heads, int head_dim, int max_keys, bool bf16) {
+  PagedPlan p{};
+  const int64_t cols = (int64_t)n * n_kv_heads * ((n_q_heads / n_kv_heads + 15) / 16);
+  // 2048 workgroups fill the chip (two to four a CU at a time) and leave room
+  // for ragged lengths; a chunk is at least one tile of each wave and at most
+  // 2048 keys, where its partial result is below a hundredth of its keys.
+  const int least = kPagedWaves * (bf16 ? 32 : 16);
+  int64_t chunk = ((int64_t)max_keys * cols + 2047) / 2048;
+  chunk = (chunk + least - 1) / least * least;
+  if (chunk < least) chunk = least;
+  if (chunk > 2048) chunk = 2048;
+  int64_t chunks = (max_keys + chunk - 1) / chunk;
+  if (chunks < 1) chunks = 1;
+  while (chunks > 1 && chunks * cols > (1 << 30)) chunks /= 2;  // the grid's limit: longer last chunks
+  p.chunk = (int)chunk;
+  p.n_chunks = (int)chunks;
+  if (chunks > 1) {
+    const size_t rows = (size_t)n * chunks * n_q_heads;
+    p.work_bytes = rows * (head_dim + 2) * 4;
+  }
+  return p;
+}
+
+template <typename T>
+void launch_paged(const fv_paged_args& x, const fv_pages& c, const PagedPlan& p, hipStream_t s) {
+  PagedCall a{};
+  const size_t layer = (size_t)x.layer * page_row(c.n_pages, c.n_kv_heads, 0, c.page_len) * c.head_dim;
+  a.q = x.q;
+  a.k = static_cast<const T*>(c.k) + layer;
+  a.v = static_cast<const T*>(c.v) + layer;
+  a.out = x.out;
+  a.seqs = x.seqs;
+  a.table = c.table;
+  a.len = c.len;
+  a.part = static_cast<float*>(x.work);
+  a.stat = a.part + (size_t)x.n * p.n_chunks * x.n_q_heads * c.head_dim;
+  a.ldq = x.ldq;
+  a.ldo = x.ldo;
+  a.n = x.n;
+  a.heads = x.n_q_heads;
+  a.n_kv = c.n_kv_heads;
+  a.group = x.n_q_heads / c.n_kv_heads;
+  a.q_tiles = (a.group + 15) / 16;
+  a.page_len = c.page_len;
+  a.n_pages = c.n_pages;
+  a.max_seqs = c.max_seqs;
+  a.max_pages = c.max_pages;
+  a.chunk = p.chunk;
+  a.n_chunks = p.n_chunks;
+  a.scale = x.scale * kLog2e;
+  switch (c.head_dim) {
+    case 64: return paged_at<T, 64>(a, s);
+    case 128: return paged_at<T, 128>(a, s);
+    case 192: return paged_at<T, 192>(a, s);
+    default: return paged_at<T, 256>(a, s);
+  }
+}
+template void launch_paged<bf16_t>(const fv_paged_args&, const fv_pages&, const PagedPlan&, hipStream_t);
+template void launch_paged<float>(const fv_paged_args&, const fv_pages&, const PagedPlan&, hipStream_t);
+
+}  // namespace fv

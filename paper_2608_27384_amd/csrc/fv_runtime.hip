@@ -9,6 +9,7 @@
 #include <string>
 #include <vector>
 
+#include "fv_error.h"
 #include "fv_internal.h"
 #include "fv_pack.h"
 
@@ -24,32 +25,6 @@ static __device__ __align__(256) unsigned char scratch[kStaticScratchBytes];
 
 namespace fv {
 namespace {
-
-struct FvError {
-  fv_status st;
-  std::string msg;
-};
-
-[[noreturn]] void fail(fv_status st, const std::string& m) { throw FvError{st, m}; }
-
-#define FV_HIP(x)                                                                       \
-  do {                                                                                  \
-    hipError_t e_ = (x);                                                                \
-    if (e_ != hipSuccess) fail(FV_ERR_HIP, std::string(#x) + ": " + hipGetErrorString(e_)); \
-  } while (0)
-
-// Restores the caller's current device on scope exit.
-struct DeviceScope {
-  int prev = -1;
-  explicit DeviceScope(int dev) {
-    if (hipGetDevice(&prev) != hipSuccess) prev = -1;
-    if (prev != dev) FV_HIP(hipSetDevice(dev));
-  }
-  ~DeviceScope() {
-    int cur = -1;
-    if (prev >= 0 && hipGetDevice(&cur) == hipSuccess && cur != prev) (void)hipSetDevice(prev);
-  }
-};
 
 template <typename Fn>
 fv_status guarded(Handle* h, Fn&& fn) {
@@ -118,10 +93,6 @@ float* upload_f32(Handle* h, const float* src, size_t n, bool round) {
   float* d = static_cast<float*>(dalloc(h, n * 4));
   FV_HIP(hipMemcpy(d, v.data(), n * 4, hipMemcpyHostToDevice));
   return d;
-}
-
-void need(const void* p, const char* what) {
-  if (!p) fail(FV_ERR_INVALID_ARG, std::string("NULL pointer: ") + what);
 }
 
 void validate_cfg(const fv_cfg& c) {

@@ -10,7 +10,8 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, c_char_p, c_float, c_int32, c_int64, c_uint64, c_void_p
+from ctypes import (POINTER, byref, c_char_p, c_float, c_int32, c_int64, c_size_t, c_uint64,
+                    c_void_p)
 from typing import Dict, Optional, Sequence
 
 import numpy as np
@@ -33,6 +34,9 @@ EXPORTED = (
     "fv_debug_stage", "fv_query", "fv_set_mask_mode", "fv_set_schedule", "fv_cold_start",
     "fv_get_valid_slots", "fv_set_valid_slots", "fv_multibuffer_velocity", "fv_set_prefix_async",
     "fv_decode_step_noalloc",
+    "fv_rope_append", "fv_prompt_attention", "fv_paged_attention_workspace", "fv_paged_attention",
+    "fv_pages_workspace", "fv_pages_grow", "fv_pages_fork", "fv_pages_free", "fv_pages_compact",
+    "fv_pages_gather", "fv_context_error",
 )
 
 
@@ -47,6 +51,38 @@ class FvWeights(ctypes.Structure):
     _fields_ = [(n, c_void_p) for n in ("w_in", "b_in", "w_t1", "b_t1", "w_t2", "b_t2")] + [
         (n, POINTER(c_void_p)) for n in ("w_mod", "b_mod", "wq", "wk", "wv", "wo", "wg", "wu",
                                          "wd")] + [("w_out", c_void_p), ("b_out", c_void_p)]
+
+
+class FvPages(ctypes.Structure):
+    _fields_ = [(n, c_int32) for n in ("dtype", "n_layers", "n_kv_heads", "head_dim", "page_len",
+                                       "n_pages", "max_seqs", "max_pages")] + [
+        (n, c_void_p) for n in ("k", "v", "table", "len", "refs")]
+
+
+class FvRopeArgs(ctypes.Structure):
+    _fields_ = [(n, c_void_p) for n in ("q", "k", "v", "q_out", "k_out")] + [
+        (n, c_int32) for n in ("ldq", "ldk", "ldv", "ldq_out", "ldk_out")] + [
+        (n, c_void_p) for n in ("pos", "seqs", "at")] + [
+        (n, c_int32) for n in ("n", "n_q_heads", "n_kv_heads", "head_dim", "dtype", "layer",
+                               "n_axes")] + [("sections", c_int32 * 4), ("theta", c_float)]
+
+
+class FvPromptArgs(ctypes.Structure):
+    _fields_ = [(n, c_void_p) for n in ("q", "k", "v", "out")] + [
+        (n, c_int32) for n in ("ldq", "ldk", "ldv", "ldo")] + [
+        (n, c_void_p) for n in ("cu_q", "cu_k")] + [
+        (n, c_int32) for n in ("n_seqs", "n_q", "n_k", "n_q_heads", "n_kv_heads", "head_dim",
+                               "dtype", "causal")] + [("scale", c_float)]
+
+
+class FvPagedArgs(ctypes.Structure):
+    _fields_ = [("q", c_void_p), ("out", c_void_p), ("ldq", c_int32), ("ldo", c_int32),
+                ("seqs", c_void_p)] + [
+        (n, c_int32) for n in ("n", "n_q_heads", "layer", "max_len")] + [
+        ("scale", c_float), ("work", c_void_p), ("work_bytes", c_size_t)]
+
+
+FV_PAGES_OK, FV_PAGES_BAD, FV_PAGES_FULL = range(3)
 
 
 class FlashVLAError(RuntimeError):
@@ -94,6 +130,21 @@ def lib() -> ctypes.CDLL:
                                      c_void_p], S),
             "fv_multibuffer_velocity": ([H, c_void_p, c_void_p, c_int32, c_int32, c_void_p,
                                          c_void_p, c_void_p, c_void_p], S),
+            "fv_rope_append": ([POINTER(FvRopeArgs), POINTER(FvPages), c_void_p], S),
+            "fv_prompt_attention": ([POINTER(FvPromptArgs), c_void_p], S),
+            "fv_paged_attention_workspace": ([POINTER(FvPagedArgs), POINTER(FvPages),
+                                              POINTER(c_size_t)], S),
+            "fv_paged_attention": ([POINTER(FvPagedArgs), POINTER(FvPages), c_void_p], S),
+            "fv_pages_workspace": ([POINTER(FvPages), POINTER(c_size_t)], S),
+            "fv_pages_grow": ([POINTER(FvPages), c_void_p, c_void_p, c_int32, c_void_p, c_void_p,
+                               c_void_p], S),
+            "fv_pages_fork": ([POINTER(FvPages), c_void_p, c_void_p, c_int32, c_void_p, c_void_p,
+                               c_void_p], S),
+            "fv_pages_free": ([POINTER(FvPages), c_void_p, c_int32, c_void_p, c_void_p], S),
+            "fv_pages_compact": ([POINTER(FvPages), c_void_p, c_void_p, c_void_p], S),
+            "fv_pages_gather": ([POINTER(FvPages), c_void_p, c_int32, c_int32, c_void_p, c_void_p,
+                                 c_void_p], S),
+            "fv_context_error": ([], c_char_p),
         }
         for name, (args, res) in sig.items():
             fn = getattr(L, name)
@@ -370,3 +421,254 @@ class Expert:
             self.close()
         except Exception:
             pass
+
+
+# ------------------------------------------------------- observation context
+
+def _check_context(status: int, what: str) -> None:
+    if status != FV_OK:
+        txt = lib().fv_status_string(status).decode()
+        raise FlashVLAError(status, f"{what}: {txt}: {lib().fv_context_error().decode()}")
+
+
+def _refuse(message: str):
+    raise FlashVLAError(FV_ERR_INVALID_ARG, message)
+
+
+def _dtype(t, what: str) -> int:
+    name = str(t.dtype)
+    if name == "torch.bfloat16":
+        return FV_BF16
+    if name != "torch.float32":
+        _refuse(f"{what} must be bfloat16 or float32, not {name}")
+    return FV_FP32
+
+
+def _rows(t, what: str, like=None, shape=None) -> int:
+    """Leading dimension of a [tokens, heads, head_dim] tensor whose heads lie side by side."""
+    if like is not None and (t.dtype != like.dtype or t.device != like.device):
+        _refuse(f"{what} must have dtype {like.dtype} on {like.device}")
+    if t.dim() != 3 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        _refuse(f"{what} has shape {tuple(t.shape)}" + (f", not {tuple(shape)}" if shape else ""))
+    n, h, d = t.shape
+    st = t.stride()
+    if (d > 1 and st[2] != 1) or (h > 1 and st[1] != d):
+        _refuse(f"the heads of {what} must lie side by side (strides {st})")
+    return st[0] if n > 1 else h * d
+
+
+def _int32(t, what: str, device, shape=None) -> int:
+    """Pointer of a dense int32 tensor."""
+    if str(t.dtype) != "torch.int32" or t.device != device or not t.is_contiguous():
+        _refuse(f"{what} must be a contiguous int32 tensor on {device}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        _refuse(f"{what} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    return t.data_ptr()
+
+
+class _On:
+    """The GPU of a tensor and the stream of a call, for its duration: the C calls
+    take the NULL stream to be the current GPU's, and a workspace has to come from
+    the allocator's pool of the stream that uses it."""
+
+    def __init__(self, device, stream):
+        import torch
+        if device.type != "cuda":
+            _refuse(f"tensors must be on a GPU, not {device}")
+        self.device, self.given, self.scope = device, stream is not None, None
+        if stream is None:
+            self.stream = torch.cuda.current_stream(device)
+        elif isinstance(stream, torch.cuda.Stream):
+            self.stream = stream
+        else:
+            self.stream = torch.cuda.ExternalStream(int(stream), device=device)
+        if self.given and self.stream.device != device:
+            _refuse(f"the stream is of {self.stream.device}, the tensors of {device}")
+        self.raw = int(self.stream.cuda_stream)
+
+    def __enter__(self):
+        import torch
+        if self.given:
+            self.scope = torch.cuda.stream(self.stream)
+        elif torch.cuda.current_device() != self.device.index:
+            self.scope = torch.cuda.device(self.device)
+        if self.scope is not None:
+            self.scope.__enter__()
+        return self
+
+    def __exit__(self, *exc):
+        if self.scope is not None:
+            self.scope.__exit__(*exc)
+        return False
+
+    def work(self, nbytes: int):
+        import torch
+        return torch.empty(nbytes, dtype=torch.uint8, device=self.device) if nbytes else None
+
+
+def prompt_attention(q, k, v, cu_q, cu_k, out, causal: bool = True, scale: Optional[float] = None,
+                     stream=None) -> None:
+    """fv_prompt_attention on torch tensors: q and out [tokens, heads, head_dim], k and v
+    [keys, kv heads, head_dim] (rows may be strided), cu_q and cu_k int32 [prompts + 1].
+    `scale` defaults to 1/sqrt(head_dim)."""
+    dtype = _dtype(q, "q")
+    ldq = _rows(q, "q")
+    ldk, ldv = _rows(k, "k", q), _rows(v, "v", q, k.shape)
+    ldo = _rows(out, "out", q, q.shape)
+    n_q, heads, dh = q.shape
+    if k.shape[2] != dh:
+        _refuse(f"head_dim of q is {dh}, of k {k.shape[2]}")
+    if cu_q.dim() != 1 or len(cu_q) < 1:
+        _refuse("cu_q must have prompts + 1 entries")
+    with _On(q.device, stream) as on:
+        args = FvPromptArgs(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), ldq, ldk, ldv,
+                            ldo, _int32(cu_q, "cu_q", q.device),
+                            _int32(cu_k, "cu_k", q.device, cu_q.shape), len(cu_q) - 1, n_q,
+                            k.shape[0], heads, k.shape[1], dh, dtype, 1 if causal else 0,
+                            dh ** -0.5 if scale is None else scale)
+        _check_context(lib().fv_prompt_attention(byref(args), on.raw), "fv_prompt_attention")
+
+
+def rope(q, k, pos, sections: Sequence[int], q_out, k_out=None, theta: float = 10000.0,
+         stream=None) -> None:
+    """fv_rope_append without a cache: rotates q into q_out and, if given, k into k_out."""
+    _rope(None, 0, q, k, None, pos, None, None, sections, theta, q_out, k_out, stream)
+
+
+def _rope(cache, layer, q, k, v, pos, seqs, at, sections, theta, q_out, k_out, stream) -> None:
+    dtype = _dtype(q, "q")
+    n, heads, dh = q.shape if q.dim() == 3 else _refuse(f"q has shape {tuple(q.shape)}")
+    if k.dim() != 3 or k.shape[0] != n or k.shape[2] != dh:
+        _refuse(f"k has shape {tuple(k.shape)}, q {tuple(q.shape)}")
+    ldq, ldk = _rows(q, "q"), _rows(k, "k", q)
+    ldv = _rows(v, "v", q, k.shape) if v is not None else 0
+    ldq_out = _rows(q_out, "q_out", q, q.shape)
+    ldk_out = _rows(k_out, "k_out", q, k.shape) if k_out is not None else 0
+    if not 1 <= len(sections) <= 4:
+        _refuse("sections must have 1 to 4 entries")
+    dev = q.device
+    args = FvRopeArgs(q.data_ptr(), k.data_ptr(), _ptr(v), q_out.data_ptr(), _ptr(k_out), ldq, ldk,
+                      ldv, ldq_out, ldk_out, _int32(pos, "pos", dev, (len(sections), n)),
+                      _int32(seqs, "seqs", dev, (n,)) if seqs is not None else None,
+                      _int32(at, "at", dev, (n,)) if at is not None else None, n, heads, k.shape[1],
+                      dh, dtype, layer, len(sections), (c_int32 * 4)(*sections), theta)
+    with _On(dev, stream) as on:
+        _check_context(lib().fv_rope_append(byref(args), byref(cache) if cache is not None else None,
+                                            on.raw), "fv_rope_append")
+
+
+class PageCache:
+    """A paged cache of keys and values (fv_pages) over torch tensors that the caller
+    owns: k, v [layers, pages, kv heads, page_len, head_dim], table int32 [sequences,
+    pages of a sequence], length int32 [sequences], refs int32 [pages].  The object
+    holds the tensors and nothing else; every call is stream-ordered and may be
+    captured into a HIP graph."""
+
+    def __init__(self, k, v, table, length, refs):
+        dtype = _dtype(k, "k")
+        if k.dim() != 5 or not k.is_contiguous():
+            _refuse("k must be contiguous [layers, pages, kv heads, page_len, head_dim]")
+        if v.shape != k.shape or v.dtype != k.dtype or v.device != k.device or not v.is_contiguous():
+            _refuse("v must be as k")
+        if table.dim() != 2:
+            _refuse("table must be [sequences, pages of a sequence]")
+        layers, pages, heads, page_len, dh = k.shape
+        dev = k.device
+        self.k, self.v, self.table, self.length, self.refs = k, v, table, length, refs
+        self.c = FvPages(dtype, layers, heads, dh, page_len, pages, table.shape[0], table.shape[1],
+                         k.data_ptr(), v.data_ptr(), _int32(table, "table", dev),
+                         _int32(length, "length", dev, table.shape[:1]),
+                         _int32(refs, "refs", dev, (pages,)))
+
+    @classmethod
+    def empty(cls, n_layers: int, n_kv_heads: int, head_dim: int, n_pages: int, max_seqs: int,
+              max_pages: int, page_len: int = 16, dtype=None, device="cuda"):
+        """A fresh cache: uninitialised pages, no sequences."""
+        import torch
+        dtype = torch.bfloat16 if dtype is None else dtype
+        shape = (n_layers, n_pages, n_kv_heads, page_len, head_dim)
+        k, v = (torch.empty(shape, dtype=dtype, device=device) for _ in range(2))
+        i32 = dict(dtype=torch.int32, device=device)
+        return cls(k, v, torch.full((max_seqs, max_pages), -1, **i32), torch.zeros(max_seqs, **i32),
+                   torch.zeros(n_pages, **i32))
+
+    def append(self, layer: int, q, k, v, pos, seqs, at, sections: Sequence[int],
+               theta: float = 10000.0, q_out=None, k_out=None, stream=None) -> None:
+        """fv_rope_append: rotates q into q_out (default: q itself) and k into the pages
+        (and k_out, if given), and stores v."""
+        if v is None or seqs is None or at is None:
+            _refuse("append needs v, seqs and at")
+        _rope(self.c, layer, q, k, v, pos, seqs, at, sections, theta, q if q_out is None else q_out,
+              k_out, stream)
+
+    def attend(self, layer: int, q, seqs, out, scale: Optional[float] = None, max_len: int = 0,
+               stream=None) -> None:
+        """fv_paged_attention: q and out [rows, heads, head_dim], seqs int32 [rows]."""
+        ldq, ldo = _rows(q, "q", self.k), _rows(out, "out", self.k, q.shape)
+        n, heads, dh = q.shape
+        if dh != self.c.head_dim:
+            _refuse(f"head_dim of q is {dh}, of the cache {self.c.head_dim}")
+        with _On(q.device, stream) as on:
+            args = FvPagedArgs(q.data_ptr(), out.data_ptr(), ldq, ldo,
+                               _int32(seqs, "seqs", q.device, (n,)), n, heads, layer, max_len,
+                               dh ** -0.5 if scale is None else scale, None, 0)
+            need = c_size_t()
+            L = lib()
+            _check_context(L.fv_paged_attention_workspace(byref(args), byref(self.c), byref(need)),
+                           "fv_paged_attention")
+            work = on.work(need.value)
+            if work is not None:
+                args.work, args.work_bytes = work.data_ptr(), need.value
+            _check_context(L.fv_paged_attention(byref(args), byref(self.c), on.raw),
+                           "fv_paged_attention")
+
+    def _upkeep(self, name: str, stream, *lists, status=None, work=True):
+        import torch
+        dev = self.k.device
+        n = lists[0].shape[0] if lists else 0
+        ptrs = [_int32(t, name + " list", dev, (n,)) for t in lists]
+        with _On(dev, stream) as on:
+            if status is None:
+                status = torch.empty(1, dtype=torch.int32, device=dev)
+            args = [byref(self.c), *ptrs, *([n] if lists else []),
+                    _int32(status, "status", dev, (1,))]
+            L = lib()
+            if work:
+                need = c_size_t()
+                _check_context(L.fv_pages_workspace(byref(self.c), byref(need)), name)
+                buf = on.work(need.value)
+                args.append(buf.data_ptr())
+            _check_context(getattr(L, name)(*args, on.raw), name)
+        return status
+
+    def grow(self, seqs, add, status=None, stream=None):
+        """fv_pages_grow; returns the status tensor (int32 [1]: FV_PAGES_*)."""
+        return self._upkeep("fv_pages_grow", stream, seqs, add, status=status)
+
+    def fork(self, parents, children, status=None, stream=None):
+        """fv_pages_fork; returns the status tensor."""
+        return self._upkeep("fv_pages_fork", stream, parents, children, status=status)
+
+    def free(self, seqs, status=None, stream=None):
+        """fv_pages_free; returns the status tensor."""
+        return self._upkeep("fv_pages_free", stream, seqs, status=status, work=False)
+
+    def compact(self, used=None, stream=None):
+        """fv_pages_compact; returns the number of pages in use (int32 [1])."""
+        return self._upkeep("fv_pages_compact", stream, status=used)
+
+    def gather(self, seqs, k_out, v_out, stream=None) -> None:
+        """fv_pages_gather: k_out and v_out [layers, entries, ld, kv heads, head_dim], as
+        Expert.set_prefix takes them."""
+        c, dev = self.c, self.k.device
+        for t, what in ((k_out, "k_out"), (v_out, "v_out")):
+            if t.dim() != 5 or t.dtype != self.k.dtype or t.device != dev or not t.is_contiguous():
+                _refuse(f"{what} must be contiguous [layers, entries, ld, kv heads, head_dim]")
+            if t.shape[0] != c.n_layers or tuple(t.shape[3:]) != (c.n_kv_heads, c.head_dim):
+                _refuse(f"{what} has shape {tuple(t.shape)}")
+        if k_out.shape != v_out.shape:
+            _refuse("k_out and v_out must have the same shape")
+        with _On(dev, stream) as on:
+            _check_context(lib().fv_pages_gather(byref(c), _int32(seqs, "seqs", dev, k_out.shape[1:2]),
+                                                 k_out.shape[1], k_out.shape[2], k_out.data_ptr(),
+                                                 v_out.data_ptr(), on.raw), "fv_pages_gather")

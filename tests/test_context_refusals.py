@@ -1,0 +1,192 @@
+"""What the observation context's operators refuse: at the C boundary from the
+arguments alone (no GPU is touched), and in the binding from the tensors'
+shapes, types and strides."""
+import ctypes
+
+import pytest
+
+from paper_2608_27384_amd import flashvla as fvb
+
+P = 1 << 20  # an aligned address that is never read
+
+
+def cache(**kw):
+    c = fvb.FvPages(fvb.FV_BF16, 2, 2, 64, 16, 10, 4, 3, P, P, P, P, P)
+    for k, v in kw.items():
+        setattr(c, k, v)
+    return c
+
+
+def rope_args(**kw):
+    a = fvb.FvRopeArgs(P, P << 1, P << 2, P << 3, P << 4, 256, 128, 128, 256, 128, P, P, P, 5, 4, 2, 64,
+                       fvb.FV_BF16, 0, 3, (ctypes.c_int32 * 4)(8, 12, 12), 1e4)
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return a
+
+
+def prompt_args(**kw):
+    a = fvb.FvPromptArgs(P, P << 1, P << 2, P << 3, 256, 128, 128, 256, P, P, 2, 9, 9, 4, 2, 64,
+                         fvb.FV_BF16, 1, 0.125)
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return a
+
+
+def paged_args(**kw):
+    a = fvb.FvPagedArgs(P, P << 1, 256, 256, P, 3, 4, 0, 0, 0.125, None, 0)
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return a
+
+
+def refused(st, word=""):
+    assert st == fvb.FV_ERR_INVALID_ARG
+    msg = fvb.lib().fv_context_error().decode()
+    assert msg and word in msg, msg
+
+
+def test_structures_match_the_header():
+    assert ctypes.sizeof(fvb.FvPages) == 32 + 5 * 8
+    assert ctypes.sizeof(fvb.FvRopeArgs) == 5 * 8 + 24 + 3 * 8 + 12 * 4
+    assert ctypes.sizeof(fvb.FvPromptArgs) == 4 * 8 + 16 + 16 + 9 * 4 + 4
+    assert ctypes.sizeof(fvb.FvPagedArgs) == 16 + 8 + 8 + 16 + 8 + 8 + 8
+
+
+CACHES = [("dtype", 2), ("dtype", -1), ("n_layers", 0), ("n_layers", 1025), ("n_kv_heads", 0),
+          ("head_dim", 80), ("page_len", 8), ("page_len", 24), ("page_len", 272), ("page_len", 0),
+          ("n_pages", 0), ("n_pages", (1 << 20) + 1), ("max_seqs", 0), ("max_seqs", 65537),
+          ("max_pages", 0), ("max_pages", 65537), ("k", None), ("v", P + 8), ("table", None),
+          ("len", P + 2), ("refs", None)]
+
+
+@pytest.mark.parametrize("field,value", CACHES)
+def test_caches(field, value):
+    L, c = fvb.lib(), cache(**{field: value})
+    b, n = ctypes.byref(c), ctypes.c_size_t()
+    refused(L.fv_pages_workspace(b, ctypes.byref(n)))
+    refused(L.fv_pages_grow(b, P, P, 1, P, P, None))
+    refused(L.fv_pages_fork(b, P, P, 1, P, P, None))
+    refused(L.fv_pages_free(b, P, 1, P, None))
+    refused(L.fv_pages_compact(b, P, P, None))
+    refused(L.fv_pages_gather(b, P, 1, 5, P, P, None))
+    refused(L.fv_paged_attention(ctypes.byref(paged_args()), b, None))
+    refused(L.fv_rope_append(ctypes.byref(rope_args()), b, None))
+
+
+@pytest.mark.parametrize("kw", [
+    dict(dtype=3), dict(head_dim=32), dict(n_q_heads=3), dict(n_q_heads=0), dict(n_q_heads=1026),
+    dict(n=-1), dict(n_axes=0), dict(n_axes=5), dict(sections=(ctypes.c_int32 * 4)(8, 12, 11)),
+    dict(sections=(ctypes.c_int32 * 4)(-8, 28, 12)), dict(theta=0.0), dict(theta=float("nan")),
+    dict(theta=float("inf")), dict(layer=2), dict(layer=-1), dict(n_kv_heads=1, ldk=64), dict(q=None),
+    dict(k=P + 4), dict(v=None), dict(q_out=None), dict(ldq=255), dict(ldq=248), dict(ldk=120),
+    dict(ldv=(1 << 20) + 8), dict(ldq_out=252), dict(ldk_out=64), dict(pos=None), dict(seqs=None),
+    dict(at=P + 1), dict(q_out=P + 64), dict(q_out=P << 1), dict(k_out=P << 2), dict(k_out=P << 3),
+    dict(q_out=P, ldq_out=264), dict(dtype=fvb.FV_FP32)], ids=str)
+def test_rope(kw):
+    refused(fvb.lib().fv_rope_append(ctypes.byref(rope_args(**kw)), ctypes.byref(cache()), None))
+
+
+@pytest.mark.parametrize("kw", [
+    dict(dtype=2), dict(head_dim=512), dict(n_q_heads=5), dict(n_kv_heads=0), dict(n_seqs=-1),
+    dict(n_seqs=65537), dict(n_q=-1), dict(n_k=-1), dict(causal=2), dict(scale=0.0), dict(scale=-1.0),
+    dict(scale=float("inf")), dict(scale=float("nan")), dict(q=None), dict(k=None), dict(v=P + 2),
+    dict(out=None), dict(ldq=128), dict(ldk=130), dict(ldo=(1 << 20) + 8), dict(cu_q=None),
+    dict(cu_k=P + 3), dict(out=P), dict(out=(P << 1) + 1024), dict(out=P << 2),
+    dict(n_q=1 << 30)], ids=str)
+def test_prompts(kw):
+    refused(fvb.lib().fv_prompt_attention(ctypes.byref(prompt_args(**kw)), None))
+
+
+@pytest.mark.parametrize("kw", [
+    dict(n=-1), dict(n=65537), dict(n_q_heads=3), dict(max_len=-1), dict(layer=2), dict(scale=0.0),
+    dict(q=None), dict(out=P + 8), dict(out=P + 512), dict(ldq=128), dict(ldo=260), dict(seqs=None)],
+    ids=str)
+def test_paged(kw):
+    refused(fvb.lib().fv_paged_attention(ctypes.byref(paged_args(**kw)), ctypes.byref(cache()), None))
+
+
+def test_paged_workspace_too_small():
+    L, c = fvb.lib(), cache(max_pages=4000)
+    n = ctypes.c_size_t()
+    a = paged_args()
+    assert L.fv_paged_attention_workspace(ctypes.byref(a), ctypes.byref(c), ctypes.byref(n)) == 0
+    assert n.value > 0
+    refused(L.fv_paged_attention(ctypes.byref(a), ctypes.byref(c), None), "work")
+    a = paged_args(work=P << 4, work_bytes=n.value - 1)
+    refused(L.fv_paged_attention(ctypes.byref(a), ctypes.byref(c), None), "work")
+
+
+def test_lists():
+    L, c = fvb.lib(), cache()
+    b = ctypes.byref(c)
+    for n in (-1, 5):
+        refused(L.fv_pages_grow(b, P, P, n, P, P, None))
+        refused(L.fv_pages_fork(b, P, P, n, P, P, None))
+        refused(L.fv_pages_free(b, P, n, P, None))
+    refused(L.fv_pages_grow(b, P, None, 1, P, P, None))
+    refused(L.fv_pages_grow(b, P, P, 1, None, P, None))
+    refused(L.fv_pages_grow(b, P, P, 1, P, P + 4, None))
+    refused(L.fv_pages_fork(b, None, P, 1, P, P, None))
+    refused(L.fv_pages_free(b, P + 1, 1, P, None))
+    refused(L.fv_pages_compact(b, None, P, None))
+    refused(L.fv_pages_compact(b, P, None, None))
+    refused(L.fv_pages_gather(b, P, -1, 5, P, P, None))
+    refused(L.fv_pages_gather(b, P, 1, -5, P, P, None))
+    refused(L.fv_pages_gather(b, P, 1, 5, P + 8, P, None))
+
+
+def test_null_arguments_and_the_message():
+    L = fvb.lib()
+    assert L.fv_rope_append(None, None, None) == fvb.FV_ERR_INVALID_ARG
+    assert L.fv_prompt_attention(None, None) == fvb.FV_ERR_INVALID_ARG
+    assert L.fv_paged_attention(None, None, None) == fvb.FV_ERR_INVALID_ARG
+    assert L.fv_pages_workspace(None, None) == fvb.FV_ERR_INVALID_ARG
+    assert b"NULL" in L.fv_context_error()
+    # calls of nothing touch no GPU and succeed
+    assert L.fv_prompt_attention(ctypes.byref(prompt_args(n_q=0, q=None)), None) == 0
+    assert L.fv_paged_attention(ctypes.byref(paged_args(n=0)), ctypes.byref(cache()), None) == 0
+    assert L.fv_rope_append(ctypes.byref(rope_args(n=0)), None, None) == 0
+    assert L.fv_context_error() == b""
+
+
+def test_binding_refuses_tensors():
+    torch = pytest.importorskip("torch")
+    q, k = torch.zeros(3, 4, 64), torch.zeros(3, 2, 64)
+    cu = torch.tensor([0, 3], dtype=torch.int32)
+
+    def no(fn, *a, **kw):
+        with pytest.raises(fvb.FlashVLAError) as e:
+            fn(*a, **kw)
+        assert e.value.status == fvb.FV_ERR_INVALID_ARG
+
+    pa = fvb.prompt_attention
+    no(pa, q, k, k.clone(), cu, cu, torch.zeros_like(q))  # not on a GPU
+    no(pa, q.half(), k, k, cu, cu, q)
+    no(pa, q, k.bfloat16(), k, cu, cu, q)
+    no(pa, q, k, k[:2], cu, cu, q)
+    no(pa, q, k, k, cu, cu, q[:, :2])
+    no(pa, q.transpose(0, 1), k, k, cu, cu, q)
+    no(pa, q, k[..., :32], k[..., :32], cu, cu, q)
+    pool, refs = torch.zeros(2, 10, 2, 16, 64), torch.zeros(10, dtype=torch.int32)
+    table, length = torch.zeros(4, 3, dtype=torch.int32), torch.zeros(4, dtype=torch.int32)
+    c = fvb.PageCache(pool, pool.clone(), table, length, refs)
+    no(fvb.PageCache, pool, pool[:1], table, length, refs)
+    no(fvb.PageCache, pool.half(), pool.half(), table, length, refs)
+    no(fvb.PageCache, pool, pool.clone(), table.long(), length, refs)
+    no(fvb.PageCache, pool, pool.clone(), table, length[:3], refs)
+    no(fvb.PageCache, pool, pool.clone(), table, length, refs[:9])
+    seqs = torch.zeros(3, dtype=torch.int32)
+    no(c.attend, 0, q, seqs, q.clone())
+    no(c.attend, 0, q.bfloat16(), seqs, q.bfloat16())
+    no(c.attend, 0, q, seqs.long(), q.clone())
+    no(c.attend, 0, q, seqs[:2], q.clone())
+    no(c.grow, seqs, seqs[:2])
+    no(c.grow, seqs, seqs)
+    no(c.gather, seqs, torch.zeros(2, 3, 5, 2, 64), torch.zeros(2, 3, 6, 2, 64))
+    no(c.gather, seqs, torch.zeros(1, 3, 5, 2, 64), torch.zeros(1, 3, 5, 2, 64))
+    pos = torch.zeros(3, 3, dtype=torch.int32)
+    no(c.append, 0, q, k, None, pos, seqs, seqs, (8, 12, 12))
+    no(c.append, 0, q, k, k, pos[:2], seqs, seqs, (8, 12, 12))
+    no(c.append, 0, q, k, k, pos, seqs, seqs, (8, 8, 4, 4, 8))
+    no(fvb.rope, q, k[:2], pos, (8, 12, 12), q)

@@ -1,0 +1,183 @@
+"""Prompt attention against the 64-bit form: packed lengths from zero to several
+tiles, keys longer and shorter than the queries, every head dim, grouped heads,
+strided rows; what a query does not see has no influence; refusals leave no
+trace."""
+import numpy as np
+import pytest
+
+import context_util as cu
+
+pytestmark = pytest.mark.gpu
+
+SHAPES = [("bf16", 8, 1, 256), ("bf16", 8, 2, 128), ("bf16", 4, 4, 64), ("bf16", 6, 2, 192),
+          ("bf16", 5, 1, 128), ("fp32", 4, 2, 64), ("fp32", 2, 1, 256), ("fp32", 3, 3, 192),
+          ("fp32", 8, 2, 128)]
+# (queries, keys) of each prompt
+LENS = {"ragged": [(0, 0), (1, 1), (33, 33), (64, 64), (65, 65), (0, 5), (130, 130), (7, 7)],
+        "tails": [(1, 300), (5, 64), (32, 97), (3, 3), (100, 517)],
+        "empty_rows": [(9, 4), (70, 33), (5, 0), (40, 40), (1, 0)],
+        "long": [(700, 700), (31, 950)]}
+
+
+def make(shape, lens, seed=0):
+    dtype, H, G, D = shape
+    nq, nk = sum(a for a, _ in lens), sum(b for _, b in lens)
+    q, k, v = (cu.randn(dtype, seed + i, n, h, D) for i, (n, h) in
+               enumerate(((nq, H), (nk, G), (nk, G))))
+    cq = np.cumsum([0] + [a for a, _ in lens])
+    ck = np.cumsum([0] + [b for _, b in lens])
+    return q, k, v, cq, ck
+
+
+def run(q, k, v, cq, ck, causal, out=None, **kw):
+    from paper_2608_27384_amd.flashvla import prompt_attention
+    torch = cu.torch_mod()
+    out = torch.full_like(q, 7.0) if out is None else out
+    prompt_attention(q, k, v, cu.ints(cq), cu.ints(ck), out, causal=causal, **kw)
+    torch.cuda.synchronize()
+    return out
+
+
+def limits(nq, nk, causal):
+    return [max(0, min(nk, nk - nq + i + 1)) if causal else nk for i in range(nq)]
+
+
+def check(shape, out, q, k, v, cq, ck, causal, scale=None):
+    for b in range(len(cq) - 1):
+        nq, nk = cq[b + 1] - cq[b], ck[b + 1] - ck[b]
+        ref = cu.attention(q[cq[b]:cq[b + 1]], k[ck[b]:ck[b + 1]], v[ck[b]:ck[b + 1]],
+                           limits(nq, nk, causal), scale)
+        cu.check_attention(out[cq[b]:cq[b + 1]], ref, shape[0])
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("lens", LENS, ids=str)
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_against_the_definition(shape, lens, causal):
+    q, k, v, cq, ck = make(shape, LENS[lens])
+    out = run(q, k, v, cq, ck, causal)
+    check(shape, out, q, k, v, cq, ck, causal)
+    if lens == "empty_rows":
+        assert not out[cq[2]:cq[3]].any() and not out[cq[4]:].any()
+        if causal:
+            assert not out[:5].any()
+
+
+@pytest.mark.parametrize("shape", [SHAPES[1], SHAPES[3], SHAPES[5]], ids=str)
+def test_strided_rows_and_rows_behind_the_last_prompt(shape):
+    torch = cu.torch_mod()
+    dtype, H, G, D = shape
+    n = 203
+    qkv = cu.randn(dtype, 3, n + 9, (H + 2 * G) * D + 32)
+    q = qkv[:, :H * D].unflatten(1, (H, D))
+    k = qkv[:, H * D:(H + G) * D].unflatten(1, (G, D))
+    v = qkv[:, (H + G) * D:(H + 2 * G) * D].unflatten(1, (G, D))
+    wide = torch.full((n + 9, H * D + 16), 7.0, dtype=q.dtype, device="cuda")
+    out = wide[:, :H * D].unflatten(1, (H, D))
+    cq = [0, 120, n]
+    run(q, k, v, cq, cq, True, out)
+    check(shape, out, q, k, v, cq, cq, True)
+    assert (wide[n:] == 7).all() and (wide[:, H * D:] == 7).all()
+
+
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+@pytest.mark.parametrize("where", ["k", "v"])
+@pytest.mark.parametrize("shape", [SHAPES[0], SHAPES[1], SHAPES[2], SHAPES[3], SHAPES[6]], ids=str)
+def test_unseen_keys_have_no_influence(shape, where, bad):
+    """A key or value that is not finite changes only the rows that see it, bit for bit."""
+    torch = cu.torch_mod()
+    dtype, H, G, D = shape
+    lens = [(90, 90), (150, 170), (40, 40)]
+    q, k, v, cq, ck = make(shape, lens)
+    clean = run(q, k, v, cq, ck, True)
+    x = {"k": k, "v": v}[where]
+    x[ck[1] + 100] = bad           # seen by the rows from 80 of prompt 1 on
+    x[ck[2] - 1, :, :3] = bad      # seen by the last row of prompt 1
+    x[ck[3] - 1] = bad             # seen by the last row of prompt 2
+    out = run(q, k, v, cq, ck, True)
+    hidden = torch.ones(cq[-1], dtype=torch.bool, device="cuda")
+    hidden[cq[1] + 80:cq[2]] = False
+    hidden[-1] = False
+    assert torch.equal(out[hidden], clean[hidden])
+    if where == "v":
+        seen = out[cq[1] + 80:cq[2] - 1]
+        assert (seen.isnan() if np.isnan(bad) else seen == bad).all()
+        assert (out[-1].isnan() if np.isnan(bad) else out[-1] == bad).all()
+    elif np.isnan(bad):
+        assert out[cq[1] + 80:cq[2]].isnan().all()
+
+
+@pytest.mark.parametrize("shape", [SHAPES[0], SHAPES[2], SHAPES[5]], ids=str)
+def test_scores_without_a_softmax_and_rising_ones(shape):
+    torch = cu.torch_mod()
+    dtype, H, G, D = shape
+    n = 300
+    q, k, v, cq, ck = make(shape, [(n, n)])
+    q[:, :, 0] = 1.0
+    # a first run of keys that weigh nothing, then scores that rise by 300 over the prompt
+    k[:, :, 0] = torch.linspace(0, 300 * D ** 0.5, n, device="cuda").to(k.dtype)[:, None]
+    k[:70, :, 0] = -np.inf
+    out = run(q, k, v, cq, ck, True)
+    assert out[:70].isnan().all()
+    k2 = k.clone()
+    k2[:70, :, 0] = 0
+    ref = torch.cat([cu.attention(q[i:i + 1], k2[70:i + 1], v[70:i + 1], [i - 69])[0]
+                     for i in range(70, n, 23)])
+    size = cu.attention(q, k2, v, limits(n, n, True))
+    got = out[70:n:23]
+    # products up to 300 sqrt(D): scores in fp32 are off by at most S of the definition's bound
+    tol = (2.0 ** -7 if dtype == "bf16" else 0) + float((size[2] / size[1].clamp(min=1e-30)).max())
+    assert float((got.double() - ref).abs().max()) <= tol * float(v.double().abs().max())
+
+
+def test_many_short_prompts():
+    """More prompts than one step of the search looks at, some empty."""
+    shape = ("bf16", 4, 2, 64)
+    lens = [(i * 7 % 4, i * 7 % 4) for i in range(5000)]
+    q, k, v, cq, ck = make(shape, lens)
+    out = run(q, k, v, cq, ck, True)
+    for b in list(range(0, 5000, 311)) + [1, 2, 3, 4997, 4998, 4999]:
+        if lens[b][0]:
+            sl = slice(cq[b], cq[b + 1])
+            ref = cu.attention(q[sl], k[sl], v[sl], limits(*lens[b], True))
+            cu.check_attention(out[sl], ref, "bf16")
+    assert not (out == 7).all(-1).any()
+
+
+def test_scale_and_no_rows():
+    torch = cu.torch_mod()
+    shape = SHAPES[1]
+    q, k, v, cq, ck = make(shape, [(50, 80)])
+    check(shape, run(q, k, v, cq, ck, False, scale=0.3), q, k, v, cq, ck, False, 0.3)
+    out = run(q, k, v, [0], [0], True)
+    assert (out == 7).all()
+    out = run(q, k, v, [0, 0, 0], [0, 0, 80], True)
+    assert (out == 7).all()
+
+
+def test_replayed_graph_and_other_stream():
+    torch = cu.torch_mod()
+    from paper_2608_27384_amd.flashvla import prompt_attention
+    shape = SHAPES[0]
+    q, k, v, cq, ck = make(shape, [(100, 100), (61, 90)])
+    dq, dk = cu.ints(cq), cu.ints(ck)
+    want = run(q, k, v, cq, ck, True)
+    out = torch.zeros_like(q)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        prompt_attention(q, k, v, dq, dk, out)
+    for i in range(3):
+        out.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+    q.mul_(0.5)  # the graph reads what the tensors hold when it runs
+    want = run(q, k, v, cq, ck, True)
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    prompt_attention(q, k, v, dq, dk, out, stream=s)
+    s.synchronize()
+    assert torch.equal(out, want)
