@@ -14,6 +14,8 @@
 // LDS tile by transposing reads.
 #include "fv_context.h"
 
+#include <type_traits>
+
 namespace fv {
 namespace {
 
@@ -71,51 +73,71 @@ __device__ __forceinline__ float other_half_sum(float x) {
   return __uint_as_float(a[0]) + __uint_as_float(a[1]);
 }
 
-// Value operands of keys that only some rows of a wave see.  A weight of zero
-// does not silence a value that is not finite, so such values are taken out of
-// the product; `plus` and `minus` hold a one for +inf and -inf, both for NaN.
-struct Unruly {
-  u32x4 plus, minus;
-};
-__device__ __forceinline__ bool has_unruly(u32x4 x, bf16_t) {
-  uint32_t any = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    any |= ((x[i] & 0x7f80u) == 0x7f80u) | ((x[i] & 0x7f800000u) == 0x7f800000u);
-  return __any(any);
-}
-__device__ __forceinline__ Unruly take_unruly(u32x4& x, bf16_t) {
-  Unruly u;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    uint32_t keep = 0, plus = 0, minus = 0;
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const uint32_t b = x[i] >> (16 * half) & 0xffffu;
-      const bool bad = (b & 0x7f80u) == 0x7f80u, nan = (b & 0x7fffu) > 0x7f80u;
-      keep |= (bad ? 0u : b) << (16 * half);
-      plus |= (bad && (nan || b == 0x7f80u) ? 0x3f80u : 0u) << (16 * half);
-      minus |= (bad && (nan || b == 0xff80u) ? 0x3f80u : 0u) << (16 * half);
-    }
-    x[i] = keep;
-    u.plus[i] = plus;
-    u.minus[i] = minus;
-  }
-  return u;
-}
-// Adds what the seen ones among them make of the sums: an infinity, or NaN.
-__device__ __forceinline__ void add_unruly(f32x16& o, const f32x16& plus, const f32x16& minus) {
-#pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    o[r] += plus[r] > 0.f ? INFINITY : 0.f;
-    o[r] -= minus[r] > 0.f ? INFINITY : 0.f;
-  }
-}
 __device__ __forceinline__ f32x16 zeros16() {
   f32x16 z;
 #pragma unroll
   for (int r = 0; r < 16; ++r) z[r] = 0.f;
   return z;
+}
+
+// Values at the edge, where a wave's rows differ in what they see.  A weight of
+// zero does not silence a value that is not finite, so such values are taken out
+// of the product there; afterwards, products of ones in their place (for +inf, for
+// -inf, for both where the value is NaN) with the rows' view say which sums they
+// make infinite.
+__device__ __forceinline__ bool is_unruly(u32x4 x, bf16_t) {
+  bool any = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    any |= (x[i] & 0x7f80u) == 0x7f80u || (x[i] & 0x7f800000u) == 0x7f800000u;
+  return any;
+}
+__device__ __forceinline__ bool is_unruly(float x, float) { return !(fabsf(x) < INFINITY); }
+// The operand without them.
+__device__ __forceinline__ u32x4 ruly(u32x4 x, bf16_t) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if ((x[i] & 0x7f80u) == 0x7f80u) x[i] &= 0xffff0000u;
+    if ((x[i] & 0x7f800000u) == 0x7f800000u) x[i] &= 0x0000ffffu;
+  }
+  return x;
+}
+__device__ __forceinline__ float ruly(float x, float) { return is_unruly(x, x) ? 0.f : x; }
+// Ones for the values of SIGN times infinity, or NaN.
+template <int SIGN> __device__ __forceinline__ u32x4 ones_for(u32x4 x, bf16_t) {
+  u32x4 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    r[i] = 0;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const uint32_t b = x[i] >> (16 * half) & 0xffffu;
+      if ((b & 0x7fffu) > 0x7f80u || b == (SIGN > 0 ? 0x7f80u : 0xff80u)) r[i] |= 0x3f80u << (16 * half);
+    }
+  }
+  return r;
+}
+template <int SIGN> __device__ __forceinline__ float ones_for(float x, float) {
+  return x != x || x == SIGN * INFINITY ? 1.f : 0.f;
+}
+template <int SIGN> __device__ __forceinline__ void add_infinities(f32x16& o, const f32x16& seen) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) o[r] += seen[r] > 0.f ? SIGN * INFINITY : 0.f;
+}
+// For operand c of V (see vread) and a lane whose row sees the keys below lim.
+template <int SIGN>
+__device__ __forceinline__ void add_unruly(u32x4 v, int c, int key0, int lh, int lim, f32x16& o, bf16_t) {
+  u16x8 seen;
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    seen[e] = key0 + 16 * c + 8 * (e >> 2) + 4 * lh + (e & 3) < lim ? 0x3f80 : 0;
+  add_infinities<SIGN>(o, mma32(ones_for<SIGN>(v, bf16_t{}), __builtin_bit_cast(u32x4, seen), zeros16(),
+                                bf16_t{}));
+}
+template <int SIGN>
+__device__ __forceinline__ void add_unruly(float v, int c, int key0, int lh, int lim, f32x16& o, float) {
+  const float seen = key0 + 8 * (c >> 2) + 4 * lh + (c & 3) < lim ? 1.f : 0.f;
+  add_infinities<SIGN>(o, __builtin_amdgcn_mfma_f32_32x32x2f32(ones_for<SIGN>(v, v), seen, zeros16(), 0, 0, 0));
 }
 
 __device__ __forceinline__ int clamped(const int* cu, int s, int n) { return min(max(cu[s], 0), n); }
@@ -142,212 +164,311 @@ __device__ __forceinline__ int prompt_of(const PromptCall& a, int slot, int* fir
   return lo;
 }
 
-template <typename T, int DH> struct PromptTile {
-  static constexpr int KT = sizeof(T) == 2 ? 64 : 32;  // keys of a tile
-  static constexpr int PIECES = DH * (int)sizeof(T) / 16;
-  static constexpr int ROW = DH * (int)sizeof(T);
-  static constexpr int BYTES = KT * ROW;  // of K, and of V
-};
+// One workgroup's walk over the keys of its rows: RT 32-row tiles a wave (with
+// two, every operand read from LDS serves two products).
+template <typename T, int DH, int WAVES, int RT>
+struct Walk {
+  static constexpr int E = (int)sizeof(T);
+  static constexpr int KT = E == 2 && WAVES == 8 ? 64 : 32;    // keys of a tile
+  static constexpr int ROW = DH * E, PIECES = ROW / 16;
+  static constexpr int BYTES = KT * ROW;                       // of a K tile, and of a V tile
+  static constexpr int SW = E == 4 || DH % 128 == 0 ? 16 : 8;  // pieces that a swizzle permutes
+  static constexpr int R = 32 * RT * WAVES;                    // rows of a workgroup
+  static constexpr int ND = DH / 32;                           // 32-row tiles of O^T
+  static constexpr int NI = BYTES / 1024 / WAVES;              // direct loads of a wave per tensor and tile
+  static constexpr int NK = PIECES / 2;                        // K operands of 32 keys
+  static constexpr int PV = E == 2 ? 2 : 16;                   // V operands of 32 keys and 32 elements
+  static_assert(NI * 1024 * WAVES == BYTES && 32 * WAVES * ROW <= 4 * BYTES, "tile split");
+  typedef typename std::conditional<E == 2, u32x4, float>::type vop;
 
-template <typename T, int DH, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void prompt_kernel(PromptCall a) {
-  using G = PromptTile<T, DH>;
-  constexpr int KT = G::KT, PIECES = G::PIECES, ROW = G::ROW, BYTES = G::BYTES;
-  constexpr int R = 32 * WAVES;
-  constexpr int ND = DH / 32;                      // 32-row tiles of O^T
-  constexpr int NI = BYTES / 1024 / WAVES;         // direct loads of a wave per tensor and tile
-  constexpr int E = (int)sizeof(T);
-  static_assert(NI * 1024 * WAVES == BYTES && R * ROW <= 4 * BYTES, "tile split");
-  __shared__ __attribute__((aligned(1024))) unsigned char ring[4 * BYTES];
+  const PromptCall& a;
+  unsigned char* ring;  // two stages of K and V
+  int lane, wave, l32, lh, kh, q0, k0, nk, rows, row0, wrow, diff, tiles, kaddr, vaddr;
 
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int l32 = lane & 31, lh = lane >> 5;
-  // the heaviest tiles of a causal prompt, its last ones, go first
-  const int kh = blockIdx.x % a.n_kv, slot = a.n_slots - 1 - (int)(blockIdx.x / a.n_kv);
-  int first;
-  const int s = prompt_of<R>(a, slot, &first);
-  const int q0 = clamped(a.cu_q, s, a.n_q), k0 = clamped(a.cu_k, s, a.n_k);
-  const int nq = max(0, clamped(a.cu_q, s + 1, a.n_q) - q0);
-  const int nk = max(0, clamped(a.cu_k, s + 1, a.n_k) - k0);
-  const int rows = nq * a.group, row0 = (slot - first) * R;
-  if (row0 >= rows) return;
-
-  // visible keys [0, lim) of the lane's row, of the wave's first and last, of the block's last
-  const int wrow = row0 + 32 * wave;
-  const int diff = nk - nq + 1;
-  auto limit = [&](int row) {
+  __device__ __forceinline__ Walk(const PromptCall& call, unsigned char* lds) : a(call), ring(lds) {
+    lane = threadIdx.x & 63;
+    wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    l32 = lane & 31;
+    lh = lane >> 5;
+    // the heaviest tiles of a causal prompt, its last ones, go first
+    const int slot = a.n_slots - 1 - (int)(blockIdx.x / a.n_kv);
+    kh = blockIdx.x % a.n_kv;
+    int first;
+    const int s = prompt_of<R>(a, slot, &first);
+    q0 = clamped(a.cu_q, s, a.n_q);
+    k0 = clamped(a.cu_k, s, a.n_k);
+    const int nq = max(0, clamped(a.cu_q, s + 1, a.n_q) - q0);
+    nk = max(0, clamped(a.cu_k, s + 1, a.n_k) - k0);
+    rows = nq * a.group;
+    row0 = (slot - first) * R;
+    wrow = row0 + 32 * RT * wave;
+    diff = nk - nq + 1;
+    tiles = (limit(row0 + R - 1) + KT - 1) / KT;
+    // LDS addresses of the operands: one register each for K and V and a constant
+    // exclusive or (the swizzle), so that they cost an instruction and no registers.
+    kaddr = l32 * ROW + ((lh ^ swizzle<T, DH>(l32)) << 4);
+    const int i16 = lane & 15, r = 4 * lh + (i16 >> 2);
+    vaddr = E == 2 ? BYTES + r * ROW +
+                         (((2 * ((lane >> 4) & 1) + ((i16 >> 1) & 1)) ^ swizzle<T, DH>(r)) << 4) +
+                         (i16 & 1) * 8
+                   : BYTES + 4 * lh * ROW + (((l32 >> 2) ^ (lh << 3)) << 4) + (l32 & 3) * 4;
+  }
+  // A row sees the keys [0, limit), which do not fall from one row to the next.
+  __device__ __forceinline__ int limit(int row) const {
     return a.causal ? min(max(diff + min(row, rows - 1) / a.group, 0), nk) : nk;
-  };
-  const int row = min(wrow + l32, rows - 1), tok = row / a.group, head = kh * a.group + row - tok * a.group;
-  const int lim = limit(row);
-  const int full = limit(wrow), wend = wrow < rows ? limit(wrow + 31) : 0;
-  const int tiles = (limit(row0 + R - 1) + KT - 1) / KT;
-
-  u32x4 qf[PIECES / 2];
-  {
+  }
+  // The lane's query of row tile t, as products' operands, and its place in the output.
+  __device__ __forceinline__ long long query(int t, u32x4 (&qf)[NK]) const {
+    const int row = min(wrow + 32 * t + l32, rows - 1);
+    const int tok = row / a.group, head = kh * a.group + row - tok * a.group;
     const T* q = static_cast<const T*>(a.q) + (size_t)(q0 + tok) * a.ldq + head * DH;
 #pragma unroll
-    for (int p = 0; p < PIECES / 2; ++p)
+    for (int p = 0; p < NK; ++p)
       qf[p] = *reinterpret_cast<const u32x4*>(q + (2 * p + lh) * (16 / E));
+    return (long long)(q0 + tok) * a.ldo + head * DH;
   }
-
-  // Direct loads: slot u of a tile, 16 bytes, is piece u % PIECES of row u / PIECES.
-  const T* kbase = static_cast<const T*>(a.k) + (size_t)k0 * a.ldk + kh * DH;
-  const T* vbase = static_cast<const T*>(a.v) + (size_t)k0 * a.ldv + kh * DH;
-  auto issue = [&](int t, int stage) __attribute__((always_inline)) {
+  // Direct loads of key tile kt: slot u, 16 bytes, is piece u % PIECES of row u / PIECES.
+  __device__ __forceinline__ void issue(int kt, int stage) const {
     unsigned char* to = ring + stage * 2 * BYTES + wave * NI * 1024;
-    const lds_src ks = lds_source(kbase + (size_t)t * KT * a.ldk);
-    const lds_src vs = lds_source(vbase + (size_t)t * KT * a.ldv);
-    const int most = nk - 1 - t * KT;  // rows past the prompt's last repeat it
+    const lds_src ks = lds_source(static_cast<const T*>(a.k) + (size_t)(k0 + kt * KT) * a.ldk + kh * DH);
+    const lds_src vs = lds_source(static_cast<const T*>(a.v) + (size_t)(k0 + kt * KT) * a.ldv + kh * DH);
+    const int most = nk - 1 - kt * KT;  // rows past the prompt's last repeat it
+    int mine = lane;
+    asm volatile("" : "+v"(mine));  // not 2 NI offsets kept over the loop
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-      const int u = 64 * (NI * wave + i) + lane, r = u / PIECES;
+      const int u = 64 * (NI * wave + i) + mine, r = u / PIECES;
       const int c = (u % PIECES) ^ swizzle<T, DH>(r), rr = min(r, most);
       lds_dma16(ks, to + 1024 * i, rr * a.ldk * E + 16 * c, 0);
       lds_dma16(vs, to + BYTES + 1024 * i, rr * a.ldv * E + 16 * c, 0);
     }
-  };
-
-  f32x16 o[ND];
-#pragma unroll
-  for (int d = 0; d < ND; ++d)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
-  float m = -INFINITY, l = 0.f;  // l over the lane half's keys only
-
-  const int ksw = swizzle<T, DH>(l32);
-  if (tiles > 0) issue(0, 0);
-  for (int t = 0; t < tiles; ++t) {
-    // this wave's part of tile t has landed and its reads of tile t - 1 are
-    // done; past the barrier both hold for every wave
+  }
+  // Every wave's loads have landed, every wave's reads are done.
+  __device__ __forceinline__ void meet() const {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    if (t + 1 < tiles) issue(t + 1, (t + 1) & 1);
-    const unsigned char* sk = ring + (t & 1) * 2 * BYTES;
-    const unsigned char* sv = sk + BYTES;
+  }
+  __device__ __forceinline__ u32x4 kread(int base, int sub, int p) const {
+    return *reinterpret_cast<const u32x4*>(ring + (base ^ ((2 * p & (SW - 1)) << 4)) +
+                                           32 * sub * ROW + 2 * p / SW * SW * 16);
+  }
+  // Operand c of V for the elements from 32 d on of the head: 16 keys from 16 c on
+  // (bf16), the keys of score register c (fp32).
+  __device__ __forceinline__ vop vread(int base, int sub, int d, int c) const {
+    if constexpr (E == 2) {
+      const unsigned char* p = ring + (32 * sub + 16 * c) * ROW + 4 * d / SW * SW * 16;
+      const int x = base ^ ((4 * d & (SW - 1)) << 4);
+      const u32x2 lo = read_transposed(p + x), hi = read_transposed(p + (x ^ 32) + 8 * ROW);
+      return u32x4{lo[0], lo[1], hi[0], hi[1]};
+    } else {
+      const int j = c >> 2, r = c & 3;
+      const int x = base ^ ((8 * d & 15) << 4) ^ (r << 5) ^ ((j & 1) << 4);
+      return *reinterpret_cast<const float*>(ring + x + (32 * sub + 8 * j + r) * ROW + 8 * d / 16 * 256);
+    }
+  }
+  static __device__ __forceinline__ f32x16 product(vop v, const f32x16& p, const u32x4 (&pf)[2], int c,
+                                                   f32x16 o) {
+    if constexpr (E == 2)
+      return mma32(v, pf[c], o, T{});
+    else
+      return __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[c], o, 0, 0, 0);
+  }
+  // Scores of 32 keys to probabilities (pf: as bf16 operands), with the row's
+  // reference m and sum l; calls rescale(f) where the reference moves.
+  template <bool EDGE, typename Rescale>
+  __device__ __forceinline__ void softmax(f32x16& sc, int key0, int lim, float& m, float& l,
+                                          u32x4 (&pf)[2], Rescale rescale) const {
+    if (EDGE) {
 #pragma unroll
-    for (int sub = 0; sub < KT / 32; ++sub) {
-      const int key0 = t * KT + 32 * sub;
-      if (key0 >= wend) break;
-      f32x16 sc;
+      for (int r = 0; r < 16; ++r)
+        if (key0 + 8 * (r >> 2) + 4 * lh + (r & 3) >= lim) sc[r] = -INFINITY;
+    }
+    float top = sc[0];
 #pragma unroll
-      for (int r = 0; r < 16; ++r) sc[r] = 0.f;
+    for (int r = 1; r < 16; ++r) top = fmaxf(top, sc[r]);
+    top = other_half_max(top) * a.scale;
+    if (__any(top > m + kSlack)) {
+      const float now = fmaxf(m, top);
+      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - now);
+      m = now;
+      l *= f;
+      rescale(f);
+    }
+    const float ref = m == -INFINITY ? 0.f : -m;
 #pragma unroll
-      for (int p = 0; p < PIECES / 2; ++p) {
-        const u32x4 kf = *reinterpret_cast<const u32x4*>(sk + (32 * sub + l32) * ROW +
-                                                         (((2 * p + lh) ^ ksw) << 4));
-        sc = mma32(kf, qf[p], sc, T{});
-      }
-      const bool edge = key0 + 32 > full;  // some row of the wave does not see all 32 keys
-      if (edge) {
+    for (int r = 0; r < 16; ++r) {
+      sc[r] = __builtin_amdgcn_exp2f(fmaf(sc[r], a.scale, ref));
+      l += sc[r];
+    }
+    if constexpr (E == 2) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (key0 + 8 * (r >> 2) + 4 * lh + (r & 3) >= lim) sc[r] = -INFINITY;
-      }
-      float top = sc[0];
+      for (int c = 0; c < 2; ++c) {
+        u16x8 w;
 #pragma unroll
-      for (int r = 1; r < 16; ++r) top = fmaxf(top, sc[r]);
-      top = other_half_max(top) * a.scale;
-      if (__any(top > m + kSlack)) {
-        const float now = fmaxf(m, top);
-        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - now);
-        m = now;
-        l *= f;
-#pragma unroll
-        for (int d = 0; d < ND; ++d) o[d] *= f;
-      }
-      const float ref = m == -INFINITY ? 0.f : -m;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        sc[r] = __builtin_amdgcn_exp2f(fmaf(sc[r], a.scale, ref));
-        l += sc[r];
-      }
-      if constexpr (E == 2) {
-        u32x4 pf[2];
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          u16x8 w;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) w[e] = f32_to_bf16(sc[8 * c + e]);
-          pf[c] = __builtin_bit_cast(u32x4, w);
-        }
-        const int i = lane & 15, grp = (lane >> 4) & 1;
-#pragma unroll
-        for (int d = 0; d < ND; ++d)
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            const int key = 32 * sub + 16 * c + 4 * lh + (i >> 2);
-            const int piece = 4 * d + 2 * grp + ((i >> 1) & 1);
-            const u32x2 a0 = read_transposed(sv + key * ROW + ((piece ^ swizzle<T, DH>(key)) << 4) + (i & 1) * 8);
-            const u32x2 a1 = read_transposed(sv + (key + 8) * ROW + ((piece ^ swizzle<T, DH>(key + 8)) << 4) + (i & 1) * 8);
-            u32x4 vf = u32x4{a0[0], a0[1], a1[0], a1[1]};
-            if (edge && has_unruly(vf, T{})) {
-              const Unruly bad = take_unruly(vf, T{});
-              u16x8 seen;
-#pragma unroll
-              for (int e = 0; e < 8; ++e)
-                seen[e] = key0 + 16 * c + 8 * (e >> 2) + 4 * lh + (e & 3) < lim ? 0x3f80 : 0;
-              const u32x4 w = __builtin_bit_cast(u32x4, seen);
-              add_unruly(o[d], mma32(bad.plus, w, zeros16(), T{}), mma32(bad.minus, w, zeros16(), T{}));
-            }
-            o[d] = mma32(vf, pf[c], o[d], T{});
-          }
-      } else {
-#pragma unroll
-        for (int d = 0; d < ND; ++d)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int key = 8 * (r >> 2) + 4 * lh + (r & 3);
-            const int at = 32 * d + l32;
-            float x = *reinterpret_cast<const float*>(
-                sv + key * ROW + (((at >> 2) ^ swizzle<T, DH>(key)) << 4) + (at & 3) * 4);
-            if (edge && __any(!(fabsf(x) < INFINITY))) {
-              const float w = key0 + key < lim ? 1.f : 0.f;
-              const bool ok = fabsf(x) < INFINITY;
-              const float plus = !ok && !(x < 0.f) ? 1.f : 0.f, minus = !ok && !(x > 0.f) ? 1.f : 0.f;
-              add_unruly(o[d], __builtin_amdgcn_mfma_f32_32x32x2f32(plus, w, zeros16(), 0, 0, 0),
-                         __builtin_amdgcn_mfma_f32_32x32x2f32(minus, w, zeros16(), 0, 0, 0));
-              x = ok ? x : 0.f;
-            }
-            o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, sc[r], o[d], 0, 0, 0);
-          }
+        for (int e = 0; e < 8; ++e) w[e] = f32_to_bf16(sc[8 * c + e]);
+        pf[c] = __builtin_bit_cast(u32x4, w);
       }
     }
+  }
+  // No key seen: zeros; keys that all score -inf: 0/0, as the formula has it.
+  static __device__ __forceinline__ float inverse(float l, int lim) {
+    return lim > 0 ? 1.0f / other_half_sum(l) : 0.f;
   }
 
-  // Rows go out whole, through LDS.  No key seen: zeros; keys that all score
-  // -inf: 0/0, as the formula has it.
-  l = other_half_sum(l);
-  const float inv = lim > 0 ? 1.0f / l : 0.f;
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-  unsigned char* so = ring + wave * 32 * ROW;
+  // *again: a word of LDS, cleared by the caller.
+  __device__ __forceinline__ void run(int* again) const {
+    constexpr int AHEAD = RT == 2 ? 2 : 3;  // operands read ahead of their product
+    int lim[RT];
+    long long mine[RT];
+    u32x4 qf[RT][NK];
 #pragma unroll
-  for (int d = 0; d < ND; ++d)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int at = 32 * d + 8 * j + 4 * lh;  // first of four elements
-      T* p = reinterpret_cast<T*>(so + l32 * ROW + (((at * E >> 4) ^ (l32 & 7)) << 4) + (at * E & 15));
-      store4(p, o[d][4 * j] * inv, o[d][4 * j + 1] * inv, o[d][4 * j + 2] * inv, o[d][4 * j + 3] * inv);
+    for (int t = 0; t < RT; ++t) {
+      lim[t] = limit(wrow + 32 * t + l32);
+      mine[t] = query(t, qf[t]);
     }
-  const long long mine = (long long)(q0 + tok) * a.ldo + head * DH;
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-  for (int u = lane; u < 32 * PIECES; u += 64) {
-    const int r = u / PIECES, c = u % PIECES;
-    const long long at = __shfl(mine, r);
-    if (wrow + r < rows)
-      *reinterpret_cast<u32x4*>(static_cast<T*>(a.out) + at + c * (16 / E)) =
-          *reinterpret_cast<const u32x4*>(so + r * ROW + ((c ^ (r & 7)) << 4));
+    const int end = wrow < rows ? limit(wrow + 32 * RT - 1) : 0;
+    f32x16 o[RT][ND];
+    float m[RT], l[RT];  // l over the lane half's keys only
+    bool unruly = false;
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      m[t] = -INFINITY;
+      l[t] = 0.f;
+#pragma unroll
+      for (int d = 0; d < ND; ++d) o[t][d] = zeros16();
+    }
+    // 32 keys.  EDGE: some row may not see them all, and values there are sifted.
+    auto step = [&](auto at_edge, int kt, int sub) __attribute__((always_inline)) {
+      constexpr bool EDGE = decltype(at_edge)::value;
+      const int key0 = kt * KT + 32 * sub;
+      int kb = kaddr + (kt & 1) * 2 * BYTES, vb = vaddr + (kt & 1) * 2 * BYTES;
+      asm volatile("" : "+v"(kb), "+v"(vb));  // not 16 addresses kept over the loop
+
+      // Each product and the read that takes its place are pinned in this order:
+      // left alone, the scheduler reads just before it multiplies.
+      f32x16 sc[RT];
+#pragma unroll
+      for (int t = 0; t < RT; ++t) sc[t] = zeros16();
+      u32x4 kf[AHEAD];
+#pragma unroll
+      for (int p = 0; p < AHEAD; ++p) kf[p] = kread(kb, sub, p);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int p = 0; p < NK; ++p) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t) sc[t] = mma32(kf[p % AHEAD], qf[t][p], sc[t], T{});
+        if (p + AHEAD < NK) kf[p % AHEAD] = kread(kb, sub, p + AHEAD);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      vop vf[AHEAD];
+#pragma unroll
+      for (int n = 0; n < AHEAD; ++n) vf[n] = vread(vb, sub, n / PV, n % PV);
+      __builtin_amdgcn_sched_barrier(0);
+
+      u32x4 pf[RT][2];
+#pragma unroll
+      for (int t = 0; t < RT; ++t)
+        softmax<EDGE>(sc[t], key0, lim[t], m[t], l[t], pf[t], [&](float f) {
+#pragma unroll
+          for (int d = 0; d < ND; ++d) o[t][d] *= f;
+        });
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int n = 0; n < ND * PV; ++n) {
+        vop v = vf[n % AHEAD];
+        if (EDGE) {
+          unruly |= __any(is_unruly(v, T{}));
+          v = ruly(v, T{});
+        }
+#pragma unroll
+        for (int t = 0; t < RT; ++t) o[t][n / PV] = product(v, sc[t], pf[t], n % PV, o[t][n / PV]);
+        if (n + AHEAD < ND * PV) vf[n % AHEAD] = vread(vb, sub, (n + AHEAD) / PV, (n + AHEAD) % PV);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    const int whole = limit(row0) / KT;  // tiles that every row of the workgroup sees
+    if (tiles > 0) issue(0, 0);
+    for (int kt = 0; kt < whole; ++kt) {
+      meet();  // tile kt is there and tile kt - 1 is done with
+      if (kt + 1 < tiles) issue(kt + 1, (kt + 1) & 1);
+#pragma unroll
+      for (int sub = 0; sub < KT / 32; ++sub) step(std::false_type{}, kt, sub);
+    }
+    for (int kt = whole; kt < tiles; ++kt) {
+      meet();
+      if (kt + 1 < tiles) issue(kt + 1, (kt + 1) & 1);
+      for (int sub = 0; sub < KT / 32; ++sub)
+        if (kt * KT + 32 * sub < end) step(std::true_type{}, kt, sub);
+    }
+    if (unruly) *again = 1;
+    meet();
+    // What the values left out of the edges make of the sums of rows that see them.
+    if (__builtin_amdgcn_readfirstlane(*again))
+      for (int kt = whole; kt < tiles; ++kt) {
+        issue(kt, 0);
+        meet();
+        for (int sub = 0; sub < KT / 32; ++sub) {
+          const int key0 = kt * KT + 32 * sub;
+          if (key0 >= end) continue;
+#pragma unroll
+          for (int d = 0; d < ND; ++d)
+#pragma unroll 1
+            for (int c = 0; c < PV; ++c) {
+              const vop v = vread(vaddr, sub, d, c);
+              if (!__any(is_unruly(v, T{}))) continue;
+#pragma unroll
+              for (int t = 0; t < RT; ++t) {
+                add_unruly<1>(v, c, key0, lh, lim[t], o[t][d], T{});
+                add_unruly<-1>(v, c, key0, lh, lim[t], o[t][d], T{});
+              }
+            }
+        }
+        meet();
+      }
+
+    // rows go out whole, through LDS
+    unsigned char* so = ring + wave * 32 * ROW;
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      const float inv = inverse(l[t], lim[t]);
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int at = 32 * d + 8 * j + 4 * lh;  // first of four elements
+          T* p = reinterpret_cast<T*>(so + l32 * ROW + (((at * E >> 4) ^ (l32 & 7)) << 4) + (at * E & 15));
+          const f32x16& x = o[t][d];
+          store4(p, x[4 * j] * inv, x[4 * j + 1] * inv, x[4 * j + 2] * inv, x[4 * j + 3] * inv);
+        }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      for (int u = lane; u < 32 * PIECES; u += 64) {
+        const int r = u / PIECES, c = u % PIECES;
+        const long long at = __shfl(mine[t], r);
+        if (wrow + 32 * t + r < rows)
+          *reinterpret_cast<u32x4*>(static_cast<T*>(a.out) + at + c * (16 / E)) =
+              *reinterpret_cast<const u32x4*>(so + r * ROW + ((c ^ (r & 7)) << 4));
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
   }
+};
+
+template <typename T, int DH, int WAVES, int RT>
+__global__ __launch_bounds__(64 * WAVES, 2) void prompt_kernel(PromptCall a) {
+  typedef Walk<T, DH, WAVES, RT> W;
+  __shared__ __attribute__((aligned(1024))) unsigned char ring[4 * W::BYTES];
+  __shared__ int again;
+  if (threadIdx.x == 0) again = 0;
+  const W w(a, ring);
+  if (w.row0 < w.rows) w.run(&again);
 }
 
-template <typename T, int DH, int WAVES>
+template <typename T, int DH, int WAVES, int RT>
 void prompt_at(PromptCall& a, hipStream_t s) {
-  const int64_t slots = (int64_t)a.n_q * a.group / (32 * WAVES) + a.n_seqs;
+  const int64_t slots = (int64_t)a.n_q * a.group / (32 * RT * WAVES) + a.n_seqs;
   a.n_slots = (int)slots;
-  hipLaunchKernelGGL((prompt_kernel<T, DH, WAVES>), dim3((unsigned)(slots * a.n_kv)),
+  hipLaunchKernelGGL((prompt_kernel<T, DH, WAVES, RT>), dim3((unsigned)(slots * a.n_kv)),
                      dim3(64 * WAVES), 0, s, a);
 }
 
@@ -373,12 +494,20 @@ void launch_prompt(const fv_prompt_args& x, hipStream_t s) {
   a.group = x.n_q_heads / x.n_kv_heads;
   a.causal = x.causal;
   a.scale = x.scale * kLog2e;
-  constexpr int W = sizeof(T) == 2 ? 8 : 4;
-  switch (x.head_dim) {
-    case 64: return prompt_at<T, 64, W>(a, s);
-    case 128: return prompt_at<T, 128, W>(a, s);
-    case 192: return prompt_at<T, 192, W>(a, s);
-    default: return prompt_at<T, 256, W>(a, s);
+  if constexpr (sizeof(T) == 2) {
+    switch (x.head_dim) {
+      case 64: return prompt_at<T, 64, 4, 2>(a, s);
+      case 128: return prompt_at<T, 128, 4, 2>(a, s);
+      case 192: return prompt_at<T, 192, 8, 1>(a, s);
+      default: return prompt_at<T, 256, 8, 1>(a, s);
+    }
+  } else {
+    switch (x.head_dim) {
+      case 64: return prompt_at<T, 64, 4, 1>(a, s);
+      case 128: return prompt_at<T, 128, 4, 1>(a, s);
+      case 192: return prompt_at<T, 192, 4, 1>(a, s);
+      default: return prompt_at<T, 256, 4, 1>(a, s);
+    }
   }
 }
 template void launch_prompt<bf16_t>(const fv_prompt_args&, hipStream_t);
