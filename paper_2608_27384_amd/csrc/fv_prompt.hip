@@ -43,6 +43,23 @@ __device__ __forceinline__ u32x2 read_transposed(const unsigned char* p) {
   return __builtin_bit_cast(u32x2, r);
 }
 
+// A direct-to-LDS load (see lds_dma16) that the compiler does not know of: it waits
+// for all those it knows of before a transposing read, the next tile's among them.
+// Whoever reads the data waits for the loads itself.
+__device__ __forceinline__ u32x4 dma_source(const void* base) {
+  const uint64_t p = reinterpret_cast<uint64_t>(base);
+  return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)p),
+               (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(p >> 32)), 0x7fffffffu, 0x00020000u};
+}
+__device__ __forceinline__ void dma16(u32x4 src, const unsigned char* lds, int off) {
+  const uint32_t to = (uint32_t)reinterpret_cast<uintptr_t>(
+      (const __attribute__((address_space(3))) unsigned char*)lds);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(
+                   __builtin_amdgcn_readfirstlane((int)to)),
+               "v"(off), "s"(src)
+               : "memory");
+}
+
 // 32x32 products over two 16-byte pieces a row (one of each lane half).
 __device__ __forceinline__ f32x16 mma32(u32x4 x, u32x4 y, f32x16 c, bf16_t) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x),
@@ -73,71 +90,56 @@ __device__ __forceinline__ float other_half_sum(float x) {
   return __uint_as_float(a[0]) + __uint_as_float(a[1]);
 }
 
+// Values at the edge, where a wave's rows differ in what they see.  A weight of
+// zero does not silence a value that is not finite, so such values are taken out
+// of the product there and added afterwards to the sums of the rows that see them
+// (add_unruly), which makes the infinity or NaN that the formula has.
+// odd(x): high bits for bf16 pairs (or an fp32 value) whose exponent is all ones.
+__device__ __forceinline__ uint32_t odd(uint32_t x, bf16_t) { return (x & 0x7f807f80u) + 0x00800080u; }
+__device__ __forceinline__ uint32_t odd(uint32_t x, float) { return (x & 0x7f800000u) + 0x00800000u; }
+__device__ __forceinline__ bool any_odd(uint32_t odds, bf16_t) { return __any(odds & 0x80008000u); }
+__device__ __forceinline__ bool any_odd(uint32_t odds, float) { return __any(odds >> 31); }
+__device__ __forceinline__ uint32_t even(uint32_t x, bf16_t t) {  // without the odd ones
+  const uint32_t b = odd(x, t) & 0x80008000u;
+  return x & ~(b | (b - (b >> 15)));
+}
+__device__ __forceinline__ uint32_t even(uint32_t x, float t) { return odd(x, t) >> 31 ? 0u : x; }
+// Operands of V.
+template <typename T> __device__ __forceinline__ uint32_t odds_of(u32x4 v, T t) {
+  return odd(v[0], t) | odd(v[1], t) | odd(v[2], t) | odd(v[3], t);
+}
+template <typename T> __device__ __forceinline__ uint32_t odds_of(float v, T t) { return odd(__float_as_uint(v), t); }
+template <typename T> __device__ __forceinline__ u32x4 even_of(u32x4 v, T t) {
+  return u32x4{even(v[0], t), even(v[1], t), even(v[2], t), even(v[3], t)};
+}
+template <typename T> __device__ __forceinline__ float even_of(float v, T t) {
+  return __uint_as_float(even(__float_as_uint(v), t));
+}
+// Adds the odd values of the keys [from, to) (rows of v, ldv apart) to the staged
+// results of a wave's 32 rows that see them; lane l holds the view of row l % 32,
+// and at(row, d) is the place of a result.
+template <int DH, typename T, typename At>
+__device__ __forceinline__ void add_unruly(const T* v, int ldv, int from, int to, int lim, At at) {
+  for (int key = from; key < to; ++key)
+    for (int d = threadIdx.x & 63; d < DH; d += 64) {
+      const float x = to_f32(v[(size_t)key * ldv + d]);
+      const bool skip = fabsf(x) < INFINITY;
+      if (!__any(!skip)) continue;
+      for (int r = 0; r < 32; ++r) {
+        const bool sees = key < __shfl(lim, r);
+        if (sees && !skip) {
+          auto* p = at(r, d);
+          typedef typename std::remove_pointer<decltype(p)>::type O;
+          *p = from_f32<O>(to_f32(*p) + x);
+        }
+      }
+    }
+}
 __device__ __forceinline__ f32x16 zeros16() {
   f32x16 z;
 #pragma unroll
   for (int r = 0; r < 16; ++r) z[r] = 0.f;
   return z;
-}
-
-// Values at the edge, where a wave's rows differ in what they see.  A weight of
-// zero does not silence a value that is not finite, so such values are taken out
-// of the product there; afterwards, products of ones in their place (for +inf, for
-// -inf, for both where the value is NaN) with the rows' view say which sums they
-// make infinite.
-__device__ __forceinline__ bool is_unruly(u32x4 x, bf16_t) {
-  bool any = false;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    any |= (x[i] & 0x7f80u) == 0x7f80u || (x[i] & 0x7f800000u) == 0x7f800000u;
-  return any;
-}
-__device__ __forceinline__ bool is_unruly(float x, float) { return !(fabsf(x) < INFINITY); }
-// The operand without them.
-__device__ __forceinline__ u32x4 ruly(u32x4 x, bf16_t) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if ((x[i] & 0x7f80u) == 0x7f80u) x[i] &= 0xffff0000u;
-    if ((x[i] & 0x7f800000u) == 0x7f800000u) x[i] &= 0x0000ffffu;
-  }
-  return x;
-}
-__device__ __forceinline__ float ruly(float x, float) { return is_unruly(x, x) ? 0.f : x; }
-// Ones for the values of SIGN times infinity, or NaN.
-template <int SIGN> __device__ __forceinline__ u32x4 ones_for(u32x4 x, bf16_t) {
-  u32x4 r;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    r[i] = 0;
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const uint32_t b = x[i] >> (16 * half) & 0xffffu;
-      if ((b & 0x7fffu) > 0x7f80u || b == (SIGN > 0 ? 0x7f80u : 0xff80u)) r[i] |= 0x3f80u << (16 * half);
-    }
-  }
-  return r;
-}
-template <int SIGN> __device__ __forceinline__ float ones_for(float x, float) {
-  return x != x || x == SIGN * INFINITY ? 1.f : 0.f;
-}
-template <int SIGN> __device__ __forceinline__ void add_infinities(f32x16& o, const f32x16& seen) {
-#pragma unroll
-  for (int r = 0; r < 16; ++r) o[r] += seen[r] > 0.f ? SIGN * INFINITY : 0.f;
-}
-// For operand c of V (see vread) and a lane whose row sees the keys below lim.
-template <int SIGN>
-__device__ __forceinline__ void add_unruly(u32x4 v, int c, int key0, int lh, int lim, f32x16& o, bf16_t) {
-  u16x8 seen;
-#pragma unroll
-  for (int e = 0; e < 8; ++e)
-    seen[e] = key0 + 16 * c + 8 * (e >> 2) + 4 * lh + (e & 3) < lim ? 0x3f80 : 0;
-  add_infinities<SIGN>(o, mma32(ones_for<SIGN>(v, bf16_t{}), __builtin_bit_cast(u32x4, seen), zeros16(),
-                                bf16_t{}));
-}
-template <int SIGN>
-__device__ __forceinline__ void add_unruly(float v, int c, int key0, int lh, int lim, f32x16& o, float) {
-  const float seen = key0 + 8 * (c >> 2) + 4 * lh + (c & 3) < lim ? 1.f : 0.f;
-  add_infinities<SIGN>(o, __builtin_amdgcn_mfma_f32_32x32x2f32(ones_for<SIGN>(v, v), seen, zeros16(), 0, 0, 0));
 }
 
 __device__ __forceinline__ int clamped(const int* cu, int s, int n) { return min(max(cu[s], 0), n); }
@@ -164,28 +166,91 @@ __device__ __forceinline__ int prompt_of(const PromptCall& a, int slot, int* fir
   return lo;
 }
 
-// One workgroup's walk over the keys of its rows: RT 32-row tiles a wave (with
-// two, every operand read from LDS serves two products).
-template <typename T, int DH, int WAVES, int RT>
-struct Walk {
+// O^T += V^T P^T for operand c of V, of the probabilities p (pf: as bf16 operands).
+__device__ __forceinline__ f32x16 product(u32x4 v, const f32x16&, const u32x4 (&pf)[2], int c, f32x16 o) {
+  return mma32(v, pf[c], o, bf16_t{});
+}
+__device__ __forceinline__ f32x16 product(float v, const f32x16& p, const u32x4 (&)[2], int c, f32x16 o) {
+  return __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[c], o, 0, 0, 0);
+}
+// Scores of 32 keys to probabilities (pf: as bf16 operands), with the row's
+// reference m and sum l; calls rescale(f) where the reference moves, and tick(r)
+// after the r-th of 16 probabilities.
+template <typename T, typename Rescale, typename Tick>
+__device__ __forceinline__ void softmax(f32x16& sc, bool edge, int key0, int lh, int lim, float scale, float& m,
+                                        float& l, u32x4 (&pf)[2], Rescale rescale, Tick tick) {
+  if (edge) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      if (key0 + 8 * (r >> 2) + 4 * lh + (r & 3) >= lim) sc[r] = -INFINITY;
+  }
+  float top = sc[0];
+#pragma unroll
+  for (int r = 1; r < 16; ++r) top = fmaxf(top, sc[r]);
+  top = other_half_max(top) * scale;
+  if (__any(top > m + kSlack)) {
+    const float now = fmaxf(m, top);
+    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - now);
+    m = now;
+    l *= f;
+    rescale(f);
+  }
+  const float ref = m == -INFINITY ? 0.f : -m;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    sc[r] = __builtin_amdgcn_exp2f(fmaf(sc[r], scale, ref));
+    l += sc[r];
+    tick(r);
+  }
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      u16x8 w;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = f32_to_bf16(sc[8 * c + e]);
+      pf[c] = __builtin_bit_cast(u32x4, w);
+    }
+  }
+}
+// No key seen: zeros; keys that all score -inf: 0/0, as the formula has it.
+__device__ __forceinline__ float inverse(float l, int lim) {
+  return lim > 0 ? 1.0f / other_half_sum(l) : 0.f;
+}
+
+// Row and byte in it of a lane's 16 bytes in the n-th kilobyte of a staged tile.
+// Where a kilobyte is whole rows, both are the lane's of the first one moved by
+// constants (the swizzle is linear over exclusive or).
+template <typename T, int DH> struct Slots {
+  static constexpr int PIECES = DH * (int)sizeof(T) / 16, PER = 64 / PIECES;
+  static constexpr bool WHOLE = PIECES <= 64 && (PIECES & (PIECES - 1)) == 0;
+  int lane, row0, byte0;
+  __device__ __forceinline__ explicit Slots(int l) : lane(l) {
+    row0 = l / PIECES;
+    byte0 = ((l % PIECES) ^ swizzle<T, DH>(row0)) << 4;
+  }
+  __device__ __forceinline__ void find(int n, int& row, int& byte) const {
+    if constexpr (WHOLE) {
+      row = PER * n + row0;
+      byte = byte0 ^ (swizzle<T, DH>(PER * n) << 4);
+    } else {
+      const int u = 64 * n + lane;
+      row = u / PIECES;
+      byte = ((u % PIECES) ^ swizzle<T, DH>(row)) << 4;
+    }
+  }
+};
+
+// What a workgroup of R rows knows of its prompt.
+template <typename T, int DH, int R>
+struct Rows {
   static constexpr int E = (int)sizeof(T);
-  static constexpr int KT = E == 2 && WAVES == 8 ? 64 : 32;    // keys of a tile
-  static constexpr int ROW = DH * E, PIECES = ROW / 16;
-  static constexpr int BYTES = KT * ROW;                       // of a K tile, and of a V tile
-  static constexpr int SW = E == 4 || DH % 128 == 0 ? 16 : 8;  // pieces that a swizzle permutes
-  static constexpr int R = 32 * RT * WAVES;                    // rows of a workgroup
-  static constexpr int ND = DH / 32;                           // 32-row tiles of O^T
-  static constexpr int NI = BYTES / 1024 / WAVES;              // direct loads of a wave per tensor and tile
-  static constexpr int NK = PIECES / 2;                        // K operands of 32 keys
-  static constexpr int PV = E == 2 ? 2 : 16;                   // V operands of 32 keys and 32 elements
-  static_assert(NI * 1024 * WAVES == BYTES && 32 * WAVES * ROW <= 4 * BYTES, "tile split");
-  typedef typename std::conditional<E == 2, u32x4, float>::type vop;
+  static constexpr int NK = DH * E / 32;  // K operands of 32 keys
+  static constexpr int ND = DH / 32;      // 32-row tiles of O^T
 
   const PromptCall& a;
-  unsigned char* ring;  // two stages of K and V
-  int lane, wave, l32, lh, kh, q0, k0, nk, rows, row0, wrow, diff, tiles, kaddr, vaddr;
+  int lane, wave, l32, lh, kh, q0, k0, nk, rows, row0, diff;
 
-  __device__ __forceinline__ Walk(const PromptCall& call, unsigned char* lds) : a(call), ring(lds) {
+  __device__ __forceinline__ explicit Rows(const PromptCall& call) : a(call) {
     lane = threadIdx.x & 63;
     wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     l32 = lane & 31;
@@ -201,46 +266,102 @@ struct Walk {
     nk = max(0, clamped(a.cu_k, s + 1, a.n_k) - k0);
     rows = nq * a.group;
     row0 = (slot - first) * R;
-    wrow = row0 + 32 * RT * wave;
     diff = nk - nq + 1;
-    tiles = (limit(row0 + R - 1) + KT - 1) / KT;
-    // LDS addresses of the operands: one register each for K and V and a constant
-    // exclusive or (the swizzle), so that they cost an instruction and no registers.
-    kaddr = l32 * ROW + ((lh ^ swizzle<T, DH>(l32)) << 4);
-    const int i16 = lane & 15, r = 4 * lh + (i16 >> 2);
-    vaddr = E == 2 ? BYTES + r * ROW +
-                         (((2 * ((lane >> 4) & 1) + ((i16 >> 1) & 1)) ^ swizzle<T, DH>(r)) << 4) +
-                         (i16 & 1) * 8
-                   : BYTES + 4 * lh * ROW + (((l32 >> 2) ^ (lh << 3)) << 4) + (l32 & 3) * 4;
   }
   // A row sees the keys [0, limit), which do not fall from one row to the next.
   __device__ __forceinline__ int limit(int row) const {
     return a.causal ? min(max(diff + min(row, rows - 1) / a.group, 0), nk) : nk;
   }
-  // The lane's query of row tile t, as products' operands, and its place in the output.
-  __device__ __forceinline__ long long query(int t, u32x4 (&qf)[NK]) const {
-    const int row = min(wrow + 32 * t + l32, rows - 1);
+  // The lane's query of the 32 rows from r0 on, as products' operands, and its
+  // place in the output.  A lane wants a row of its own, which as loads is 32 bytes
+  // of each of 32 rows at a time (4 times the cycles of whole rows): the rows go
+  // whole to `lds` (32 of them) and from there to the lanes, shared by `waves` waves.
+  template <bool KNOWN>  // loads that the compiler knows of
+  __device__ __forceinline__ long long query(int r0, u32x4 (&qf)[NK], unsigned char* lds, int waves) const {
+    constexpr int ROW = DH * E, SW = E == 4 || DH % 128 == 0 ? 16 : 8, N = 32 * ROW / 1024;
+    const int row = min(r0 + l32, rows - 1);
     const int tok = row / a.group, head = kh * a.group + row - tok * a.group;
-    const T* q = static_cast<const T*>(a.q) + (size_t)(q0 + tok) * a.ldq + head * DH;
+    const int tok0 = __builtin_amdgcn_readfirstlane(tok);
+    const T* from = static_cast<const T*>(a.q) + (size_t)(q0 + tok0) * a.ldq;
+    const int off = ((tok - tok0) * a.ldq + head * DH) * E;
+    const Slots<T, DH> at(lane);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // what was there has been read
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      if (waves > 1 && n % waves != wave) continue;
+      int r, byte;
+      at.find(n, r, byte);
+      if constexpr (KNOWN)
+        lds_dma16(lds_source(from), lds + 1024 * n, __shfl(off, r) + byte, 0);
+      else
+        dma16(dma_source(from), lds + 1024 * n, __shfl(off, r) + byte);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if (waves > 1) {
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+    }
+    const int base = l32 * ROW + ((lh ^ swizzle<T, DH>(l32)) << 4);
 #pragma unroll
     for (int p = 0; p < NK; ++p)
-      qf[p] = *reinterpret_cast<const u32x4*>(q + (2 * p + lh) * (16 / E));
+      qf[p] = *reinterpret_cast<const u32x4*>(lds + (base ^ ((2 * p & (SW - 1)) << 4)) + 2 * p / SW * SW * 16);
     return (long long)(q0 + tok) * a.ldo + head * DH;
+  }
+};
+
+// The walk over the keys with tiles staged in LDS, 128 rows a workgroup.  KG 1:
+// four waves of 32 rows, tiles of 32 keys.  KG 2 (bf16): eight waves, tiles of 64
+// keys, of which half the waves take the first 32 and half the others; they join
+// at the end.  A workgroup's walk then has half the steps, for where there are not
+// enough of them to fill the chip.
+template <typename T, int DH, int KG>
+struct Walk : Rows<T, DH, 128> {
+  typedef Rows<T, DH, 128> Base;
+  using Base::a, Base::lane, Base::wave, Base::l32, Base::lh, Base::kh, Base::k0, Base::nk, Base::rows,
+      Base::row0, Base::limit, Base::E, Base::NK, Base::ND;
+  static constexpr int R = 128, WAVES = 4 * KG;
+  static constexpr int KT = 32 * KG;                           // keys of a tile
+  static constexpr int ROW = DH * E, PIECES = ROW / 16;
+  static constexpr int BYTES = KT * ROW;                       // of a K tile, and of a V tile
+  static constexpr int SW = E == 4 || DH % 128 == 0 ? 16 : 8;  // pieces that a swizzle permutes
+  static constexpr int NI = BYTES / 1024 / WAVES;              // direct loads of a wave per tensor and tile
+  static constexpr int PV = E == 2 ? 2 : 16;                   // V operands of 32 keys and 32 elements
+  static_assert(NI * 1024 * WAVES == BYTES && 32 * WAVES * ROW <= 4 * BYTES, "tile split");
+  static_assert(KG == 1 || (KG == 2 && 4 * 32 * DH * 4 <= 4 * BYTES), "join");
+  typedef typename std::conditional<E == 2, u32x4, float>::type vop;
+
+  unsigned char* ring;  // two stages of K and V
+  int wrow, half, tiles, kaddr, vaddr;
+
+  __device__ __forceinline__ Walk(const PromptCall& call, unsigned char* lds) : Base(call), ring(lds) {
+    half = wave / 4;
+    wrow = row0 + 32 * (wave % 4);
+    tiles = (limit(row0 + R - 1) + KT - 1) / KT;
+    // LDS addresses of the operands: one register each for K and V and a constant
+    // exclusive or (the swizzle), so that they cost an instruction and no registers.
+    kaddr = (32 * half + l32) * ROW + ((lh ^ swizzle<T, DH>(l32)) << 4);
+    const int i16 = lane & 15, r = 4 * lh + (i16 >> 2);
+    vaddr = E == 2 ? BYTES + (32 * half + r) * ROW +
+                         (((2 * ((lane >> 4) & 1) + ((i16 >> 1) & 1)) ^ swizzle<T, DH>(r)) << 4) +
+                         (i16 & 1) * 8
+                   : BYTES + 4 * lh * ROW + (((l32 >> 2) ^ (lh << 3)) << 4) + (l32 & 3) * 4;
   }
   // Direct loads of key tile kt: slot u, 16 bytes, is piece u % PIECES of row u / PIECES.
   __device__ __forceinline__ void issue(int kt, int stage) const {
     unsigned char* to = ring + stage * 2 * BYTES + wave * NI * 1024;
-    const lds_src ks = lds_source(static_cast<const T*>(a.k) + (size_t)(k0 + kt * KT) * a.ldk + kh * DH);
-    const lds_src vs = lds_source(static_cast<const T*>(a.v) + (size_t)(k0 + kt * KT) * a.ldv + kh * DH);
+    const u32x4 ks = dma_source(static_cast<const T*>(a.k) + (size_t)(k0 + kt * KT) * a.ldk + kh * DH);
+    const u32x4 vs = dma_source(static_cast<const T*>(a.v) + (size_t)(k0 + kt * KT) * a.ldv + kh * DH);
     const int most = nk - 1 - kt * KT;  // rows past the prompt's last repeat it
     int mine = lane;
     asm volatile("" : "+v"(mine));  // not 2 NI offsets kept over the loop
+    const Slots<T, DH> at(mine);
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-      const int u = 64 * (NI * wave + i) + mine, r = u / PIECES;
-      const int c = (u % PIECES) ^ swizzle<T, DH>(r), rr = min(r, most);
-      lds_dma16(ks, to + 1024 * i, rr * a.ldk * E + 16 * c, 0);
-      lds_dma16(vs, to + BYTES + 1024 * i, rr * a.ldv * E + 16 * c, 0);
+      int row, byte;
+      at.find(NI * wave + i, row, byte);
+      row = min(row, most);
+      dma16(ks, to + 1024 * i, __umul24(row, a.ldk * E) + byte);
+      dma16(vs, to + BYTES + 1024 * i, __umul24(row, a.ldv * E) + byte);
     }
   }
   // Every wave's loads have landed, every wave's reads are done.
@@ -249,141 +370,77 @@ struct Walk {
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   }
-  __device__ __forceinline__ u32x4 kread(int base, int sub, int p) const {
+  __device__ __forceinline__ u32x4 kread(int base, int p) const {
     return *reinterpret_cast<const u32x4*>(ring + (base ^ ((2 * p & (SW - 1)) << 4)) +
-                                           32 * sub * ROW + 2 * p / SW * SW * 16);
+                                           2 * p / SW * SW * 16);
   }
   // Operand c of V for the elements from 32 d on of the head: 16 keys from 16 c on
   // (bf16), the keys of score register c (fp32).
-  __device__ __forceinline__ vop vread(int base, int sub, int d, int c) const {
+  __device__ __forceinline__ vop vread(int base, int d, int c) const {
     if constexpr (E == 2) {
-      const unsigned char* p = ring + (32 * sub + 16 * c) * ROW + 4 * d / SW * SW * 16;
+      const unsigned char* p = ring + 16 * c * ROW + 4 * d / SW * SW * 16;
       const int x = base ^ ((4 * d & (SW - 1)) << 4);
       const u32x2 lo = read_transposed(p + x), hi = read_transposed(p + (x ^ 32) + 8 * ROW);
       return u32x4{lo[0], lo[1], hi[0], hi[1]};
     } else {
       const int j = c >> 2, r = c & 3;
       const int x = base ^ ((8 * d & 15) << 4) ^ (r << 5) ^ ((j & 1) << 4);
-      return *reinterpret_cast<const float*>(ring + x + (32 * sub + 8 * j + r) * ROW + 8 * d / 16 * 256);
+      return *reinterpret_cast<const float*>(ring + x + (8 * j + r) * ROW + 8 * d / 16 * 256);
     }
   }
-  static __device__ __forceinline__ f32x16 product(vop v, const f32x16& p, const u32x4 (&pf)[2], int c,
-                                                   f32x16 o) {
-    if constexpr (E == 2)
-      return mma32(v, pf[c], o, T{});
-    else
-      return __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[c], o, 0, 0, 0);
-  }
-  // Scores of 32 keys to probabilities (pf: as bf16 operands), with the row's
-  // reference m and sum l; calls rescale(f) where the reference moves.
-  template <bool EDGE, typename Rescale>
-  __device__ __forceinline__ void softmax(f32x16& sc, int key0, int lim, float& m, float& l,
-                                          u32x4 (&pf)[2], Rescale rescale) const {
-    if (EDGE) {
+  // stats: LDS for the maximum and sum of the waves that give theirs to others.
+  __device__ __forceinline__ void run(float* stats) const {
+    constexpr int AHEAD = 3;  // operands read ahead of their product
+    u32x4 qf[NK];
+    const long long mine = this->template query<false>(wrow, qf, ring + wave * 32 * ROW, 1);
+    const int lim = limit(wrow + l32);
+    meet();  // the ring is the tiles' from here on
+    const int end = wrow < rows ? limit(wrow + 31) : 0;
+    f32x16 o[ND];
+    float m = -INFINITY, l = 0.f;  // l over the lane half's keys only
+    uint32_t odds = 0;
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (key0 + 8 * (r >> 2) + 4 * lh + (r & 3) >= lim) sc[r] = -INFINITY;
-    }
-    float top = sc[0];
-#pragma unroll
-    for (int r = 1; r < 16; ++r) top = fmaxf(top, sc[r]);
-    top = other_half_max(top) * a.scale;
-    if (__any(top > m + kSlack)) {
-      const float now = fmaxf(m, top);
-      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - now);
-      m = now;
-      l *= f;
-      rescale(f);
-    }
-    const float ref = m == -INFINITY ? 0.f : -m;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      sc[r] = __builtin_amdgcn_exp2f(fmaf(sc[r], a.scale, ref));
-      l += sc[r];
-    }
-    if constexpr (E == 2) {
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        u16x8 w;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = f32_to_bf16(sc[8 * c + e]);
-        pf[c] = __builtin_bit_cast(u32x4, w);
-      }
-    }
-  }
-  // No key seen: zeros; keys that all score -inf: 0/0, as the formula has it.
-  static __device__ __forceinline__ float inverse(float l, int lim) {
-    return lim > 0 ? 1.0f / other_half_sum(l) : 0.f;
-  }
-
-  // *again: a word of LDS, cleared by the caller.
-  __device__ __forceinline__ void run(int* again) const {
-    constexpr int AHEAD = RT == 2 ? 2 : 3;  // operands read ahead of their product
-    int lim[RT];
-    long long mine[RT];
-    u32x4 qf[RT][NK];
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      lim[t] = limit(wrow + 32 * t + l32);
-      mine[t] = query(t, qf[t]);
-    }
-    const int end = wrow < rows ? limit(wrow + 32 * RT - 1) : 0;
-    f32x16 o[RT][ND];
-    float m[RT], l[RT];  // l over the lane half's keys only
-    bool unruly = false;
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      m[t] = -INFINITY;
-      l[t] = 0.f;
-#pragma unroll
-      for (int d = 0; d < ND; ++d) o[t][d] = zeros16();
-    }
+    for (int d = 0; d < ND; ++d) o[d] = zeros16();
     // 32 keys.  EDGE: some row may not see them all, and values there are sifted.
-    auto step = [&](auto at_edge, int kt, int sub) __attribute__((always_inline)) {
+    auto step = [&](auto at_edge, int kt) __attribute__((always_inline)) {
       constexpr bool EDGE = decltype(at_edge)::value;
-      const int key0 = kt * KT + 32 * sub;
+      const int key0 = kt * KT + 32 * half;
       int kb = kaddr + (kt & 1) * 2 * BYTES, vb = vaddr + (kt & 1) * 2 * BYTES;
       asm volatile("" : "+v"(kb), "+v"(vb));  // not 16 addresses kept over the loop
 
       // Each product and the read that takes its place are pinned in this order:
       // left alone, the scheduler reads just before it multiplies.
-      f32x16 sc[RT];
-#pragma unroll
-      for (int t = 0; t < RT; ++t) sc[t] = zeros16();
+      f32x16 sc = zeros16();
       u32x4 kf[AHEAD];
 #pragma unroll
-      for (int p = 0; p < AHEAD; ++p) kf[p] = kread(kb, sub, p);
+      for (int p = 0; p < AHEAD; ++p) kf[p] = kread(kb, p);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int p = 0; p < NK; ++p) {
-#pragma unroll
-        for (int t = 0; t < RT; ++t) sc[t] = mma32(kf[p % AHEAD], qf[t][p], sc[t], T{});
-        if (p + AHEAD < NK) kf[p % AHEAD] = kread(kb, sub, p + AHEAD);
+        sc = mma32(kf[p % AHEAD], qf[p], sc, T{});
+        if (p + AHEAD < NK) kf[p % AHEAD] = kread(kb, p + AHEAD);
         __builtin_amdgcn_sched_barrier(0);
       }
       vop vf[AHEAD];
 #pragma unroll
-      for (int n = 0; n < AHEAD; ++n) vf[n] = vread(vb, sub, n / PV, n % PV);
+      for (int n = 0; n < AHEAD; ++n) vf[n] = vread(vb, n / PV, n % PV);
       __builtin_amdgcn_sched_barrier(0);
 
-      u32x4 pf[RT][2];
+      u32x4 pf[2];
+      softmax<T>(sc, EDGE, key0, lh, lim, a.scale, m, l, pf, [&](float f) {
 #pragma unroll
-      for (int t = 0; t < RT; ++t)
-        softmax<EDGE>(sc[t], key0, lim[t], m[t], l[t], pf[t], [&](float f) {
-#pragma unroll
-          for (int d = 0; d < ND; ++d) o[t][d] *= f;
-        });
+        for (int d = 0; d < ND; ++d) o[d] *= f;
+      }, [](int) {});
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int n = 0; n < ND * PV; ++n) {
         vop v = vf[n % AHEAD];
         if (EDGE) {
-          unruly |= __any(is_unruly(v, T{}));
-          v = ruly(v, T{});
+          odds |= odds_of(v, T{});
+          v = even_of(v, T{});
         }
-#pragma unroll
-        for (int t = 0; t < RT; ++t) o[t][n / PV] = product(v, sc[t], pf[t], n % PV, o[t][n / PV]);
-        if (n + AHEAD < ND * PV) vf[n % AHEAD] = vread(vb, sub, (n + AHEAD) / PV, (n + AHEAD) % PV);
+        o[n / PV] = product(v, sc, pf, n % PV, o[n / PV]);
+        if (n + AHEAD < ND * PV) vf[n % AHEAD] = vread(vb, (n + AHEAD) / PV, (n + AHEAD) % PV);
         __builtin_amdgcn_sched_barrier(0);
       }
     };
@@ -392,84 +449,333 @@ struct Walk {
     for (int kt = 0; kt < whole; ++kt) {
       meet();  // tile kt is there and tile kt - 1 is done with
       if (kt + 1 < tiles) issue(kt + 1, (kt + 1) & 1);
-#pragma unroll
-      for (int sub = 0; sub < KT / 32; ++sub) step(std::false_type{}, kt, sub);
+      step(std::false_type{}, kt);
     }
     for (int kt = whole; kt < tiles; ++kt) {
       meet();
       if (kt + 1 < tiles) issue(kt + 1, (kt + 1) & 1);
-      for (int sub = 0; sub < KT / 32; ++sub)
-        if (kt * KT + 32 * sub < end) step(std::true_type{}, kt, sub);
+      if (kt * KT + 32 * half < end) step(std::true_type{}, kt);
     }
-    if (unruly) *again = 1;
+    bool unruly = any_odd(odds, T{});
     meet();
-    // What the values left out of the edges make of the sums of rows that see them.
-    if (__builtin_amdgcn_readfirstlane(*again))
-      for (int kt = whole; kt < tiles; ++kt) {
-        issue(kt, 0);
-        meet();
-        for (int sub = 0; sub < KT / 32; ++sub) {
-          const int key0 = kt * KT + 32 * sub;
-          if (key0 >= end) continue;
+    if constexpr (KG == 2) {
+      f32x4* so = reinterpret_cast<f32x4*>(ring) + (wave % 4) * (4 * ND * 64) + lane;
+      float* st = stats + (wave % 4) * 128 + lane;
+      if (half) {
 #pragma unroll
-          for (int d = 0; d < ND; ++d)
-#pragma unroll 1
-            for (int c = 0; c < PV; ++c) {
-              const vop v = vread(vaddr, sub, d, c);
-              if (!__any(is_unruly(v, T{}))) continue;
+        for (int d = 0; d < ND; ++d)
 #pragma unroll
-              for (int t = 0; t < RT; ++t) {
-                add_unruly<1>(v, c, key0, lh, lim[t], o[t][d], T{});
-                add_unruly<-1>(v, c, key0, lh, lim[t], o[t][d], T{});
-              }
-            }
-        }
-        meet();
+          for (int j = 0; j < 4; ++j)
+            so[(4 * d + j) * 64] = f32x4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]};
+        st[0] = m;
+        st[64] = l;
+        if (lane == 0) stats[512 + wave % 4] = unruly;
       }
-
+      meet();
+      if (!half) {
+        unruly |= stats[512 + wave] != 0.f;
+        const float other = st[0], now = fmaxf(m, other), ref = now == -INFINITY ? 0.f : now;
+        const float f = __builtin_amdgcn_exp2f(m - ref), g = __builtin_amdgcn_exp2f(other - ref);
+        l = l * f + st[64] * g;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const f32x4 x = so[(4 * d + j) * 64];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[d][4 * j + e] = o[d][4 * j + e] * f + x[e] * g;
+          }
+      }
+      meet();
+      if (half) return;
+    }
     // rows go out whole, through LDS
     unsigned char* so = ring + wave * 32 * ROW;
+    const float inv = inverse(l, lim);
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      const float inv = inverse(l[t], lim[t]);
+    for (int d = 0; d < ND; ++d)
 #pragma unroll
-      for (int d = 0; d < ND; ++d)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int at = 32 * d + 8 * j + 4 * lh;  // first of four elements
-          T* p = reinterpret_cast<T*>(so + l32 * ROW + (((at * E >> 4) ^ (l32 & 7)) << 4) + (at * E & 15));
-          const f32x16& x = o[t][d];
-          store4(p, x[4 * j] * inv, x[4 * j + 1] * inv, x[4 * j + 2] * inv, x[4 * j + 3] * inv);
-        }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      for (int u = lane; u < 32 * PIECES; u += 64) {
-        const int r = u / PIECES, c = u % PIECES;
-        const long long at = __shfl(mine[t], r);
-        if (wrow + 32 * t + r < rows)
-          *reinterpret_cast<u32x4*>(static_cast<T*>(a.out) + at + c * (16 / E)) =
-              *reinterpret_cast<const u32x4*>(so + r * ROW + ((c ^ (r & 7)) << 4));
+      for (int j = 0; j < 4; ++j) {
+        const int at = 32 * d + 8 * j + 4 * lh;  // first of four elements
+        T* p = reinterpret_cast<T*>(so + l32 * ROW + (((at * E >> 4) ^ (l32 & 7)) << 4) + (at * E & 15));
+        const f32x16& x = o[d];
+        store4(p, x[4 * j] * inv, x[4 * j + 1] * inv, x[4 * j + 2] * inv, x[4 * j + 3] * inv);
       }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (unruly) {
+      add_unruly<DH>(static_cast<const T*>(a.v) + (size_t)k0 * a.ldv + kh * DH, a.ldv, whole * KT,
+                     min(end, nk), lim, [&](int r, int d) {
+                       return reinterpret_cast<T*>(so + r * ROW + (((d * E >> 4) ^ (r & 7)) << 4) + (d * E & 15));
+                     });
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+    for (int u = lane; u < 32 * PIECES; u += 64) {
+      const int r = u / PIECES, c = u % PIECES;
+      const long long at = __shfl(mine, r);
+      if (wrow + r < rows)
+        *reinterpret_cast<u32x4*>(static_cast<T*>(a.out) + at + c * (16 / E)) =
+            *reinterpret_cast<const u32x4*>(so + r * ROW + ((c ^ (r & 7)) << 4));
     }
   }
 };
 
-template <typename T, int DH, int WAVES, int RT>
-__global__ __launch_bounds__(64 * WAVES, 2) void prompt_kernel(PromptCall a) {
-  typedef Walk<T, DH, WAVES, RT> W;
+template <typename T, int DH, int KG>
+__global__ __launch_bounds__(256 * KG, DH * sizeof(T) > 512 ? 1 : 2) void prompt_kernel(PromptCall a) {
+  typedef Walk<T, DH, KG> W;
   __shared__ __attribute__((aligned(1024))) unsigned char ring[4 * W::BYTES];
-  __shared__ int again;
-  if (threadIdx.x == 0) again = 0;
+  __shared__ float stats[KG == 2 ? 516 : 1];
   const W w(a, ring);
-  if (w.row0 < w.rows) w.run(&again);
+  if (w.row0 < w.rows) w.run(stats);
 }
 
-template <typename T, int DH, int WAVES, int RT>
-void prompt_at(PromptCall& a, hipStream_t s) {
-  const int64_t slots = (int64_t)a.n_q * a.group / (32 * RT * WAVES) + a.n_seqs;
-  a.n_slots = (int)slots;
-  hipLaunchKernelGGL((prompt_kernel<T, DH, WAVES, RT>), dim3((unsigned)(slots * a.n_kv)),
-                     dim3(64 * WAVES), 0, s, a);
+// 32 keys of V from memory into registers.  A lane takes W = DH/32 consecutive
+// elements of each of its 16 keys (those of its score registers), a whole row by
+// 32 lanes; row i of O^T's tile j is then the head's element W i + j.
+template <typename T, int DH> struct FewV {
+  static constexpr int W = DH / 32, DW = W * (int)sizeof(T) / 4;
+  uint32_t w[16][DW];
+  // x-th row: `off` bytes past the source.
+  __device__ __forceinline__ void load(int x, lds_src src, int off) {
+    constexpr int B = DW / 4 * 4;
+#pragma unroll
+    for (int i = 0; i < B; i += 4) {
+      const auto y = __builtin_amdgcn_raw_buffer_load_b128(src, off + 4 * i, 0, 0);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[x][i + e] = y[e];
+    }
+    if constexpr (DW % 4 == 3) {
+      const auto y = __builtin_amdgcn_raw_buffer_load_b96(src, off + 4 * B, 0, 0);
+#pragma unroll
+      for (int e = 0; e < 3; ++e) w[x][B + e] = y[e];
+    } else if constexpr (DW % 4 == 2) {
+      const auto y = __builtin_amdgcn_raw_buffer_load_b64(src, off + 4 * B, 0, 0);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) w[x][B + e] = y[e];
+    } else if constexpr (DW % 4 == 1) {
+      w[x][B] = __builtin_amdgcn_raw_buffer_load_b32(src, off + 4 * B, 0, 0);
+    }
+  }
+  // Takes out what is not finite; whether there was any.
+  __device__ __forceinline__ bool sift() {
+    uint32_t odds = 0;
+#pragma unroll
+    for (int x = 0; x < 16; ++x)
+#pragma unroll
+      for (int i = 0; i < DW; ++i) odds |= odd(w[x][i], T{});
+    if (__builtin_expect(!any_odd(odds, T{}), 1)) return false;
+#pragma unroll
+    for (int x = 0; x < 16; ++x)
+#pragma unroll
+      for (int i = 0; i < DW; ++i) w[x][i] = even(w[x][i], T{});
+    return true;
+  }
+  // Operand c of tile j: 16 keys from 16 c on (bf16, a turned 8 x 2 block), the
+  // keys of score register c (fp32).
+  __device__ __forceinline__ auto operand(int j, int c) const {
+    if constexpr (sizeof(T) == 2) {
+      u32x4 r;
+#pragma unroll
+      for (int y = 0; y < 4; ++y)
+        r[y] = __builtin_amdgcn_perm(w[8 * c + 2 * y + 1][j >> 1], w[8 * c + 2 * y][j >> 1],
+                                     j & 1 ? 0x07060302u : 0x05040100u);
+      return r;
+    } else {
+      return __uint_as_float(w[c][j]);
+    }
+  }
+};
+
+// Few rows: 32 of them a workgroup, whose waves share the keys out and join in
+// LDS.  Waves do not wait for each other before that.  Values come from the caches
+// straight into registers, whole rows by 32 lanes; keys, of which a lane wants a
+// row of its own (32 bytes of each of 32 rows a load), through a wave's own LDS in
+// bf16, one step ahead, and into registers in fp32, whose products take the longer.
+constexpr int kFewWaves = 4;
+template <typename T, int DH>
+__global__ __launch_bounds__(64 * kFewWaves, 1) void prompt_few_kernel(PromptCall a) {
+  typedef Rows<T, DH, 32> Base;
+  constexpr int E = Base::E, NK = Base::NK, ND = Base::ND, PV = E == 2 ? 2 : 16, W = DH / 32;
+  constexpr int PITCH = DH + 4;
+  constexpr int ROW = DH * E, SW = DH % 128 == 0 ? 16 : 8, NI = 32 * ROW / 1024;
+  constexpr int KEYS = E == 2 ? 2 * 32 * ROW : 0, JOIN = 32 * PITCH * 4;  // bytes of a wave
+  __shared__ float sm[kFewWaves][32], sl[kFewWaves][32];
+  __shared__ long long place[32];
+  constexpr int WORK = kFewWaves * (KEYS > JOIN ? KEYS : JOIN);
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[WORK + (E == 2 ? 32 * ROW : 0)];
+  unsigned char* queries = lds + (E == 2 ? WORK : 0);
+  const Base b(a);
+  if (b.row0 >= b.rows) return;
+  const int l32 = b.l32, lh = b.lh, wave = b.wave;
+  const int whole = b.limit(b.row0) / 32, steps = (b.limit(b.row0 + 31) + 31) / 32;
+  const T* kbase = static_cast<const T*>(a.k) + (size_t)b.k0 * a.ldk + b.kh * DH;
+  const T* vbase = static_cast<const T*>(a.v) + (size_t)b.k0 * a.ldv + b.kh * DH;
+  u32x4 kf[E == 4 ? NK : 1];
+  unsigned char* ring = lds + wave * KEYS;
+  const int kaddr = l32 * ROW + ((lh ^ swizzle<T, DH>(l32)) << 4);
+  // Part n of NI of the keys of step i (bf16); of no step, past the last.
+  auto load_keys = [&](int i, int stage, int n) __attribute__((always_inline)) {
+    lds_src src = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<T*>(kbase + (size_t)32 * min(i, steps - 1) * a.ldk), 0, i < steps ? 0x7fffffff : 0, 0x00020000);
+    const Slots<T, DH> at(b.lane);
+    int row, byte;
+    at.find(n, row, byte);
+    lds_dma16(src, ring + stage * 32 * ROW + 1024 * n, __umul24(min(row, b.nk - 1 - 32 * i), a.ldk * E) + byte, 0);
+  };
+  auto load_keys_fp32 = [&](int i) __attribute__((always_inline)) {
+    const T* row = kbase + (size_t)min(32 * i + l32, b.nk - 1) * a.ldk;
+#pragma unroll
+    for (int p = 0; p < NK; ++p)
+      if constexpr (E == 4) kf[p] = *reinterpret_cast<const u32x4*>(row + (2 * p + lh) * (16 / E));
+  };
+  if (wave < steps) {
+    if constexpr (E == 2) {
+#pragma unroll
+      for (int n = 0; n < NI; ++n) load_keys(wave, 0, n);
+    } else {
+      load_keys_fp32(wave);
+    }
+  }
+  u32x4 qf[NK];
+  const long long mine = b.template query<true>(b.row0, qf, queries, kFewWaves);
+  const int lim = b.limit(b.row0 + l32);
+  f32x16 o[ND];
+#pragma unroll
+  for (int d = 0; d < ND; ++d) o[d] = zeros16();
+  float m = -INFINITY, l = 0.f;  // l over the lane half's keys only
+  bool unruly = false;
+  int stage = 0;
+  for (int i = wave; i < steps; i += kFewWaves, stage ^= 1) {
+    const bool edge = i >= whole;
+    FewV<T, DH> v;
+    const lds_src vs = lds_source(vbase + (size_t)32 * i * a.ldv);
+    const int most = b.nk - 1 - 32 * i;  // rows past the prompt's last repeat it
+    auto load_value = [&](int x) __attribute__((always_inline)) {
+      v.load(x, vs, __umul24(min(8 * (x >> 2) + (x & 3) + 4 * lh, most), a.ldv * E) + W * E * l32);
+    };
+    f32x16 sc = zeros16();
+    u32x4 pf[2];
+    auto rescale = [&](float f) __attribute__((always_inline)) {
+#pragma unroll
+      for (int d = 0; d < ND; ++d) o[d] *= f;
+    };
+    if constexpr (E == 2) {
+      // A load holds its wave up for 16 cycles and more when four waves load: the
+      // values' go out among the scores' products, the next keys' among the softmax.
+      __builtin_amdgcn_s_waitcnt(0x7 << 4);  // this step's keys are there, nothing is under way
+      __builtin_amdgcn_sched_barrier(0);
+      f32x16 sc1 = zeros16();  // two chains of products
+      int kb = kaddr + stage * 32 * ROW;
+      asm volatile("" : "+v"(kb));
+      auto key = [&](int p) __attribute__((always_inline)) {
+        return *reinterpret_cast<const u32x4*>(ring + (kb ^ ((2 * p & (SW - 1)) << 4)) + 2 * p / SW * SW * 16);
+      };
+      u32x4 kr[3];
+#pragma unroll
+      for (int p = 0; p < 3; ++p) kr[p] = key(p);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int p = 0; p < NK; ++p) {
+        if (p & 1)
+          sc1 = mma32(kr[p % 3], qf[p], sc1, T{});
+        else
+          sc = mma32(kr[p % 3], qf[p], sc, T{});
+        if (p + 3 < NK) kr[p % 3] = key(p + 3);
+#pragma unroll
+        for (int x = 16 * p / NK; x < 16 * (p + 1) / NK; ++x) load_value(x);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      sc += sc1;
+      softmax<T>(sc, edge, 32 * i, lh, lim, a.scale, m, l, pf, rescale, [&](int r) __attribute__((always_inline)) {
+        if (r < NI) load_keys(i + kFewWaves, stage ^ 1, r);
+      });
+    } else {
+#pragma unroll
+      for (int x = 0; x < 16; ++x) load_value(x);
+#pragma unroll
+      for (int p = 0; p < NK; ++p) sc = mma32(kf[p], qf[p], sc, T{});
+      if (i + kFewWaves < steps) load_keys_fp32(i + kFewWaves);
+      softmax<T>(sc, edge, 32 * i, lh, lim, a.scale, m, l, pf, rescale, [](int) {});
+    }
+    if (edge && v.sift()) unruly = true;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int c = 0; c < PV; ++c) o[d] = product(v.operand(d, c), sc, pf, c, o[d]);
+  }
+
+  // The waves' sums, brought to the rows' common reference, join in LDS.
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  l = other_half_sum(l);
+  if (lh == 0) {
+    sm[wave][l32] = m;
+    sl[wave][l32] = l;
+    if (wave == 0) place[l32] = mine;
+  }
+  __syncthreads();  // and every wave is done with its keys
+  float f, all = 0.f, top = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < kFewWaves; ++w) top = fmaxf(top, sm[w][l32]);
+  const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+  for (int w = 0; w < kFewWaves; ++w) all += __builtin_amdgcn_exp2f(sm[w][l32] - ref) * sl[w][l32];
+  f = lim > 0 ? __builtin_amdgcn_exp2f(m - ref) / all : 0.f;  // no key seen: zeros
+  float* so = reinterpret_cast<float*>(lds) + wave * 32 * PITCH;
+#pragma unroll
+  for (int j = 0; j < 16; ++j)
+#pragma unroll
+    for (int d = 0; d < ND; ++d) so[l32 * PITCH + W * (8 * (j >> 2) + 4 * lh + (j & 3)) + d] = o[d][j] * f;
+  if (unruly) {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    for (int i = wave; i < steps; i += kFewWaves)
+      if (i >= whole)
+        add_unruly<DH>(vbase, a.ldv, 32 * i, min(32 * i + 32, b.nk), lim,
+                       [&](int r, int d) { return so + r * PITCH + d; });
+  }
+  __syncthreads();
+  constexpr int PER = 32 * (DH / 4) / (64 * kFewWaves);
+#pragma unroll
+  for (int n = 0; n < PER; ++n) {
+    const int u = threadIdx.x + n * 64 * kFewWaves, r = u / (DH / 4), d = 4 * (u % (DH / 4));
+    f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w)
+      acc += *reinterpret_cast<const f32x4*>(reinterpret_cast<float*>(lds) + (w * 32 + r) * PITCH + d);
+    if (b.row0 + r < b.rows)
+      store4(static_cast<T*>(a.out) + place[r] + d, acc[0], acc[1], acc[2], acc[3]);
+  }
+}
+
+enum { kFew, kHalves, kTiles };
+
+template <typename T, int DH>
+void prompt_at(PromptCall& a, int form, hipStream_t s) {
+  const int R = form == kFew ? 32 : 128;
+  a.n_slots = (int)((int64_t)a.n_q * a.group / R + a.n_seqs);
+  const dim3 grid((unsigned)(a.n_slots * a.n_kv));
+  if (form == kFew)
+    hipLaunchKernelGGL((prompt_few_kernel<T, DH>), grid, dim3(64 * kFewWaves), 0, s, a);
+  else if (form == kTiles)
+    hipLaunchKernelGGL((prompt_kernel<T, DH, 1>), grid, dim3(256), 0, s, a);
+  else if constexpr (sizeof(T) == 2)
+    hipLaunchKernelGGL((prompt_kernel<T, DH, 2>), grid, dim3(512), 0, s, a);
+}
+
+// Which kernel, by the 32-row tiles of the call (256 CUs; a CU holds one or two
+// workgroups).  us, heads 8/1 of 256, prompts of 560 tokens (one prompt): kFew 17
+// (23), kHalves 22 (33), kTiles 24 (40) at 280 tiles; 41 (97), 26 (83), 26 (105) at
+// 840; 77 (320), 43 (188), 35 (231) at 1680; 193 (1996), 89 (1179), 68 (1162) at
+// 4480.  Heads 32/8 of 128: 20, 15, 17 at 560; 50 (74), 23 (34), 22 (40) at 1680; 125
+// (364), 48 (186), 39 (172) at 4480.  A long causal prompt's last tiles outlast the
+// others, which halving the walk of each makes up for until the chip is full.
+// In fp32 products are 16 times as long, and 128 rows leave CUs idle for longer:
+// heads of 64 and 560 tokens, kFew 28, kTiles 47 at 560 tiles, 97 and 110 at 2240, 186
+// and 141 at 4480; of 256, where kFew spills, 145 and 160 at 420, 244 and 163 at 840.
+int prompt_form(const fv_prompt_args& x) {
+  const int64_t tiles = (int64_t)x.n_q * x.n_q_heads / 32;
+  if (x.dtype == FV_FP32) return tiles <= (x.head_dim == 256 ? 480 : 2048) ? kFew : kTiles;
+  if (tiles < 384) return kFew;
+  const bool few_long = x.causal && x.n_k / x.n_seqs >= 2048;
+  return tiles <= (few_long ? 2048 : 1024) ? kHalves : kTiles;
 }
 
 }  // namespace
@@ -494,20 +800,12 @@ void launch_prompt(const fv_prompt_args& x, hipStream_t s) {
   a.group = x.n_q_heads / x.n_kv_heads;
   a.causal = x.causal;
   a.scale = x.scale * kLog2e;
-  if constexpr (sizeof(T) == 2) {
-    switch (x.head_dim) {
-      case 64: return prompt_at<T, 64, 4, 2>(a, s);
-      case 128: return prompt_at<T, 128, 4, 2>(a, s);
-      case 192: return prompt_at<T, 192, 8, 1>(a, s);
-      default: return prompt_at<T, 256, 8, 1>(a, s);
-    }
-  } else {
-    switch (x.head_dim) {
-      case 64: return prompt_at<T, 64, 4, 1>(a, s);
-      case 128: return prompt_at<T, 128, 4, 1>(a, s);
-      case 192: return prompt_at<T, 192, 4, 1>(a, s);
-      default: return prompt_at<T, 256, 4, 1>(a, s);
-    }
+  const int form = prompt_form(x);
+  switch (x.head_dim) {
+    case 64: return prompt_at<T, 64>(a, form, s);
+    case 128: return prompt_at<T, 128>(a, form, s);
+    case 192: return prompt_at<T, 192>(a, form, s);
+    default: return prompt_at<T, 256>(a, form, s);
   }
 }
 template void launch_prompt<bf16_t>(const fv_prompt_args&, hipStream_t);

@@ -12,6 +12,11 @@ pytestmark = pytest.mark.gpu
 SHAPES = [("bf16", 8, 1, 256), ("bf16", 8, 2, 128), ("bf16", 4, 4, 64), ("bf16", 6, 2, 192),
           ("bf16", 5, 1, 128), ("fp32", 4, 2, 64), ("fp32", 2, 1, 256), ("fp32", 3, 3, 192),
           ("fp32", 8, 2, 128)]
+# Enough rows (300 tokens or so by these heads) for the kernels of fuller chips:
+# eight waves halving the keys, four waves, fp32
+FULL = [("bf16", 64, 4, D) for D in (64, 128, 192, 256)] + [
+    ("bf16", 128, 16, D) for D in (64, 128, 192, 256)] + [("bf16", 126, 18, 128)] + [
+    ("fp32", 256, 32, D) for D in (64, 128, 192, 256)]
 # (queries, keys) of each prompt
 LENS = {"ragged": [(0, 0), (1, 1), (33, 33), (64, 64), (65, 65), (0, 5), (130, 130), (7, 7)],
         "tails": [(1, 300), (5, 64), (32, 97), (3, 3), (100, 517)],
@@ -63,7 +68,18 @@ def test_against_the_definition(shape, lens, causal):
             assert not out[:5].any()
 
 
-@pytest.mark.parametrize("shape", [SHAPES[1], SHAPES[3], SHAPES[5]], ids=str)
+@pytest.mark.parametrize("lens,causal", [("ragged", True), ("ragged", False), ("mixed", True)])
+@pytest.mark.parametrize("shape", FULL, ids=lambda s: "x".join(map(str, s)))
+def test_fuller_chips(shape, lens, causal):
+    pairs = LENS.get(lens, [(40, 9), (129, 400), (0, 3), (3, 0), (60, 260), (66, 66), (1, 700)])
+    q, k, v, cq, ck = make(shape, pairs)
+    out = run(q, k, v, cq, ck, causal)
+    check(shape, out, q, k, v, cq, ck, causal)
+    if lens == "mixed":
+        assert not out[:31].any() and not out[cq[3]:cq[4]].any()
+
+
+@pytest.mark.parametrize("shape", [SHAPES[1], SHAPES[3], SHAPES[5], FULL[1], FULL[5], FULL[9]], ids=str)
 def test_strided_rows_and_rows_behind_the_last_prompt(shape):
     torch = cu.torch_mod()
     dtype, H, G, D = shape
@@ -82,7 +98,8 @@ def test_strided_rows_and_rows_behind_the_last_prompt(shape):
 
 @pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
 @pytest.mark.parametrize("where", ["k", "v"])
-@pytest.mark.parametrize("shape", [SHAPES[0], SHAPES[1], SHAPES[2], SHAPES[3], SHAPES[6]], ids=str)
+@pytest.mark.parametrize("shape", [SHAPES[0], SHAPES[1], SHAPES[2], SHAPES[3], SHAPES[6], FULL[0], FULL[3],
+                                   FULL[5], FULL[6], FULL[9], FULL[12]], ids=str)
 def test_unseen_keys_have_no_influence(shape, where, bad):
     """A key or value that is not finite changes only the rows that see it, bit for bit."""
     torch = cu.torch_mod()
@@ -107,7 +124,7 @@ def test_unseen_keys_have_no_influence(shape, where, bad):
         assert out[cq[1] + 80:cq[2]].isnan().all()
 
 
-@pytest.mark.parametrize("shape", [SHAPES[0], SHAPES[2], SHAPES[5]], ids=str)
+@pytest.mark.parametrize("shape", [SHAPES[0], SHAPES[2], SHAPES[5], FULL[0], FULL[5], FULL[9]], ids=str)
 def test_scores_without_a_softmax_and_rising_ones(shape):
     torch = cu.torch_mod()
     dtype, H, G, D = shape
@@ -155,11 +172,11 @@ def test_scale_and_no_rows():
     assert (out == 7).all()
 
 
-def test_replayed_graph_and_other_stream():
+@pytest.mark.parametrize("shape", [SHAPES[0], FULL[1], FULL[6]], ids=str)
+def test_replayed_graph_and_other_stream(shape):
     torch = cu.torch_mod()
     from paper_2608_27384_amd.flashvla import prompt_attention
-    shape = SHAPES[0]
-    q, k, v, cq, ck = make(shape, [(100, 100), (61, 90)])
+    q, k, v, cq, ck = make(shape, [(150, 150), (111, 190)])
     dq, dk = cu.ints(cq), cu.ints(ck)
     want = run(q, k, v, cq, ck, True)
     out = torch.zeros_like(q)
