@@ -435,63 +435,75 @@ def _refuse(message: str):
     raise FlashVLAError(FV_ERR_INVALID_ARG, message)
 
 
+_torch = None
+
+
+def _tmod():
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
 def _dtype(t, what: str) -> int:
-    name = str(t.dtype)
-    if name == "torch.bfloat16":
+    torch = _tmod()
+    if t.dtype is torch.bfloat16:
         return FV_BF16
-    if name != "torch.float32":
-        _refuse(f"{what} must be bfloat16 or float32, not {name}")
+    if t.dtype is not torch.float32:
+        _refuse(f"{what} must be bfloat16 or float32, not {t.dtype}")
     return FV_FP32
 
 
-def _rows(t, what: str, like=None, shape=None) -> int:
+def _rows(t, what: str, dtype, device, shape=None) -> int:
     """Leading dimension of a [tokens, heads, head_dim] tensor whose heads lie side by side."""
-    if like is not None and (t.dtype != like.dtype or t.device != like.device):
-        _refuse(f"{what} must have dtype {like.dtype} on {like.device}")
-    if t.dim() != 3 or (shape is not None and tuple(t.shape) != tuple(shape)):
-        _refuse(f"{what} has shape {tuple(t.shape)}" + (f", not {tuple(shape)}" if shape else ""))
-    n, h, d = t.shape
-    st = t.stride()
-    if (d > 1 and st[2] != 1) or (h > 1 and st[1] != d):
-        _refuse(f"the heads of {what} must lie side by side (strides {st})")
-    return st[0] if n > 1 else h * d
+    got = t.shape
+    if t.dtype is not dtype or t.device != device:
+        _refuse(f"{what} must have dtype {dtype} on {device}")
+    if len(got) != 3 or (shape is not None and got != shape):
+        _refuse(f"{what} has shape {tuple(got)}" + (f", not {tuple(shape)}" if shape else ""))
+    n, h, d = got
+    ld, sh, sd = t.stride()
+    if (sd != 1 and d > 1) or (sh != d and h > 1):
+        _refuse(f"the heads of {what} must lie side by side (strides {(ld, sh, sd)})")
+    return ld if n > 1 else h * d
 
 
 def _int32(t, what: str, device, shape=None) -> int:
     """Pointer of a dense int32 tensor."""
-    if str(t.dtype) != "torch.int32" or t.device != device or not t.is_contiguous():
+    if t.dtype is not _tmod().int32 or t.device != device or not t.is_contiguous():
         _refuse(f"{what} must be a contiguous int32 tensor on {device}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape:
         _refuse(f"{what} has shape {tuple(t.shape)}, not {tuple(shape)}")
     return t.data_ptr()
 
 
 class _On:
-    """The GPU of a tensor and the stream of a call, for its duration: the C calls
-    take the NULL stream to be the current GPU's, and a workspace has to come from
-    the allocator's pool of the stream that uses it."""
+    """The raw stream of a call, and for the call's duration the GPU and stream that
+    it runs on as torch's current ones where they are others: the C calls take the
+    NULL stream to be the current GPU's, and a workspace has to come from the
+    allocator's pool of the stream that uses it."""
+
+    __slots__ = ("raw", "scope")
 
     def __init__(self, device, stream):
-        import torch
+        torch = _tmod()
         if device.type != "cuda":
             _refuse(f"tensors must be on a GPU, not {device}")
-        self.device, self.given, self.scope = device, stream is not None, None
+        self.scope = None
         if stream is None:
-            self.stream = torch.cuda.current_stream(device)
-        elif isinstance(stream, torch.cuda.Stream):
-            self.stream = stream
+            self.raw = torch._C._cuda_getCurrentRawStream(device.index)
+            if torch._C._cuda_getDevice() != device.index:
+                self.scope = torch.cuda.device(device)
         else:
-            self.stream = torch.cuda.ExternalStream(int(stream), device=device)
-        if self.given and self.stream.device != device:
-            _refuse(f"the stream is of {self.stream.device}, the tensors of {device}")
-        self.raw = int(self.stream.cuda_stream)
+            if not isinstance(stream, torch.cuda.Stream):
+                stream = torch.cuda.ExternalStream(int(stream), device=device)
+            if stream.device != device:
+                _refuse(f"the stream is of {stream.device}, the tensors of {device}")
+            self.raw = int(stream.cuda_stream)
+            self.scope = torch.cuda.stream(stream)
 
     def __enter__(self):
-        import torch
-        if self.given:
-            self.scope = torch.cuda.stream(self.stream)
-        elif torch.cuda.current_device() != self.device.index:
-            self.scope = torch.cuda.device(self.device)
         if self.scope is not None:
             self.scope.__enter__()
         return self
@@ -501,9 +513,9 @@ class _On:
             self.scope.__exit__(*exc)
         return False
 
-    def work(self, nbytes: int):
-        import torch
-        return torch.empty(nbytes, dtype=torch.uint8, device=self.device) if nbytes else None
+
+def _work(nbytes: int, device):
+    return _tmod().empty(nbytes, dtype=_tmod().uint8, device=device)
 
 
 def prompt_attention(q, k, v, cu_q, cu_k, out, causal: bool = True, scale: Optional[float] = None,
@@ -511,21 +523,22 @@ def prompt_attention(q, k, v, cu_q, cu_k, out, causal: bool = True, scale: Optio
     """fv_prompt_attention on torch tensors: q and out [tokens, heads, head_dim], k and v
     [keys, kv heads, head_dim] (rows may be strided), cu_q and cu_k int32 [prompts + 1].
     `scale` defaults to 1/sqrt(head_dim)."""
-    dtype = _dtype(q, "q")
-    ldq = _rows(q, "q")
-    ldk, ldv = _rows(k, "k", q), _rows(v, "v", q, k.shape)
-    ldo = _rows(out, "out", q, q.shape)
-    n_q, heads, dh = q.shape
-    if k.shape[2] != dh:
-        _refuse(f"head_dim of q is {dh}, of k {k.shape[2]}")
-    if cu_q.dim() != 1 or len(cu_q) < 1:
+    dtype, t, dev, shape = _dtype(q, "q"), q.dtype, q.device, q.shape
+    ldq, ldo = _rows(q, "q", t, dev), _rows(out, "out", t, dev, shape)
+    ldk = _rows(k, "k", t, dev)
+    ldv = _rows(v, "v", t, dev, k.shape)
+    n_q, heads, dh = shape
+    n_k, kv_heads, dk = k.shape
+    if dk != dh:
+        _refuse(f"head_dim of q is {dh}, of k {dk}")
+    prompts = cu_q.shape
+    if len(prompts) != 1 or prompts[0] < 1:
         _refuse("cu_q must have prompts + 1 entries")
-    with _On(q.device, stream) as on:
-        args = FvPromptArgs(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), ldq, ldk, ldv,
-                            ldo, _int32(cu_q, "cu_q", q.device),
-                            _int32(cu_k, "cu_k", q.device, cu_q.shape), len(cu_q) - 1, n_q,
-                            k.shape[0], heads, k.shape[1], dh, dtype, 1 if causal else 0,
-                            dh ** -0.5 if scale is None else scale)
+    args = FvPromptArgs(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), ldq, ldk, ldv, ldo,
+                        _int32(cu_q, "cu_q", dev), _int32(cu_k, "cu_k", dev, prompts),
+                        prompts[0] - 1, n_q, n_k, heads, kv_heads, dh, dtype, 1 if causal else 0,
+                        dh ** -0.5 if scale is None else scale)
+    with _On(dev, stream) as on:
         _check_context(lib().fv_prompt_attention(byref(args), on.raw), "fv_prompt_attention")
 
 
@@ -536,24 +549,25 @@ def rope(q, k, pos, sections: Sequence[int], q_out, k_out=None, theta: float = 1
 
 
 def _rope(cache, layer, q, k, v, pos, seqs, at, sections, theta, q_out, k_out, stream) -> None:
-    dtype = _dtype(q, "q")
-    n, heads, dh = q.shape if q.dim() == 3 else _refuse(f"q has shape {tuple(q.shape)}")
-    if k.dim() != 3 or k.shape[0] != n or k.shape[2] != dh:
+    dtype, t, dev = _dtype(q, "q"), q.dtype, q.device
+    ldq, ldk = _rows(q, "q", t, dev), _rows(k, "k", t, dev)
+    n, heads, dh = q.shape
+    nk, kv_heads, dk = k.shape
+    if nk != n or dk != dh:
         _refuse(f"k has shape {tuple(k.shape)}, q {tuple(q.shape)}")
-    ldq, ldk = _rows(q, "q"), _rows(k, "k", q)
-    ldv = _rows(v, "v", q, k.shape) if v is not None else 0
-    ldq_out = _rows(q_out, "q_out", q, q.shape)
-    ldk_out = _rows(k_out, "k_out", q, k.shape) if k_out is not None else 0
-    if not 1 <= len(sections) <= 4:
+    axes = len(sections)
+    if not 1 <= axes <= 4:
         _refuse("sections must have 1 to 4 entries")
-    dev = q.device
     args = FvRopeArgs(q.data_ptr(), k.data_ptr(), _ptr(v), q_out.data_ptr(), _ptr(k_out), ldq, ldk,
-                      ldv, ldq_out, ldk_out, _int32(pos, "pos", dev, (len(sections), n)),
+                      _rows(v, "v", t, dev, k.shape) if v is not None else 0,
+                      _rows(q_out, "q_out", t, dev, q.shape),
+                      _rows(k_out, "k_out", t, dev, k.shape) if k_out is not None else 0,
+                      _int32(pos, "pos", dev, (axes, n)),
                       _int32(seqs, "seqs", dev, (n,)) if seqs is not None else None,
-                      _int32(at, "at", dev, (n,)) if at is not None else None, n, heads, k.shape[1],
-                      dh, dtype, layer, len(sections), (c_int32 * 4)(*sections), theta)
+                      _int32(at, "at", dev, (n,)) if at is not None else None, n, heads, kv_heads,
+                      dh, dtype, layer, axes, tuple(sections), theta)
     with _On(dev, stream) as on:
-        _check_context(lib().fv_rope_append(byref(args), byref(cache) if cache is not None else None,
+        _check_context(lib().fv_rope_append(byref(args), None if cache is None else byref(cache),
                                             on.raw), "fv_rope_append")
 
 
@@ -579,12 +593,15 @@ class PageCache:
                          k.data_ptr(), v.data_ptr(), _int32(table, "table", dev),
                          _int32(length, "length", dev, table.shape[:1]),
                          _int32(refs, "refs", dev, (pages,)))
+        need = c_size_t()
+        _check_context(lib().fv_pages_workspace(byref(self.c), byref(need)), "PageCache")
+        self.work_bytes = need.value  # of the upkeep's calls
 
     @classmethod
     def empty(cls, n_layers: int, n_kv_heads: int, head_dim: int, n_pages: int, max_seqs: int,
               max_pages: int, page_len: int = 16, dtype=None, device="cuda"):
         """A fresh cache: uninitialised pages, no sequences."""
-        import torch
+        torch = _tmod()
         dtype = torch.bfloat16 if dtype is None else dtype
         shape = (n_layers, n_pages, n_kv_heads, page_len, head_dim)
         k, v = (torch.empty(shape, dtype=dtype, device=device) for _ in range(2))
@@ -604,41 +621,37 @@ class PageCache:
     def attend(self, layer: int, q, seqs, out, scale: Optional[float] = None, max_len: int = 0,
                stream=None) -> None:
         """fv_paged_attention: q and out [rows, heads, head_dim], seqs int32 [rows]."""
-        ldq, ldo = _rows(q, "q", self.k), _rows(out, "out", self.k, q.shape)
+        t, dev = self.k.dtype, self.k.device
+        ldq = _rows(q, "q", t, dev)
+        ldo = _rows(out, "out", t, dev, q.shape)
         n, heads, dh = q.shape
+        cache = byref(self.c)
         if dh != self.c.head_dim:
             _refuse(f"head_dim of q is {dh}, of the cache {self.c.head_dim}")
-        with _On(q.device, stream) as on:
-            args = FvPagedArgs(q.data_ptr(), out.data_ptr(), ldq, ldo,
-                               _int32(seqs, "seqs", q.device, (n,)), n, heads, layer, max_len,
-                               dh ** -0.5 if scale is None else scale, None, 0)
-            need = c_size_t()
-            L = lib()
-            _check_context(L.fv_paged_attention_workspace(byref(args), byref(self.c), byref(need)),
-                           "fv_paged_attention")
-            work = on.work(need.value)
-            if work is not None:
+        args = FvPagedArgs(q.data_ptr(), out.data_ptr(), ldq, ldo, _int32(seqs, "seqs", dev, (n,)), n,
+                           heads, layer, max_len, dh ** -0.5 if scale is None else scale, None, 0)
+        with _On(dev, stream) as on:
+            need, L, a = c_size_t(), lib(), byref(args)
+            _check_context(L.fv_paged_attention_workspace(a, cache, byref(need)), "fv_paged_attention")
+            if need.value:
+                work = _work(need.value, dev)
                 args.work, args.work_bytes = work.data_ptr(), need.value
-            _check_context(L.fv_paged_attention(byref(args), byref(self.c), on.raw),
-                           "fv_paged_attention")
+            _check_context(L.fv_paged_attention(a, cache, on.raw), "fv_paged_attention")
 
     def _upkeep(self, name: str, stream, *lists, status=None, work=True):
-        import torch
         dev = self.k.device
         n = lists[0].shape[0] if lists else 0
-        ptrs = [_int32(t, name + " list", dev, (n,)) for t in lists]
+        args = [byref(self.c), *[_int32(t, name + " list", dev, (n,)) for t in lists]]
+        if lists:
+            args.append(n)
         with _On(dev, stream) as on:
             if status is None:
-                status = torch.empty(1, dtype=torch.int32, device=dev)
-            args = [byref(self.c), *ptrs, *([n] if lists else []),
-                    _int32(status, "status", dev, (1,))]
-            L = lib()
+                status = _tmod().empty(1, dtype=_tmod().int32, device=dev)
+            args.append(_int32(status, "status", dev, (1,)))
             if work:
-                need = c_size_t()
-                _check_context(L.fv_pages_workspace(byref(self.c), byref(need)), name)
-                buf = on.work(need.value)
+                buf = _work(self.work_bytes, dev)
                 args.append(buf.data_ptr())
-            _check_context(getattr(L, name)(*args, on.raw), name)
+            _check_context(getattr(lib(), name)(*args, on.raw), name)
         return status
 
     def grow(self, seqs, add, status=None, stream=None):
