@@ -134,11 +134,18 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_kernel(PagedCall a)
   const int ch = id % a.n_chunks, row = id / a.n_chunks;
   const int s = a.seqs[row];
   if (s < 0 || s >= a.max_seqs) return;
+  const int k0 = ch * a.chunk;
+  const int* table = a.table + (size_t)s * a.max_pages;
+  auto page_at = [&](int key) __attribute__((always_inline)) {
+    const int p = key / a.page_len;
+    return p < a.max_pages ? table[p] : -1;
+  };
+  // the first page numbers are fetched together with the length
+  int page = page_at(k0 + (wave + kPagedWaves * (lane / NH)) * KT + 16 * (lane % NH));
   const int len = length_of(a, s);
   const int chunks = chunks_of(len, a.chunk, a.n_chunks);
   if (ch >= chunks && ch > 0) return;
-  const int k0 = ch * a.chunk, k1 = ch == a.n_chunks - 1 ? len : min(len, k0 + a.chunk);
-  const int* table = a.table + (size_t)s * a.max_pages;
+  const int k1 = ch == a.n_chunks - 1 ? len : min(len, k0 + a.chunk);
 
   // queries: the head of column l16, zeros past the group
   const int head = qt * 16 + l16;
@@ -165,33 +172,36 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_kernel(PagedCall a)
   constexpr int GO = 64 / NH;
   for (int base = wave; base < tiles; base += kPagedWaves * GO) {
     const int myKey = k0 + (base + kPagedWaves * (lane / NH)) * KT + 16 * (lane % NH);
-    int page = -1;
-    if (myKey < k1) {
-      page = table[myKey / a.page_len];
-      if (page < 0 || page >= a.n_pages) page = -1;
-    }
+    if (base != wave) page = page_at(myKey);
+    if (myKey >= k1 || page < 0 || page >= a.n_pages) page = -1;
     const int off = page >= 0 ? myKey % a.page_len : 0;
     const int here = min(GO, (tiles - base + kPagedWaves - 1) / kPagedWaves);
-    for (int it = 0; it < here; ++it) {
-      const int key0 = k0 + (base + kPagedWaves * it) * KT;
-      const T* krow[NH];
-      const T* vrow[NH];
-      int left[NH];  // keys of the half that are there
+    // first rows of a tile's halves, and how many of their keys are there
+    auto rows = [&](int it, const T* pool, const T* (&row)[NH], int (&left)[NH]) __attribute__((always_inline)) {
 #pragma unroll
       for (int h = 0; h < NH; ++h) {
         const int pg = __builtin_amdgcn_readlane(page, it * NH + h);
         const int of = __builtin_amdgcn_readlane(off, it * NH + h);
-        left[h] = pg < 0 ? 0 : min(16, k1 - (key0 + 16 * h));
-        const size_t at = (page_row(pg < 0 ? 0 : pg, a.n_kv, kh, a.page_len) + of) * DH;
-        krow[h] = kp + at;
-        vrow[h] = vp + at;
+        left[h] = pg < 0 ? 0 : min(16, k1 - (k0 + (base + kPagedWaves * it) * KT + 16 * h));
+        row[h] = pool + (page_row(pg < 0 ? 0 : pg, a.n_kv, kh, a.page_len) + of) * DH;
       }
-      u32x4 kf[NH][KB];
+    };
+    u32x4 kf[NH][KB];
+    auto load_keys = [&](int it) __attribute__((always_inline)) {
+      const T* row[NH];
+      int left[NH];
+      rows(it, kp, row, left);
 #pragma unroll
       for (int h = 0; h < NH; ++h)
 #pragma unroll
         for (int b = 0; b < KB; ++b)
-          kf[h][b] = *reinterpret_cast<const u32x4*>(krow[h] + (size_t)l16 * DH + EB * b + (EB / 4) * lg);
+          kf[h][b] = *reinterpret_cast<const u32x4*>(row[h] + (size_t)l16 * DH + EB * b + (EB / 4) * lg);
+    };
+    load_keys(0);
+    for (int it = 0; it < here; ++it) {
+      const T* vrow[NH];
+      int left[NH];
+      rows(it, vp, vrow, left);
       VTile<T, DH> vt;
       vt.load(vrow, l16, lg);
 
@@ -202,6 +212,8 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_kernel(PagedCall a)
 #pragma unroll
         for (int b = 0; b < KB; ++b) sc[h] = mma64(kf[h][b], qf[b], sc[h], T{});
       }
+      __builtin_amdgcn_sched_barrier(0);
+      if (it + 1 < here) load_keys(it + 1);  // while the softmax and the values are at work
       bool whole = true;
 #pragma unroll
       for (int h = 0; h < NH; ++h) {
@@ -311,31 +323,89 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_kernel(PagedCall a)
   }
 }
 
-// Joins a row's chunks: block (row, head), DH/4 threads.
-template <typename T, int DH>
-__global__ __launch_bounds__(64) void paged_join_kernel(PagedCall a) {
+// Joins a row's chunks: a workgroup per (row, head), its WAVES waves taking every
+// WAVES-th chunk, four elements a lane.  The first chunks' sums are fetched together
+// with the length, before it is known which of them hold anything; chunk c's maximum
+// and sum are a lane's, which makes the chunk's weight of them.
+template <typename T, int DH, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void paged_join_kernel(PagedCall a) {
+  constexpr int FIRST = 8;
+  __shared__ float weight[WAVES][64];
+  __shared__ float sm[WAVES], sl[WAVES];
+  __shared__ __attribute__((aligned(16))) float so[WAVES][DH];
   const int row = blockIdx.x / a.heads, qh = blockIdx.x - row * a.heads;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int s = a.seqs[row];
+  const size_t at = (size_t)row * a.n_chunks * a.heads + qh;  // of chunk 0; the next is `heads` on
+  const int d = 4 * lane < DH ? 4 * lane : 0;
+  auto part = [&](int c) __attribute__((always_inline)) {
+    return *reinterpret_cast<const f32x4*>(a.part + (at + (size_t)c * a.heads) * DH + d);
+  };
+  f32x4 x[FIRST];
+#pragma unroll
+  for (int i = 0; i < FIRST; ++i) x[i] = part(min(wave + i * WAVES, a.n_chunks - 1));
   if (s < 0 || s >= a.max_seqs) return;
   const int chunks = max(1, chunks_of(length_of(a, s), a.chunk, a.n_chunks));
-  const int d = 4 * threadIdx.x;
-  float m = -INFINITY, l = 0.f;
-  bool some = false;
-  for (int ch = 0; ch < chunks; ++ch)
-    m = fmaxf(m, a.stat[2 * (((size_t)row * a.n_chunks + ch) * a.heads + qh)]);
-  const float ref = m == -INFINITY ? 0.f : m;
+  const int mine = (chunks - wave + WAVES - 1) / WAVES;  // chunks of this wave, may be none
+
+  float m = -INFINITY, l = -1.f;  // a sum of -1: no key
   f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int ch = 0; ch < chunks; ++ch) {
-    const size_t at = ((size_t)row * a.n_chunks + ch) * a.heads + qh;
-    const float lc = a.stat[2 * at + 1];
-    if (lc == -1.f) continue;
-    some = true;
-    const float f = __builtin_amdgcn_exp2f(a.stat[2 * at] - ref);
-    l += f * lc;
-    if (d < DH) acc += f * *reinterpret_cast<const f32x4*>(a.part + at * DH + d);
+  for (int i0 = 0; i0 < mine; i0 += 64) {
+    const int n = min(64, mine - i0);
+    float mc = -INFINITY, lc = -1.f;
+    if (lane < n) {
+      const float* st = a.stat + 2 * (at + (size_t)(wave + (i0 + lane) * WAVES) * a.heads);
+      mc = st[0];
+      lc = st[1];
+    }
+    const bool here = lc != -1.f;
+    if (!__any(here)) continue;
+    float now = fmaxf(m, mc);
+#pragma unroll
+    for (int y = 1; y < 64; y <<= 1) now = fmaxf(now, __shfl_xor(now, y));
+    const float ref = now == -INFINITY ? 0.f : now;
+    const float old = l == -1.f ? 0.f : __builtin_amdgcn_exp2f(m - ref);
+    const float f = here ? __builtin_amdgcn_exp2f(mc - ref) : 0.f;
+    l = (l == -1.f ? 0.f : l * old) + wave_sum(here ? f * lc : 0.f);
+    m = now;
+    acc *= old;
+    weight[wave][lane] = here ? f : -1.f;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (i0 == 0) {
+#pragma unroll
+      for (int i = 0; i < FIRST; ++i)
+        if (i < n && weight[wave][i] != -1.f) acc += weight[wave][i] * x[i];
+    }
+#pragma unroll 8
+    for (int i = i0 == 0 ? FIRST : 0; i < n; ++i) {
+      const float w = weight[wave][i];
+      const f32x4 y = part(wave + (i0 + i) * WAVES);
+      if (w != -1.f) acc += w * y;
+    }
   }
-  if (d >= DH) return;
-  const float inv = some ? 1.0f / l : 0.f;
+  if constexpr (WAVES > 1) {
+    if (lane == 0) {
+      sm[wave] = m;
+      sl[wave] = l;
+    }
+    if (4 * lane < DH) *reinterpret_cast<f32x4*>(&so[wave][d]) = acc;
+    __syncthreads();
+    if (wave) return;
+    m = -INFINITY;
+    for (int w = 0; w < WAVES; ++w) m = fmaxf(m, sm[w]);
+    const float ref = m == -INFINITY ? 0.f : m;
+    l = -1.f;
+    acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w)
+      if (sl[w] != -1.f) {
+        const float f = __builtin_amdgcn_exp2f(sm[w] - ref);
+        l = (l == -1.f ? 0.f : l) + f * sl[w];
+        acc += f * *reinterpret_cast<const f32x4*>(&so[w][d]);
+      }
+  }
+  if (4 * lane >= DH) return;
+  const float inv = l == -1.f ? 0.f : 1.0f / l;
   store4(static_cast<T*>(a.out) + (size_t)row * a.ldo + qh * DH + d, acc[0] * inv, acc[1] * inv,
          acc[2] * inv, acc[3] * inv);
 }
@@ -344,8 +414,10 @@ template <typename T, int DH>
 void paged_at(const PagedCall& a, hipStream_t s) {
   const int blocks = a.n * a.n_chunks * a.n_kv * a.q_tiles;
   hipLaunchKernelGGL((paged_kernel<T, DH>), dim3(blocks), dim3(64 * kPagedWaves), 0, s, a);
-  if (a.n_chunks > 1)
-    hipLaunchKernelGGL((paged_join_kernel<T, DH>), dim3(a.n * a.heads), dim3(64), 0, s, a);
+  if (a.n_chunks > 16)
+    hipLaunchKernelGGL((paged_join_kernel<T, DH, 8>), dim3(a.n * a.heads), dim3(512), 0, s, a);
+  else if (a.n_chunks > 1)
+    hipLaunchKernelGGL((paged_join_kernel<T, DH, 1>), dim3(a.n * a.heads), dim3(64), 0, s, a);
 }
 
 }  // namespace

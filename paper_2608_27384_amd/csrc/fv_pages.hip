@@ -165,20 +165,25 @@ __device__ bool mark(PlanShared& sh, int s) {
 }
 
 // Pages p0 + 1024 w + 64 j + lane, j = 0..15, of the wave w: which of them `pick` takes.
-template <typename Pick>
-__device__ __forceinline__ int pick_pages(const fv_pages& c, int first, uint64_t (&m)[16], Pick pick) {
-  const int lane = threadIdx.x & 63;
+struct Holders {
   int refs[16];
+  __device__ __forceinline__ void load(const fv_pages& c, int first) {
 #pragma unroll
-  for (int j = 0; j < 16; ++j) {
-    const int p = first + 64 * j + lane;
-    refs[j] = p < c.n_pages ? c.refs[p] : 0;
+    for (int j = 0; j < 16; ++j) {
+      const int p = first + 64 * j + (int)(threadIdx.x & 63);
+      refs[j] = p < c.n_pages ? c.refs[p] : 0;
+    }
   }
+};
+template <typename Pick>
+__device__ __forceinline__ int pick_pages(const fv_pages& c, const Holders& h, int first,
+                                          uint64_t (&m)[16], Pick pick) {
+  const int lane = threadIdx.x & 63;
   int n = 0;
 #pragma unroll
   for (int j = 0; j < 16; ++j) {
     const int p = first + 64 * j + lane;
-    m[j] = __ballot(p < c.n_pages && pick(p, refs[j]));
+    m[j] = __ballot(p < c.n_pages && pick(p, h.refs[j]));
     n += __popcll(m[j]);
   }
   return n;
@@ -194,14 +199,16 @@ __device__ __forceinline__ void list_pages(const uint64_t (&m)[16], int first, i
   }
 }
 
-// The lowest `want` free pages into list; how many there are, at most want.
-__device__ int take_free(const fv_pages& c, int want, int* list, PlanShared& sh) {
+// The lowest `want` free pages into list; how many there are, at most want.  h: the
+// wave's holders of the first kScanPages, loaded while the call was being checked.
+__device__ int take_free(const fv_pages& c, Holders& h, int want, int* list, PlanShared& sh) {
   const int w = threadIdx.x >> 6;
   int found = 0;
   for (int p0 = 0; p0 < c.n_pages && found < want; p0 += kScanPages) {
     const int first = p0 + w * 1024;
+    if (p0) h.load(c, first);
     uint64_t m[16];
-    const int n = pick_pages(c, first, m, [](int, int refs) { return refs <= 0; });
+    const int n = pick_pages(c, h, first, m, [](int, int refs) { return refs <= 0; });
     __syncthreads();
     if ((threadIdx.x & 63) == 0) sh.wave[0][w] = n;
     __syncthreads();
@@ -210,7 +217,7 @@ __device__ int take_free(const fv_pages& c, int want, int* list, PlanShared& sh)
       before += i < w ? sh.wave[0][i] : 0;
       all += sh.wave[0][i];
     }
-    list_pages(m, first, found + before, want, list);
+    if (found + before < want) list_pages(m, first, found + before, want, list);
     found += all;
   }
   __syncthreads();
@@ -234,6 +241,8 @@ __global__ __launch_bounds__(kPlanThreads) void grow_plan_kernel(fv_pages c, con
   __shared__ PlanShared sh;
   int* A = work + kPagesHeader;
   int* B = A + list;
+  Holders h;
+  h.load(c, (threadIdx.x >> 6) * 1024);
   clear_seen(sh, c.max_seqs);
   long long total = 0;
   for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
@@ -260,7 +269,7 @@ __global__ __launch_bounds__(kPlanThreads) void grow_plan_kernel(fv_pages c, con
   }
   __syncthreads();
   if (sh.bad) return verdict(FV_PAGES_BAD, status, work);
-  if (total > c.n_pages || take_free(c, (int)total, A, sh) < total)
+  if (total > c.n_pages || take_free(c, h, (int)total, A, sh) < total)
     return verdict(FV_PAGES_FULL, status, work);
   verdict(FV_PAGES_OK, status, work);
 }
@@ -289,22 +298,20 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(fv_pages c, con
   __shared__ PlanShared sh;
   int* A = work + kPagesHeader;
   int* B = A + list;
+  Holders h;
+  h.load(c, (threadIdx.x >> 6) * 1024);
   clear_seen(sh, c.max_seqs);
-  for (int i = threadIdx.x; i < n; i += kPlanThreads) {
-    const int s = children[i];
-    if (s < 0 || s >= c.max_seqs || mark(sh, s) || c.len[s] != 0) sh.bad = 1;
-  }
-  __syncthreads();
+  const int holds = c.max_pages * c.page_len;
   int total = 0;
   for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
     const int i = i0 + threadIdx.x;
     int need = 0;
     if (i < n) {
-      const int s = parents[i];
-      bool ok = s >= 0 && s < c.max_seqs && !(sh.seen[s >> 5] >> (s & 31) & 1);
+      const int cs = children[i], ps = parents[i];
+      bool ok = cs >= 0 && cs < c.max_seqs && ps >= 0 && ps < c.max_seqs;
       if (ok) {
-        const int len = c.len[s];
-        ok = len >= 0 && len <= c.max_pages * c.page_len;
+        const int empty = c.len[cs], len = c.len[ps];
+        ok = !mark(sh, cs) && empty == 0 && len >= 0 && len <= holds;
         need = ok && len % c.page_len;
       }
       if (!ok) sh.bad = 1;
@@ -314,18 +321,19 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(fv_pages c, con
     if (i < n) B[i] = total + before;
     total += all;
   }
-  __syncthreads();
-  if (sh.bad) return verdict(FV_PAGES_BAD, status, work);
-  // every entry in use must be a page: one wave a parent
+  // every child is marked: no parent is one, and its entries in use are pages
   for (int i = threadIdx.x >> 6; i < n; i += kPlanWaves) {
-    const int s = parents[i], pages = pages_of(c.len[s], c.page_len);
+    const int s = parents[i];
+    if (s < 0 || s >= c.max_seqs) continue;
+    if (sh.seen[s >> 5] >> (s & 31) & 1) sh.bad = 1;
+    const int pages = pages_of(min(max(c.len[s], 0), holds), c.page_len);
     const int* row = c.table + (size_t)s * c.max_pages;
     for (int j = threadIdx.x & 63; j < pages; j += 64)
       if (!is_page(c, row[j])) sh.bad = 1;
   }
   __syncthreads();
   if (sh.bad) return verdict(FV_PAGES_BAD, status, work);
-  if (total > c.n_pages || take_free(c, total, A, sh) < total)
+  if (total > c.n_pages || take_free(c, h, total, A, sh) < total)
     return verdict(FV_PAGES_FULL, status, work);
   verdict(FV_PAGES_OK, status, work);
 }
@@ -410,9 +418,11 @@ __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(fv_pages c, 
   int* C = B + list;
   const int w = threadIdx.x >> 6;
   int mine = 0;
+  Holders h;
   for (int p0 = 0; p0 < c.n_pages; p0 += kScanPages) {
     uint64_t m[16];
-    mine += pick_pages(c, p0 + w * 1024, m, [](int, int refs) { return refs > 0; });
+    h.load(c, p0 + w * 1024);
+    mine += pick_pages(c, h, p0 + w * 1024, m, [](int, int refs) { return refs > 0; });
   }
   if ((threadIdx.x & 63) == 0) sh.wave[0][w] = mine;
   __syncthreads();
@@ -422,8 +432,9 @@ __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(fv_pages c, 
   for (int p0 = 0; p0 < c.n_pages; p0 += kScanPages) {
     const int first = p0 + w * 1024;
     uint64_t mh[16], mm[16];
-    const int nh = pick_pages(c, first, mh, [u](int p, int refs) { return p < u && refs <= 0; });
-    const int nm = pick_pages(c, first, mm, [u](int p, int refs) { return p >= u && refs > 0; });
+    if (c.n_pages > kScanPages) h.load(c, first);
+    const int nh = pick_pages(c, h, first, mh, [u](int p, int refs) { return p < u && refs <= 0; });
+    const int nm = pick_pages(c, h, first, mm, [u](int p, int refs) { return p >= u && refs > 0; });
     __syncthreads();
     if ((threadIdx.x & 63) == 0) {
       sh.wave[0][w] = nh;
