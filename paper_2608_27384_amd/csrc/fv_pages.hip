@@ -119,7 +119,11 @@ __global__ __launch_bounds__(kRopeThreads) void rope_append_kernel(RopeCall r) {
 
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanWaves = kPlanThreads / 64;
-constexpr int kScanPages = kPlanThreads * 16;  // pages looked at between two barriers
+// Pages looked at between two barriers: 64 J of each wave, J at most 16 and no more
+// than needed (a wave takes about a hundred cycles for each 64).
+__device__ __forceinline__ int scan_groups(const fv_pages& c) {
+  return min(16, (c.n_pages + kPlanThreads - 1) / kPlanThreads);
+}
 
 struct PlanShared {
   int wave[2][kPlanWaves];
@@ -164,51 +168,53 @@ __device__ bool mark(PlanShared& sh, int s) {
   return atomicOr(&sh.seen[s >> 5], bit) & bit;
 }
 
-// Pages p0 + 1024 w + 64 j + lane, j = 0..15, of the wave w: which of them `pick` takes.
+// A wave's pages first + 64 j + lane, j < J: their holders, which of them `pick` takes.
 struct Holders {
   int refs[16];
-  __device__ __forceinline__ void load(const fv_pages& c, int first) {
+  __device__ __forceinline__ void load(const fv_pages& c, int first, int J) {
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
       const int p = first + 64 * j + (int)(threadIdx.x & 63);
-      refs[j] = p < c.n_pages ? c.refs[p] : 0;
+      refs[j] = j < J && p < c.n_pages ? c.refs[p] : 0;
     }
   }
 };
 template <typename Pick>
-__device__ __forceinline__ int pick_pages(const fv_pages& c, const Holders& h, int first,
+__device__ __forceinline__ int pick_pages(const fv_pages& c, const Holders& h, int first, int J,
                                           uint64_t (&m)[16], Pick pick) {
   const int lane = threadIdx.x & 63;
   int n = 0;
 #pragma unroll
   for (int j = 0; j < 16; ++j) {
     const int p = first + 64 * j + lane;
-    m[j] = __ballot(p < c.n_pages && pick(p, h.refs[j]));
+    m[j] = j < J ? __ballot(p < c.n_pages && pick(p, h.refs[j])) : 0;
     n += __popcll(m[j]);
   }
   return n;
 }
-__device__ __forceinline__ void list_pages(const uint64_t (&m)[16], int first, int at, int limit,
+__device__ __forceinline__ void list_pages(const uint64_t (&m)[16], int first, int J, int at, int limit,
                                            int* list) {
   const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int j = 0; j < 16; ++j) {
-    const int rank = at + __popcll(m[j] & ((1ull << lane) - 1));
-    if ((m[j] >> lane & 1) && rank < limit) list[rank] = first + 64 * j + lane;
-    at += __popcll(m[j]);
+    if (j < J) {
+      const int rank = at + __popcll(m[j] & ((1ull << lane) - 1));
+      if ((m[j] >> lane & 1) && rank < limit) list[rank] = first + 64 * j + lane;
+      at += __popcll(m[j]);
+    }
   }
 }
 
 // The lowest `want` free pages into list; how many there are, at most want.  h: the
-// wave's holders of the first kScanPages, loaded while the call was being checked.
+// wave's holders of the first pages, loaded while the call was being checked.
 __device__ int take_free(const fv_pages& c, Holders& h, int want, int* list, PlanShared& sh) {
-  const int w = threadIdx.x >> 6;
+  const int w = threadIdx.x >> 6, J = scan_groups(c);
   int found = 0;
-  for (int p0 = 0; p0 < c.n_pages && found < want; p0 += kScanPages) {
-    const int first = p0 + w * 1024;
-    if (p0) h.load(c, first);
+  for (int p0 = 0; p0 < c.n_pages && found < want; p0 += kPlanThreads * J) {
+    const int first = p0 + w * 64 * J;
+    if (p0) h.load(c, first, J);
     uint64_t m[16];
-    const int n = pick_pages(c, h, first, m, [](int, int refs) { return refs <= 0; });
+    const int n = pick_pages(c, h, first, J, m, [](int, int refs) { return refs <= 0; });
     __syncthreads();
     if ((threadIdx.x & 63) == 0) sh.wave[0][w] = n;
     __syncthreads();
@@ -217,7 +223,7 @@ __device__ int take_free(const fv_pages& c, Holders& h, int want, int* list, Pla
       before += i < w ? sh.wave[0][i] : 0;
       all += sh.wave[0][i];
     }
-    if (found + before < want) list_pages(m, first, found + before, want, list);
+    if (found + before < want) list_pages(m, first, J, found + before, want, list);
     found += all;
   }
   __syncthreads();
@@ -242,7 +248,7 @@ __global__ __launch_bounds__(kPlanThreads) void grow_plan_kernel(fv_pages c, con
   int* A = work + kPagesHeader;
   int* B = A + list;
   Holders h;
-  h.load(c, (threadIdx.x >> 6) * 1024);
+  h.load(c, (threadIdx.x >> 6) * 64 * scan_groups(c), scan_groups(c));
   clear_seen(sh, c.max_seqs);
   long long total = 0;
   for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
@@ -299,7 +305,7 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(fv_pages c, con
   int* A = work + kPagesHeader;
   int* B = A + list;
   Holders h;
-  h.load(c, (threadIdx.x >> 6) * 1024);
+  h.load(c, (threadIdx.x >> 6) * 64 * scan_groups(c), scan_groups(c));
   clear_seen(sh, c.max_seqs);
   const int holds = c.max_pages * c.page_len;
   int total = 0;
@@ -416,25 +422,26 @@ __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(fv_pages c, 
   int* A = work + kPagesHeader;
   int* B = A + list;
   int* C = B + list;
-  const int w = threadIdx.x >> 6;
+  const int w = threadIdx.x >> 6, J = scan_groups(c);
   int mine = 0;
   Holders h;
-  for (int p0 = 0; p0 < c.n_pages; p0 += kScanPages) {
+  for (int p0 = 0; p0 < c.n_pages; p0 += kPlanThreads * J) {
+    const int first = p0 + w * 64 * J;
     uint64_t m[16];
-    h.load(c, p0 + w * 1024);
-    mine += pick_pages(c, h, p0 + w * 1024, m, [](int, int refs) { return refs > 0; });
+    h.load(c, first, J);
+    mine += pick_pages(c, h, first, J, m, [](int, int refs) { return refs > 0; });
   }
   if ((threadIdx.x & 63) == 0) sh.wave[0][w] = mine;
   __syncthreads();
   int u = 0;
   for (int i = 0; i < kPlanWaves; ++i) u += sh.wave[0][i];
   int holes = 0, movers = 0;
-  for (int p0 = 0; p0 < c.n_pages; p0 += kScanPages) {
-    const int first = p0 + w * 1024;
+  for (int p0 = 0; p0 < c.n_pages; p0 += kPlanThreads * J) {
+    const int first = p0 + w * 64 * J;
     uint64_t mh[16], mm[16];
-    if (c.n_pages > kScanPages) h.load(c, first);
-    const int nh = pick_pages(c, h, first, mh, [u](int p, int refs) { return p < u && refs <= 0; });
-    const int nm = pick_pages(c, h, first, mm, [u](int p, int refs) { return p >= u && refs > 0; });
+    if (c.n_pages > kPlanThreads * J) h.load(c, first, J);
+    const int nh = pick_pages(c, h, first, J, mh, [u](int p, int refs) { return p < u && refs <= 0; });
+    const int nm = pick_pages(c, h, first, J, mm, [u](int p, int refs) { return p >= u && refs > 0; });
     __syncthreads();
     if ((threadIdx.x & 63) == 0) {
       sh.wave[0][w] = nh;
@@ -448,8 +455,8 @@ __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(fv_pages c, 
       ah += sh.wave[0][i];
       am += sh.wave[1][i];
     }
-    list_pages(mh, first, holes + bh, list, A);
-    list_pages(mm, first, movers + bm, list, B);
+    list_pages(mh, first, J, holes + bh, list, A);
+    list_pages(mm, first, J, movers + bm, list, B);
     holes += ah;
     movers += am;
   }
