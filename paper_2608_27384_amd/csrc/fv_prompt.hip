@@ -414,6 +414,7 @@ struct Walk : Rows<T, DH, 128> {
       u32x4 kf[AHEAD];
 #pragma unroll
       for (int p = 0; p < AHEAD; ++p) kf[p] = kread(kb, p);
+      __builtin_amdgcn_s_setprio(1);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int p = 0; p < NK; ++p) {
@@ -421,6 +422,7 @@ struct Walk : Rows<T, DH, 128> {
         if (p + AHEAD < NK) kf[p % AHEAD] = kread(kb, p + AHEAD);
         __builtin_amdgcn_sched_barrier(0);
       }
+      __builtin_amdgcn_s_setprio(0);
       vop vf[AHEAD];
 #pragma unroll
       for (int n = 0; n < AHEAD; ++n) vf[n] = vread(vb, n / PV, n % PV);
@@ -431,6 +433,7 @@ struct Walk : Rows<T, DH, 128> {
 #pragma unroll
         for (int d = 0; d < ND; ++d) o[d] *= f;
       }, [](int) {});
+      __builtin_amdgcn_s_setprio(1);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int n = 0; n < ND * PV; ++n) {
@@ -443,6 +446,7 @@ struct Walk : Rows<T, DH, 128> {
         if (n + AHEAD < ND * PV) vf[n % AHEAD] = vread(vb, (n + AHEAD) / PV, (n + AHEAD) % PV);
         __builtin_amdgcn_sched_barrier(0);
       }
+      __builtin_amdgcn_s_setprio(0);
     };
     const int whole = limit(row0) / KT;  // tiles that every row of the workgroup sees
     if (tiles > 0) issue(0, 0);
