@@ -173,23 +173,39 @@ __device__ __forceinline__ f32x16 product(u32x4 v, const f32x16&, const u32x4 (&
 __device__ __forceinline__ f32x16 product(float v, const f32x16& p, const u32x4 (&)[2], int c, f32x16 o) {
   return __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[c], o, 0, 0, 0);
 }
+// bf16 operands of 32 probabilities.
+__device__ __forceinline__ void as_operands(const f32x16& p, u32x4 (&pf)[2]) {
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    u16x8 w;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = f32_to_bf16(p[8 * c + e]);
+    pf[c] = __builtin_bit_cast(u32x4, w);
+  }
+}
+// Scores past what the lane's row sees (keys from lim on) to -inf.
+__device__ __forceinline__ void hide(f32x16& sc, int key0, int lh, int lim) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+    if (key0 + 8 * (r >> 2) + 4 * lh + (r & 3) >= lim) sc[r] = -INFINITY;
+}
+__device__ __forceinline__ float highest(const f32x16& sc) {
+  float top = sc[0];
+#pragma unroll
+  for (int r = 1; r < 16; ++r) top = fmaxf(top, sc[r]);
+  return other_half_max(top);
+}
 // Scores of 32 keys to probabilities (pf: as bf16 operands), with the row's
 // reference m and sum l; calls rescale(f) where the reference moves, and tick(r)
 // after the r-th of 16 probabilities.
 template <typename T, typename Rescale, typename Tick>
-__device__ __forceinline__ void softmax(f32x16& sc, bool edge, int key0, int lh, int lim, float scale, float& m,
-                                        float& l, u32x4 (&pf)[2], Rescale rescale, Tick tick) {
-  if (edge) {
-#pragma unroll
-    for (int r = 0; r < 16; ++r)
-      if (key0 + 8 * (r >> 2) + 4 * lh + (r & 3) >= lim) sc[r] = -INFINITY;
-  }
-  float top = sc[0];
-#pragma unroll
-  for (int r = 1; r < 16; ++r) top = fmaxf(top, sc[r]);
-  top = other_half_max(top) * scale;
-  if (__any(top > m + kSlack)) {
-    const float now = fmaxf(m, top);
+__device__ __forceinline__ void softmax(f32x16& sc, bool edge, int key0, int lh, int lim, float scale,
+                                        float& m, float& l, u32x4 (&pf)[2], Rescale rescale, Tick tick) {
+  if (edge) hide(sc, key0, lh, lim);
+  const float top = highest(sc) * scale;
+  const bool raise = top > m + kSlack;
+  if (__any(raise)) {
+    const float now = raise ? top : m;  // its own scores alone move a row's reference
     const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - now);
     m = now;
     l *= f;
@@ -202,15 +218,48 @@ __device__ __forceinline__ void softmax(f32x16& sc, bool edge, int key0, int lh,
     l += sc[r];
     tick(r);
   }
-  if constexpr (sizeof(T) == 2) {
+  if constexpr (sizeof(T) == 2) as_operands(sc, pf);
+}
+// The same without a maximum on the usual path: probabilities against the row's
+// reference as it is, whose sum says whether it will do.  A row whose sum (of
+// either half's keys) is past kLimit, or none, takes its maximum as the reference and
+// everything again.  `minus`: minus the reference, kNoRef for a row without one,
+// against which any visible score is infinite and a hidden one still nothing.
+// Leaves the scores as they are, which takes 16 more registers: for head dims up to
+// 192.  The vector unit bounds the loop at 128 (740 of 850 cycles a step, the
+// products 512): 16 maxima less, and the kept load offsets, brought eight prompts of
+// 2000 tokens, heads 32/8 of 128, from 519 to 485 us (1.08 PFLOP/s).
+constexpr float kLimit = 1024.0f;  // sums stay within 2^10 of the largest value's size
+constexpr float kNoRef = 3.402823466e38f;
+template <typename Rescale>
+__device__ __forceinline__ void softmax_by_sum(f32x16& sc, bool edge, int key0, int lh, int lim,
+                                               float scale, float& minus, float& l, u32x4 (&pf)[2],
+                                               Rescale rescale) {
+  if (edge) hide(sc, key0, lh, lim);
+  f32x16 p;
+  auto weigh = [&] {
+    float sum = 0.f;
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      u16x8 w;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) w[e] = f32_to_bf16(sc[8 * c + e]);
-      pf[c] = __builtin_bit_cast(u32x4, w);
+    for (int r = 0; r < 16; ++r) {
+      p[r] = __builtin_amdgcn_exp2f(fmaf(sc[r], scale, minus));
+      sum += p[r];
     }
+    return sum;
+  };
+  float sum = weigh();
+  if (__builtin_expect(__any(!(sum <= kLimit)), 0)) {
+    const bool raise = !(other_half_max(sum <= kLimit ? 0.f : 1.f) == 0.f);
+    const float top = highest(sc) * scale;
+    // NaN scores have no maximum: the reference stays, and the sum is NaN
+    const float now = raise && top > -INFINITY ? -top : minus;
+    const float f = minus == kNoRef ? (now == kNoRef ? 1.f : 0.f) : __builtin_amdgcn_exp2f(now - minus);
+    minus = now;
+    l *= f;
+    rescale(f);
+    sum = weigh();
   }
+  l += sum;
+  as_operands(p, pf);
 }
 // No key seen: zeros; keys that all score -inf: 0/0, as the formula has it.
 __device__ __forceinline__ float inverse(float l, int lim) {
@@ -347,11 +396,39 @@ struct Walk : Rows<T, DH, 128> {
                    : BYTES + 4 * lh * ROW + (((l32 >> 2) ^ (lh << 3)) << 4) + (l32 & 3) * 4;
   }
   // Direct loads of key tile kt: slot u, 16 bytes, is piece u % PIECES of row u / PIECES.
-  __device__ __forceinline__ void issue(int kt, int stage) const {
+  // offs: the offsets of a whole tile (Offsets), which the narrower heads have the
+  // registers to keep; the vector unit is what their loop is bound by.
+  static constexpr bool KEEP = E == 2 && DH <= 128;
+  struct Offsets {
+    int k[KEEP ? NI : 1], v[KEEP ? NI : 1];
+  };
+  __device__ __forceinline__ void find(Offsets& offs) const {
+    if constexpr (KEEP) {
+      const Slots<T, DH> at(lane);
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        int row, byte;
+        at.find(NI * wave + i, row, byte);
+        offs.k[i] = __umul24(row, a.ldk * E) + byte;
+        offs.v[i] = __umul24(row, a.ldv * E) + byte;
+      }
+    }
+  }
+  __device__ __forceinline__ void issue(int kt, int stage, const Offsets& offs) const {
     unsigned char* to = ring + stage * 2 * BYTES + wave * NI * 1024;
     const u32x4 ks = dma_source(static_cast<const T*>(a.k) + (size_t)(k0 + kt * KT) * a.ldk + kh * DH);
     const u32x4 vs = dma_source(static_cast<const T*>(a.v) + (size_t)(k0 + kt * KT) * a.ldv + kh * DH);
     const int most = nk - 1 - kt * KT;  // rows past the prompt's last repeat it
+    if constexpr (KEEP) {
+      if (most >= KT - 1) {
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          dma16(ks, to + 1024 * i, offs.k[i]);
+          dma16(vs, to + BYTES + 1024 * i, offs.v[i]);
+        }
+        return;
+      }
+    }
     int mine = lane;
     asm volatile("" : "+v"(mine));  // not 2 NI offsets kept over the loop
     const Slots<T, DH> at(mine);
@@ -396,8 +473,9 @@ struct Walk : Rows<T, DH, 128> {
     const int lim = limit(wrow + l32);
     meet();  // the ring is the tiles' from here on
     const int end = wrow < rows ? limit(wrow + 31) : 0;
+    constexpr bool BY_SUM = E == 2 && DH <= 192;
     f32x16 o[ND];
-    float m = -INFINITY, l = 0.f;  // l over the lane half's keys only
+    float m = BY_SUM ? kNoRef : -INFINITY, l = 0.f;  // l over the lane half's keys only
     uint32_t odds = 0;
 #pragma unroll
     for (int d = 0; d < ND; ++d) o[d] = zeros16();
@@ -429,10 +507,14 @@ struct Walk : Rows<T, DH, 128> {
       __builtin_amdgcn_sched_barrier(0);
 
       u32x4 pf[2];
-      softmax<T>(sc, EDGE, key0, lh, lim, a.scale, m, l, pf, [&](float f) {
+      auto rescale = [&](float f) __attribute__((always_inline)) {
 #pragma unroll
         for (int d = 0; d < ND; ++d) o[d] *= f;
-      }, [](int) {});
+      };
+      if constexpr (BY_SUM)
+        softmax_by_sum(sc, EDGE, key0, lh, lim, a.scale, m, l, pf, rescale);
+      else
+        softmax<T>(sc, EDGE, key0, lh, lim, a.scale, m, l, pf, rescale, [](int) {});
       __builtin_amdgcn_s_setprio(1);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -449,18 +531,21 @@ struct Walk : Rows<T, DH, 128> {
       __builtin_amdgcn_s_setprio(0);
     };
     const int whole = limit(row0) / KT;  // tiles that every row of the workgroup sees
-    if (tiles > 0) issue(0, 0);
+    Offsets offs;
+    find(offs);
+    if (tiles > 0) issue(0, 0, offs);
     for (int kt = 0; kt < whole; ++kt) {
       meet();  // tile kt is there and tile kt - 1 is done with
-      if (kt + 1 < tiles) issue(kt + 1, (kt + 1) & 1);
+      if (kt + 1 < tiles) issue(kt + 1, (kt + 1) & 1, offs);
       step(std::false_type{}, kt);
     }
     for (int kt = whole; kt < tiles; ++kt) {
       meet();
-      if (kt + 1 < tiles) issue(kt + 1, (kt + 1) & 1);
+      if (kt + 1 < tiles) issue(kt + 1, (kt + 1) & 1, offs);
       if (kt * KT + 32 * half < end) step(std::true_type{}, kt);
     }
     bool unruly = any_odd(odds, T{});
+    if (BY_SUM) m = m == kNoRef ? -INFINITY : -m;
     meet();
     if constexpr (KG == 2) {
       f32x4* so = reinterpret_cast<f32x4*>(ring) + (wave % 4) * (4 * ND * 64) + lane;

@@ -147,6 +147,31 @@ def test_scores_without_a_softmax_and_rising_ones(shape):
     assert float((got.double() - ref).abs().max()) <= tol * float(v.double().abs().max())
 
 
+@pytest.mark.parametrize("shape", [SHAPES[0], FULL[0], FULL[1], FULL[2], FULL[3], FULL[5], FULL[10]], ids=str)
+def test_jumping_scores_and_large_values(shape):
+    """Scores that jump far above what a row has seen, some rows only, now and then; values
+    whose sums must not leave the range of fp32 on the way."""
+    torch = cu.torch_mod()
+    dtype, H, G, D = shape
+    n = 330
+    q, k, v, cq, ck = make(shape, [(n, n)])
+    q[:, :, 0] = 0
+    q[::3, :, 0] = 1.0       # these rows feel the jumps
+    k[:, :, 0] = 0
+    for i, x in ((40, 12), (41, 300), (100, 305), (170, 900), (260, 890), (300, 5000)):
+        k[i, :, 0] = x * D ** 0.5
+    v *= 2.0 ** 100
+    out = run(q, k, v, cq, ck, True)
+    assert out.isfinite().all()
+    # products up to 5000 sqrt(D): the scores' own rounding, by the definition's bound
+    ref = cu.attention(q, k, v, limits(n, n, True))
+    cu.check_attention(out, ref, dtype)
+    calm = torch.ones(n, dtype=torch.bool, device="cuda")
+    calm[::3] = False
+    k[:, :, 0] = 0
+    assert torch.equal(run(q, k, v, cq, ck, True)[calm], out[calm])
+
+
 def test_many_short_prompts():
     """More prompts than one step of the search looks at, some empty."""
     shape = ("bf16", 4, 2, 64)
