@@ -617,14 +617,16 @@ __global__ __launch_bounds__(256 * KG, DH * sizeof(T) > 512 ? 1 : 2) void prompt
   if (w.row0 < w.rows) w.run(stats);
 }
 
-// 32 keys of V from memory into registers.  A lane takes W = DH/32 consecutive
+// Keys of V from memory into registers.  A lane takes W = DH/32 consecutive
 // elements of each of its 16 keys (those of its score registers), a whole row by
-// 32 lanes; row i of O^T's tile j is then the head's element W i + j.
+// 32 lanes; row i of O^T's tile j is then the head's element W i + j.  bf16 wants
+// all 16 at once (ROWS), fp32 one after another.
 template <typename T, int DH> struct FewV {
-  static constexpr int W = DH / 32, DW = W * (int)sizeof(T) / 4;
-  uint32_t w[16][DW];
-  // x-th row: `off` bytes past the source.
-  __device__ __forceinline__ void load(int x, lds_src src, int off) {
+  static constexpr int W = DH / 32, DW = W * (int)sizeof(T) / 4, ROWS = sizeof(T) == 2 ? 16 : 4;
+  uint32_t w[ROWS][DW];
+  // Row x: `off` bytes past the source.
+  __device__ __forceinline__ void load(int row, lds_src src, int off) {
+    const int x = row % ROWS;
     constexpr int B = DW / 4 * 4;
 #pragma unroll
     for (int i = 0; i < B; i += 4) {
@@ -644,18 +646,18 @@ template <typename T, int DH> struct FewV {
       w[x][B] = __builtin_amdgcn_raw_buffer_load_b32(src, off + 4 * B, 0, 0);
     }
   }
-  // Takes out what is not finite; whether there was any.
-  __device__ __forceinline__ bool sift() {
+  // Takes what is not finite out of the rows [first, last); whether there was any.
+  __device__ __forceinline__ bool sift(int first, int last) {
     uint32_t odds = 0;
 #pragma unroll
-    for (int x = 0; x < 16; ++x)
+    for (int x = first; x < last; ++x)
 #pragma unroll
-      for (int i = 0; i < DW; ++i) odds |= odd(w[x][i], T{});
+      for (int i = 0; i < DW; ++i) odds |= odd(w[x % ROWS][i], T{});
     if (__builtin_expect(!any_odd(odds, T{}), 1)) return false;
 #pragma unroll
-    for (int x = 0; x < 16; ++x)
+    for (int x = first; x < last; ++x)
 #pragma unroll
-      for (int i = 0; i < DW; ++i) w[x][i] = even(w[x][i], T{});
+      for (int i = 0; i < DW; ++i) w[x % ROWS][i] = even(w[x % ROWS][i], T{});
     return true;
   }
   // Operand c of tile j: 16 keys from 16 c on (bf16, a turned 8 x 2 block), the
@@ -669,7 +671,7 @@ template <typename T, int DH> struct FewV {
                                      j & 1 ? 0x07060302u : 0x05040100u);
       return r;
     } else {
-      return __uint_as_float(w[c][j]);
+      return __uint_as_float(w[c % ROWS][j]);
     }
   }
 };
@@ -678,7 +680,8 @@ template <typename T, int DH> struct FewV {
 // LDS.  Waves do not wait for each other before that.  Values come from the caches
 // straight into registers, whole rows by 32 lanes; keys, of which a lane wants a
 // row of its own (32 bytes of each of 32 rows a load), through a wave's own LDS in
-// bf16, one step ahead, and into registers in fp32, whose products take the longer.
+// bf16, one step ahead, and into registers in fp32, whose products take 16 times as
+// long and need no more than a few operands at a time.
 constexpr int kFewWaves = 4;
 template <typename T, int DH>
 __global__ __launch_bounds__(64 * kFewWaves, 1) void prompt_few_kernel(PromptCall a) {
@@ -698,7 +701,6 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void prompt_few_kernel(PromptCal
   const int whole = b.limit(b.row0) / 32, steps = (b.limit(b.row0 + 31) + 31) / 32;
   const T* kbase = static_cast<const T*>(a.k) + (size_t)b.k0 * a.ldk + b.kh * DH;
   const T* vbase = static_cast<const T*>(a.v) + (size_t)b.k0 * a.ldv + b.kh * DH;
-  u32x4 kf[E == 4 ? NK : 1];
   unsigned char* ring = lds + wave * KEYS;
   const int kaddr = l32 * ROW + ((lh ^ swizzle<T, DH>(l32)) << 4);
   // Part n of NI of the keys of step i (bf16); of no step, past the last.
@@ -710,19 +712,9 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void prompt_few_kernel(PromptCal
     at.find(n, row, byte);
     lds_dma16(src, ring + stage * 32 * ROW + 1024 * n, __umul24(min(row, b.nk - 1 - 32 * i), a.ldk * E) + byte, 0);
   };
-  auto load_keys_fp32 = [&](int i) __attribute__((always_inline)) {
-    const T* row = kbase + (size_t)min(32 * i + l32, b.nk - 1) * a.ldk;
+  if (E == 2 && wave < steps) {
 #pragma unroll
-    for (int p = 0; p < NK; ++p)
-      if constexpr (E == 4) kf[p] = *reinterpret_cast<const u32x4*>(row + (2 * p + lh) * (16 / E));
-  };
-  if (wave < steps) {
-    if constexpr (E == 2) {
-#pragma unroll
-      for (int n = 0; n < NI; ++n) load_keys(wave, 0, n);
-    } else {
-      load_keys_fp32(wave);
-    }
+    for (int n = 0; n < NI; ++n) load_keys(wave, 0, n);
   }
   u32x4 qf[NK];
   const long long mine = b.template query<true>(b.row0, qf, queries, kFewWaves);
@@ -777,19 +769,38 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void prompt_few_kernel(PromptCal
       softmax<T>(sc, edge, 32 * i, lh, lim, a.scale, m, l, pf, rescale, [&](int r) __attribute__((always_inline)) {
         if (r < NI) load_keys(i + kFewWaves, stage ^ 1, r);
       });
+      if (edge && v.sift(0, 16)) unruly = true;
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int c = 0; c < PV; ++c) o[d] = product(v.operand(d, c), sc, pf, c, o[d]);
     } else {
+      constexpr int AHEAD = 6;
+      const T* row = kbase + (size_t)min(32 * i + l32, b.nk - 1) * a.ldk;
+      auto key = [&](int p) __attribute__((always_inline)) {
+        return *reinterpret_cast<const u32x4*>(row + (2 * p + lh) * (16 / E));
+      };
+      u32x4 kr[AHEAD];
 #pragma unroll
-      for (int x = 0; x < 16; ++x) load_value(x);
+      for (int p = 0; p < AHEAD; ++p) kr[p] = key(p);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int p = 0; p < NK; ++p) sc = mma32(kf[p], qf[p], sc, T{});
-      if (i + kFewWaves < steps) load_keys_fp32(i + kFewWaves);
+      for (int p = 0; p < NK; ++p) {
+        sc = mma32(kr[p % AHEAD], qf[p], sc, T{});
+        if (p + AHEAD < NK) kr[p % AHEAD] = key(p + AHEAD);
+        if (p >= NK - FewV<T, DH>::ROWS) load_value(p - NK + FewV<T, DH>::ROWS);
+        __builtin_amdgcn_sched_barrier(0);
+      }
       softmax<T>(sc, edge, 32 * i, lh, lim, a.scale, m, l, pf, rescale, [](int) {});
+#pragma unroll
+      for (int c = 0; c < PV; ++c) {
+        if (edge && v.sift(c, c + 1)) unruly = true;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) o[d] = product(v.operand(d, c), sc, pf, c, o[d]);
+        if (c + FewV<T, DH>::ROWS < PV) load_value(c + FewV<T, DH>::ROWS);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
-    if (edge && v.sift()) unruly = true;
-#pragma unroll
-    for (int d = 0; d < ND; ++d)
-#pragma unroll
-      for (int c = 0; c < PV; ++c) o[d] = product(v.operand(d, c), sc, pf, c, o[d]);
   }
 
   // The waves' sums, brought to the rows' common reference, join in LDS.
@@ -850,21 +861,22 @@ void prompt_at(PromptCall& a, int form, hipStream_t s) {
 }
 
 // Which kernel, by the 32-row tiles of the call (256 CUs; a CU holds one or two
-// workgroups).  us, heads 8/1 of 256, prompts of 560 tokens (one prompt): kFew 17
-// (23), kHalves 22 (33), kTiles 24 (40) at 280 tiles; 41 (97), 26 (83), 26 (105) at
-// 840; 77 (320), 43 (188), 35 (231) at 1680; 193 (1996), 89 (1179), 68 (1162) at
-// 4480.  Heads 32/8 of 128: 20, 15, 17 at 560; 50 (74), 23 (34), 22 (40) at 1680; 125
-// (364), 48 (186), 39 (172) at 4480.  A long causal prompt's last tiles outlast the
-// others, which halving the walk of each makes up for until the chip is full.
-// In fp32 products are 16 times as long, and 128 rows leave CUs idle for longer:
-// heads of 64 and 560 tokens, kFew 28, kTiles 47 at 560 tiles, 97 and 110 at 2240, 186
-// and 141 at 4480; of 256, where kFew spills, 145 and 160 at 420, 244 and 163 at 840.
+// workgroups).  us at prompts of 560 tokens (one prompt), heads 8/1 of 256: kFew 17
+// (22), kHalves 22 (33), kTiles 24 (39) at 280 tiles; 41 (95), 25 (81), 26 (104) at
+// 840; 75 (314), 42 (184), 33 (231) at 1680; 191 (1971), 87 (1164), 67 (1105) at
+// 4480.  Heads 32/8 of 128: 20 (20), 14 (15), 15 (15) at 560; 49 (73), 23 (32), 20 (38)
+// at 1680; 125 (363), 47 (173), 37 (161) at 4480.  A long causal prompt's last tiles
+// outlast the others, which halving the walk of each makes up for until the chip is
+// full.  In fp32, where products are 16 times as long and the loads of few rows no
+// matter, kFew and kTiles take: heads of 256, 81 (207) and 161 (583) at 560, 279 (2592)
+// and 309 (2862) at 2240, 541 (10082) and 527 (10700) at 4480; of 128, 44 (44) and 81
+// (80), 154 (390) and 133 (432), 298 (1425) and 240 (1260).
 int prompt_form(const fv_prompt_args& x) {
   const int64_t tiles = (int64_t)x.n_q * x.n_q_heads / 32;
-  if (x.dtype == FV_FP32) return tiles <= (x.head_dim == 256 ? 480 : 2048) ? kFew : kTiles;
+  if (x.dtype == FV_FP32) return tiles <= (x.head_dim == 128 ? 2048 : 4096) ? kFew : kTiles;
   if (tiles < 384) return kFew;
   const bool few_long = x.causal && x.n_k / x.n_seqs >= 2048;
-  return tiles <= (few_long ? 2048 : 1024) ? kHalves : kTiles;
+  return tiles <= (few_long ? 2560 : 1024) ? kHalves : kTiles;
 }
 
 }  // namespace

@@ -16,7 +16,7 @@ SHAPES = [("bf16", 8, 1, 256), ("bf16", 8, 2, 128), ("bf16", 4, 4, 64), ("bf16",
 # eight waves halving the keys, four waves, fp32
 FULL = [("bf16", 64, 4, D) for D in (64, 128, 192, 256)] + [
     ("bf16", 128, 16, D) for D in (64, 128, 192, 256)] + [("bf16", 126, 18, 128)] + [
-    ("fp32", 256, 32, D) for D in (64, 128, 192, 256)]
+    ("fp32", 512, 32, D) for D in (64, 128, 192, 256)]
 # (queries, keys) of each prompt
 LENS = {"ragged": [(0, 0), (1, 1), (33, 33), (64, 64), (65, 65), (0, 5), (130, 130), (7, 7)],
         "tails": [(1, 300), (5, 64), (32, 97), (3, 3), (100, 517)],
