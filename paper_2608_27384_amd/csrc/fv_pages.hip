@@ -237,6 +237,11 @@ __device__ __forceinline__ void verdict(int st, int* status, int* work) {
   }
 }
 
+// Entries that a plan kernel can carry out by itself: a launch of its own costs 3.4
+// us of the host and 3 to 4 us of the GPU.
+constexpr int kInline = kPlanThreads;      // requests of a grow
+constexpr int kInlineRows = 8192;          // table entries of a free
+
 // Workspace: [0] the call's status; lists A, B, C of `list` ints each.
 // A: pages taken.  B[i]: how many were taken for the entries before i.
 
@@ -245,15 +250,17 @@ __global__ __launch_bounds__(kPlanThreads) void grow_plan_kernel(fv_pages c, con
                                                                  int* status, int* work,
                                                                  int list) {
   __shared__ PlanShared sh;
+  __shared__ int first[kInline], place[kInline];  // of a request's pages: in A, in the table
   int* A = work + kPagesHeader;
   int* B = A + list;
   Holders h;
   h.load(c, (threadIdx.x >> 6) * 64 * scan_groups(c), scan_groups(c));
   clear_seen(sh, c.max_seqs);
   long long total = 0;
+  int mine = -1, now = 0;  // the thread's sequence, if the lists are short, and its length to be
   for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
     const int i = i0 + threadIdx.x;
-    int need = 0;
+    int need = 0, have = 0;
     if (i < n) {
       const int s = seqs[i];
       bool ok = s >= 0 && s < c.max_seqs && !mark(sh, s);
@@ -264,13 +271,24 @@ __global__ __launch_bounds__(kPlanThreads) void grow_plan_kernel(fv_pages c, con
           const int last = c.table[(size_t)s * c.max_pages + len / c.page_len];
           ok = is_page(c, last) && c.refs[last] <= 1;
         }
-        if (ok) need = pages_of(len + more, c.page_len) - pages_of(len, c.page_len);
+        if (ok) {
+          have = pages_of(len, c.page_len);
+          need = pages_of(len + more, c.page_len) - have;
+          mine = s;
+          now = len + more;
+        }
       }
       if (!ok) sh.bad = 1;
     }
     int all;
     const int before = block_scan(need, sh.wave[1], &all);
-    if (i < n) B[i] = (int)(total + before);
+    if (i < n) {
+      B[i] = (int)(total + before);
+      if (n <= kInline) {
+        first[i] = before;
+        place[i] = have;
+      }
+    }
     total += all;
   }
   __syncthreads();
@@ -278,6 +296,21 @@ __global__ __launch_bounds__(kPlanThreads) void grow_plan_kernel(fv_pages c, con
   if (total > c.n_pages || take_free(c, h, (int)total, A, sh) < total)
     return verdict(FV_PAGES_FULL, status, work);
   verdict(FV_PAGES_OK, status, work);
+  if (n > kInline) return;
+  for (int t = threadIdx.x; t < (int)total; t += kPlanThreads) {
+    int lo = 0, hi = n;  // the last request whose pages start at t or before
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (first[mid] <= t)
+        lo = mid;
+      else
+        hi = mid;
+    }
+    const int page = A[t];
+    c.table[(size_t)seqs[lo] * c.max_pages + place[lo] + t - first[lo]] = page;
+    c.refs[page] = 1;
+  }
+  if (mine >= 0) c.len[mine] = now;
 }
 
 __global__ __launch_bounds__(64) void grow_apply_kernel(fv_pages c, const int* seqs, const int* add,
@@ -397,6 +430,16 @@ __global__ __launch_bounds__(kPlanThreads) void free_plan_kernel(fv_pages c, con
   }
   __syncthreads();
   verdict(sh.bad ? FV_PAGES_BAD : FV_PAGES_OK, status, nullptr);
+  if (sh.bad || (long long)n * c.max_pages > kInlineRows) return;
+  for (int t = threadIdx.x; t < n * c.max_pages; t += kPlanThreads) {
+    const int i = t / c.max_pages, j = t - i * c.max_pages, s = seqs[i];
+    int* at = c.table + (size_t)s * c.max_pages + j;
+    const int p = *at;
+    if (j * c.page_len < c.len[s] && is_page(c, p)) atomicSub(&c.refs[p], 1);
+    *at = -1;
+  }
+  __syncthreads();  // the lengths have been read
+  for (int i = threadIdx.x; i < n; i += kPlanThreads) c.len[seqs[i]] = 0;
 }
 
 __global__ __launch_bounds__(256) void free_apply_kernel(fv_pages c, const int* seqs,
@@ -564,7 +607,8 @@ void launch_pages_grow(const fv_pages& c, const int* seqs, const int* add, int n
   const int list = (int)pages_list(c);
   hipLaunchKernelGGL(grow_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, c, seqs, add, n, status,
                      work, list);
-  if (n) hipLaunchKernelGGL(grow_apply_kernel, dim3(n), dim3(64), 0, s, c, seqs, add, work, list);
+  if (n > kInline)
+    hipLaunchKernelGGL(grow_apply_kernel, dim3(n), dim3(64), 0, s, c, seqs, add, work, list);
 }
 
 void launch_pages_fork(const fv_pages& c, const int* parents, const int* children, int n,
@@ -579,7 +623,8 @@ void launch_pages_fork(const fv_pages& c, const int* parents, const int* childre
 
 void launch_pages_free(const fv_pages& c, const int* seqs, int n, int* status, hipStream_t s) {
   hipLaunchKernelGGL(free_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, c, seqs, n, status);
-  if (n) hipLaunchKernelGGL(free_apply_kernel, dim3(n), dim3(256), 0, s, c, seqs, status);
+  if ((int64_t)n * c.max_pages > kInlineRows)
+    hipLaunchKernelGGL(free_apply_kernel, dim3(n), dim3(256), 0, s, c, seqs, status);
 }
 
 void launch_pages_compact(const fv_pages& c, int* used, int* work, hipStream_t s) {

@@ -114,6 +114,31 @@ def test_refused_lists_change_nothing():
     assert int(cache.free(t([1]))) == 0  # what is no page is skipped
 
 
+@pytest.mark.parametrize("n,width", [(1024, 5), (1025, 5), (2600, 4), (40, 300)])
+def test_long_lists(n, width):
+    """More entries than a plan carries out by itself, and just as many."""
+    cache, model = fresh(2 * n * min(width, 5) + 30000, 2 * n + 3, width, layers=1, heads=1)
+    rng = random.Random(n)
+    seqs = rng.sample(range(n), n)
+    for most in (40, 20):
+        add = [rng.choice([0, 1, 16, 17, rng.randint(0, most)]) for _ in seqs]
+        if width > 100 and most == 40:
+            add[3], add[30] = 4000, 2500
+        assert int(cache.grow(cu.ints(seqs), cu.ints(add))) == model.grow(seqs, add) == 0
+        same(cache, model)
+    par, kids = rng.choices(range(n), k=n), rng.sample(range(n, 2 * n + 3), n)
+    assert int(cache.fork(cu.ints(par), cu.ints(kids))) == 0
+    assert model.fork(par, kids)[0] == 0
+    same(cache, model)
+    assert int(cache.free(cu.ints(seqs + seqs[:1]))) == 1
+    same(cache, model)
+    assert int(cache.free(cu.ints(seqs[::-1]))) == model.free(seqs) == 0
+    same(cache, model)
+    assert (cache.table[:n] == -1).all()
+    assert int(cache.compact()) == model.compact()[0]
+    same(cache, model)
+
+
 def test_empty_lists():
     torch = cu.torch_mod()
     cache, model = fresh(10, 4, 4)
