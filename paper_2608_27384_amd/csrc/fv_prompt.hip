@@ -317,6 +317,8 @@ struct Rows {
     row0 = (slot - first) * R;
     diff = nk - nq + 1;
   }
+  // False: a spare slot, or one that no prompt has (offsets that do not ascend from 0).
+  __device__ __forceinline__ bool any() const { return row0 >= 0 && row0 < rows; }
   // A row sees the keys [0, limit), which do not fall from one row to the next.
   __device__ __forceinline__ int limit(int row) const {
     return a.causal ? min(max(diff + min(row, rows - 1) / a.group, 0), nk) : nk;
@@ -614,7 +616,7 @@ __global__ __launch_bounds__(256 * KG, DH * sizeof(T) > 512 ? 1 : 2) void prompt
   __shared__ __attribute__((aligned(1024))) unsigned char ring[4 * W::BYTES];
   __shared__ float stats[KG == 2 ? 516 : 1];
   const W w(a, ring);
-  if (w.row0 < w.rows) w.run(stats);
+  if (w.any()) w.run(stats);
 }
 
 // Keys of V from memory into registers.  A lane takes W = DH/32 consecutive
@@ -696,7 +698,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void prompt_few_kernel(PromptCal
   __shared__ __attribute__((aligned(1024))) unsigned char lds[WORK + (E == 2 ? 32 * ROW : 0)];
   unsigned char* queries = lds + (E == 2 ? WORK : 0);
   const Base b(a);
-  if (b.row0 >= b.rows) return;
+  if (!b.any()) return;
   const int l32 = b.l32, lh = b.lh, wave = b.wave;
   const int whole = b.limit(b.row0) / 32, steps = (b.limit(b.row0 + 31) + 31) / 32;
   const T* kbase = static_cast<const T*>(a.k) + (size_t)b.k0 * a.ldk + b.kh * DH;

@@ -265,6 +265,24 @@ def test_rotary_append(shape, n):
     assert cache.k[0, page, :, p % 16].equal(ko[keep])
 
 
+def test_rotary_rows_far_apart():
+    """Rows 2^20 elements apart: offsets past 2^32 bytes."""
+    torch = cu.torch_mod()
+    from paper_2608_27384_amd.flashvla import rope
+    n, D = 4300, 64
+    wide = torch.empty(n, 1 << 20, dtype=torch.bfloat16, device="cuda")
+    q, k = wide[:, :2 * D].unflatten(1, (2, D)), wide[:, 2 * D:3 * D].unflatten(1, (1, D))
+    q.copy_(cu.randn("bf16", 1, n, 2, D))
+    k.copy_(cu.randn("bf16", 2, n, 1, D))
+    pos = cu.ints([np.arange(n)])
+    qo, ko = torch.empty(n, 2, D, dtype=q.dtype, device="cuda"), torch.empty(n, 1, D, dtype=q.dtype, device="cuda")
+    rope(q, k, pos, (D // 2,), qo, ko)
+    ref = cu.rotate(q.contiguous(), [np.arange(n)], (D // 2,), 1e4)
+    cu.check_rotated(qo, ref, "bf16", n * 2.0 ** -50)
+    rope(q, k, pos, (D // 2,), q, k)
+    assert q.equal(qo) and k.equal(ko)
+
+
 def test_one_axis_is_the_action_tokens_rotation():
     """Equal positions on every axis turn as one axis does."""
     torch = cu.torch_mod()

@@ -186,6 +186,50 @@ def test_many_short_prompts():
     assert not (out == 7).all(-1).any()
 
 
+@pytest.mark.parametrize("shape", [SHAPES[1], FULL[1], FULL[5]], ids=str)
+def test_offsets_that_are_wrong_stay_inside(shape):
+    """Offsets that start late, fall or leave the tensors touch nothing but the rows of a
+    prompt that they do describe; guard rows around every operand keep their values."""
+    torch = cu.torch_mod()
+    dtype, H, G, D = shape
+    n, pad = 300, 64
+    big = [cu.randn(dtype, 5 + i, n + 2 * pad, h, D) for i, h in enumerate((H, G, G))]
+    q, k, v = (x[pad:pad + n] for x in big)
+    whole = torch.full_like(big[0], 7.0)
+    out = whole[pad:pad + n]
+    run(q, k, v, [20, 90, 90, 220], [3, 70, 80, 260], True, out)
+    assert (whole[:pad + 20] == 7).all() and (whole[pad + 220:] == 7).all()
+    for a, b, c, d in ((20, 90, 3, 70), (90, 220, 80, 260)):
+        ref = cu.attention(q[a:b], k[c:d], v[c:d], limits(b - a, d - c, True))
+        cu.check_attention(out[a:b], ref, dtype)
+    for bad in ([0, -5, 700, 20, 1 << 30], [1 << 30, 0, 0, 300, 10], [-9, -1 << 31, 5, 2, 299],
+                [300, 200, 100, 50, 0], [150, 10, 290, 10, 2000]):
+        run(q, k, v, bad, bad[::-1], True, out)
+        run(q, k, v, bad, [0, 100, 200, 250, 300], False, out)
+        assert (whole[:pad] == 7).all() and (whole[pad + n:] == 7).all()
+
+
+@pytest.mark.parametrize("heads,group", [(2, 2), (16, 4)])
+def test_rows_far_apart(heads, group):
+    """Rows 2^20 elements apart: offsets past 2^32 bytes in every operand."""
+    torch = cu.torch_mod()
+    D, n, kv = 64, 4400, heads // group
+    wide = torch.empty(n, 1 << 20, dtype=torch.bfloat16, device="cuda")
+    cols = [0]
+    for h in (heads, kv, kv, heads):
+        cols.append(cols[-1] + h * D)
+    q, k, v, out = (wide[:, a:b].unflatten(1, (-1, D)) for a, b in zip(cols, cols[1:]))
+    for i, x in enumerate((q, k, v)):
+        x.copy_(cu.randn("bf16", i, *x.shape))
+    far = torch.empty(n, 1 << 20, dtype=torch.bfloat16, device="cuda")[:, :heads * D].unflatten(1, (-1, D))
+    cq = [0, 100, 4300, n]
+    run(q, k, v, cq, cq, True, far)
+    dense = run(*(x.contiguous() for x in (q, k, v)), cq, cq, True)
+    assert torch.equal(far, dense)
+    tail = slice(4300, n)
+    cu.check_attention(far[tail], cu.attention(q[tail], k[tail], v[tail], limits(100, 100, True)), "bf16")
+
+
 def test_scale_and_no_rows():
     torch = cu.torch_mod()
     shape = SHAPES[1]
