@@ -476,11 +476,12 @@ typedef struct {
  *  seqs, at  int32 [n]: the token becomes position at of sequence seqs of the
  *            cache.  A token whose place does not exist (seqs or at out of range,
  *            a table entry that is no page) is rotated and not stored: a padded
- *            batch passes seqs = -1.  Two tokens of one place: either is stored.
+ *            batch passes seqs = -1.  Of two tokens with one place, parts of
+ *            both may be stored.
  *  cache     the pages, or NULL: rotate only (then seqs, at and v are not read)
  * len is neither read nor changed; fv_pages_grow makes room beforehand.
  * q_out may be q and k_out may be k (same leading dimension); otherwise outputs
- * and inputs must not overlap.  n = 0 does nothing.
+ * and inputs must not overlap.  n = 0 does nothing; n is at most 2^26.
  * Errors: FV_ERR_INVALID_ARG, FV_ERR_HIP.
  */
 typedef struct {
@@ -507,8 +508,8 @@ fv_status fv_rope_append(const fv_rope_args *args, const fv_pages *cache, void *
  * does not see has no influence on its result, also where it is infinite or NaN.
  * Scores, softmax and sums are fp32; in bf16 the probabilities are rounded to
  * bf16 before they meet the values.  out must not overlap q, k or v.
- * Errors: FV_ERR_INVALID_ARG (a size below 0, n_seqs > 65536, strides,
- * pointers), FV_ERR_HIP.
+ * Errors: FV_ERR_INVALID_ARG (a size below 0, n_seqs > 65536, n_q * n_q_heads >
+ * 2^30, n_seqs * n_kv_heads > 2^22, strides, pointers), FV_ERR_HIP.
  */
 typedef struct {
   const void *q, *k, *v;
@@ -534,7 +535,8 @@ fv_status fv_prompt_attention(const fv_prompt_args *args, void *stream);
  *  work     fv_paged_attention_workspace bytes, overwritten (calls that may run
  *           at the same time need one each); NULL where that is 0
  * Rounding as in fv_prompt_attention; the result does not depend on the other
- * rows' lengths.  out must not overlap q.
+ * rows' lengths.  out must not overlap q.  n is at most 65536, n * n_q_heads at
+ * most 2^22.
  * Errors: FV_ERR_INVALID_ARG, FV_ERR_HIP.
  */
 typedef struct {
@@ -562,7 +564,8 @@ fv_status fv_paged_attention(const fv_paged_args *args, const fv_pages *cache, v
  *  fv_pages_grow     sequence seqs[i] gets add[i] >= 0 more positions, with pages
  *                    for them.  FV_PAGES_BAD: a sequence out of range or listed
  *                    twice, add[i] < 0, more than max_pages pages, or a part-filled
- *                    last page that another sequence holds too.
+ *                    last page that is not the sequence's alone (refs other
+ *                    than 1) or no page.
  *  fv_pages_fork     children[i], an empty sequence, becomes a copy of parents[i]:
  *                    full pages are shared, the rows in use of a part-filled last
  *                    page are copied to a page of its own in every layer (its other

@@ -88,6 +88,9 @@ void apart(const Span& a, const Span& b, const char* what) {
   if (a.lo < b.hi && b.lo < a.hi) bad(std::string(what) + " must not overlap");
 }
 
+// A launch holds less than 2^32 threads: the bounds of n, n * heads and n_seqs * heads in the
+// calls below keep every grid under that (the largest, 512 threads for each of n * heads
+// joined rows, 2^31).
 void check_launch() {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) fail(FV_ERR_HIP, std::string("kernel launch: ") + hipGetErrorString(e));
@@ -113,6 +116,7 @@ void check_paged(const fv_paged_args* a, const fv_pages* c) {
   check_cache(c);
   check_heads(a->n_q_heads, c->n_kv_heads, c->head_dim);
   if (a->n < 0 || a->n > 65536) bad("n must be 0 to 65536");
+  if ((int64_t)a->n * a->n_q_heads > 1 << 22) bad("n * n_q_heads must be at most 2^22");
   if (a->max_len < 0) bad("max_len must not be negative");
   if (a->layer < 0 || a->layer >= c->n_layers) bad("layer out of range");
 }
@@ -143,7 +147,7 @@ fv_status fv_rope_append(const fv_rope_args* a, const fv_pages* c, void* stream)
     need(a, "args");
     const size_t e = type_size(a->dtype);
     check_heads(a->n_q_heads, a->n_kv_heads, a->head_dim);
-    if (a->n < 0) bad("n must not be negative");
+    if (a->n < 0 || a->n > 1 << 26) bad("n must be 0 to 2^26");
     if (a->n_axes < 1 || a->n_axes > 4) bad("n_axes must be 1 to 4");
     int64_t pairs = 0;
     for (int i = 0; i < a->n_axes; ++i) {
@@ -205,8 +209,9 @@ fv_status fv_prompt_attention(const fv_prompt_args* a, void* stream) {
     if (a->causal != 0 && a->causal != 1) bad("causal must be 0 or 1");
     if (!(a->scale > 0.f) || !std::isfinite(a->scale)) bad("scale must be positive and finite");
     if (a->n_seqs == 0 || a->n_q == 0) return;
-    if ((int64_t)a->n_q * a->n_q_heads + (int64_t)a->n_seqs * a->n_kv_heads > INT32_MAX)
-      bad("n_q * n_q_heads + n_seqs * n_kv_heads must be below 2^31");
+    if ((int64_t)a->n_q * a->n_q_heads > 1 << 30) bad("n_q * n_q_heads must be at most 2^30");
+    if ((int64_t)a->n_seqs * a->n_kv_heads > 1 << 22)
+      bad("n_seqs * n_kv_heads must be at most 2^22");
     const int rq = a->n_q_heads * a->head_dim, rk = a->n_kv_heads * a->head_dim;
     const Span q = operand(a->q, a->n_q, a->ldq, rq, e, "q");
     const Span o = operand(a->out, a->n_q, a->ldo, rq, e, "out");

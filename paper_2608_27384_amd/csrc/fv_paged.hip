@@ -438,7 +438,7 @@ PagedPlan plan_paged(int n, int n_q_heads, int n_kv_heads, int head_dim, int max
   if (chunk > 2048) chunk = 2048;
   int64_t chunks = (max_keys + chunk - 1) / chunk;
   if (chunks < 1) chunks = 1;
-  while (chunks > 1 && chunks * cols > (1 << 30)) chunks /= 2;  // the grid's limit: longer last chunks
+  while (chunks > 1 && chunks * cols > 1 << 23) chunks /= 2;  // the grid's limit: longer last chunks
   p.chunk = (int)chunk;
   p.n_chunks = (int)chunks;
   if (chunks > 1) {

@@ -269,7 +269,7 @@ __global__ __launch_bounds__(kPlanThreads) void grow_plan_kernel(fv_pages c, con
         ok = len >= 0 && len <= holds && more >= 0 && more <= holds - len;
         if (ok && more > 0 && len % c.page_len) {
           const int last = c.table[(size_t)s * c.max_pages + len / c.page_len];
-          ok = is_page(c, last) && c.refs[last] <= 1;
+          ok = is_page(c, last) && c.refs[last] == 1;
         }
         if (ok) {
           have = pages_of(len, c.page_len);

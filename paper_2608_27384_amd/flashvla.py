@@ -466,6 +466,8 @@ def _rows(t, what: str, dtype, device, shape=None) -> int:
     ld, sh, sd = t.stride()
     if (sd != 1 and d > 1) or (sh != d and h > 1):
         _refuse(f"the heads of {what} must lie side by side (strides {(ld, sh, sd)})")
+    if n > 1 and ld > 1 << 20:
+        _refuse(f"the rows of {what} lie {ld} elements apart, more than 2^20")
     return ld if n > 1 else h * d
 
 
@@ -615,6 +617,7 @@ class PageCache:
         (and k_out, if given), and stores v."""
         if v is None or seqs is None or at is None:
             _refuse("append needs v, seqs and at")
+        self._layer(layer)
         _rope(self.c, layer, q, k, v, pos, seqs, at, sections, theta, q if q_out is None else q_out,
               k_out, stream)
 
@@ -626,6 +629,7 @@ class PageCache:
         ldo = _rows(out, "out", t, dev, q.shape)
         n, heads, dh = q.shape
         cache = byref(self.c)
+        self._layer(layer)
         if dh != self.c.head_dim:
             _refuse(f"head_dim of q is {dh}, of the cache {self.c.head_dim}")
         args = FvPagedArgs(q.data_ptr(), out.data_ptr(), ldq, ldo, _int32(seqs, "seqs", dev, (n,)), n,
@@ -637,6 +641,10 @@ class PageCache:
                 work = _work(need.value, dev)
                 args.work, args.work_bytes = work.data_ptr(), need.value
             _check_context(L.fv_paged_attention(a, cache, on.raw), "fv_paged_attention")
+
+    def _layer(self, layer: int) -> None:
+        if not 0 <= layer < self.c.n_layers:
+            _refuse(f"layer {layer} of {self.c.n_layers}")
 
     def _upkeep(self, name: str, stream, *lists, status=None, work=True):
         dev = self.k.device

@@ -190,3 +190,44 @@ def test_binding_refuses_tensors():
     no(c.append, 0, q, k, k, pos[:2], seqs, seqs, (8, 12, 12))
     no(c.append, 0, q, k, k, pos, seqs, seqs, (8, 8, 4, 4, 8))
     no(fvb.rope, q, k[:2], pos, (8, 12, 12), q)
+
+
+def test_sizes_beyond_a_launch():
+    """Sizes whose grid would hold 2^32 threads or more are refused before anything is launched."""
+    L, ref = fvb.lib(), ctypes.byref
+    refused(L.fv_rope_append(ref(rope_args(n=(1 << 26) + 1)), None, None), "2^26")
+    refused(L.fv_prompt_attention(ref(prompt_args(n_q=(1 << 28) + 1)), None), "2^30")
+    wide = dict(n_seqs=65536, n_q_heads=128, n_kv_heads=128, ldq=8192, ldk=8192, ldv=8192, ldo=8192)
+    refused(L.fv_prompt_attention(ref(prompt_args(**wide)), None), "2^22")
+    many = cache(n_kv_heads=128, max_seqs=65536, max_pages=65536)
+    n = ctypes.c_size_t()
+    refused(L.fv_paged_attention_workspace(ref(paged_args(n=65536, n_q_heads=128)), ref(many), ref(n)),
+            "2^22")
+    refused(L.fv_paged_attention(ref(paged_args(n=65536, n_q_heads=128)), ref(many), None), "2^22")
+    # the most rows that are taken: two chunks each, 2^23 workgroups
+    assert L.fv_paged_attention_workspace(ref(paged_args(n=32768, n_q_heads=128)), ref(many), ref(n)) == 0
+    assert n.value == 2 * 32768 * 128 * (64 + 2) * 4
+
+
+def test_binding_refuses_what_32_bits_would_lose():
+    torch = pytest.importorskip("torch")
+    apart = torch.zeros(1).expand(1).as_strided((1, 4, 64), (256, 0, 0))
+    far = torch.empty_strided((2, 4, 64), ((1 << 32) + 256, 64, 1), device="meta")
+    near = torch.empty((2, 4, 64), device="meta")
+    k = torch.empty((2, 2, 64), device="meta")
+    cu = torch.empty(2, dtype=torch.int32, device="meta")
+    for q, out in ((far, near), (near, far)):
+        with pytest.raises(fvb.FlashVLAError, match="2\\^20"):
+            fvb.prompt_attention(q, k, k, cu, cu, out)
+    with pytest.raises(fvb.FlashVLAError, match="side by side"):
+        fvb.prompt_attention(apart, apart, apart, cu, cu, apart)
+    pool, refs = torch.zeros(2, 10, 2, 16, 64), torch.zeros(10, dtype=torch.int32)
+    table, length = torch.zeros(4, 3, dtype=torch.int32), torch.zeros(4, dtype=torch.int32)
+    c = fvb.PageCache(pool, pool.clone(), table, length, refs)
+    q, k = torch.zeros(3, 4, 64), torch.zeros(3, 2, 64)
+    seqs, pos = torch.zeros(3, dtype=torch.int32), torch.zeros(1, 3, dtype=torch.int32)
+    for layer in (2, -1, 1 << 32):
+        with pytest.raises(fvb.FlashVLAError, match="layer"):
+            c.attend(layer, q, seqs, q.clone())
+        with pytest.raises(fvb.FlashVLAError, match="layer"):
+            c.append(layer, q, k, k, pos, seqs, seqs, (32,))

@@ -114,6 +114,16 @@ def test_refused_lists_change_nothing():
     assert int(cache.free(t([1]))) == 0  # what is no page is skipped
 
 
+@pytest.mark.parametrize("refs", [0, 2, -1])
+def test_a_last_page_that_is_not_the_sequences_alone_is_not_grown_into(refs):
+    cache, model = fresh(12, 4, 3)
+    assert cache.grow(cu.ints([1]), cu.ints([5])).item() == 0
+    cache.refs[0] = refs
+    before = state(cache)
+    assert cache.grow(cu.ints([1]), cu.ints([1])).item() == 1
+    assert unchanged(cache, before)
+
+
 @pytest.mark.parametrize("n,width", [(1024, 5), (1025, 5), (2600, 4), (40, 300)])
 def test_long_lists(n, width):
     """More entries than a plan carries out by itself, and just as many."""
