@@ -72,9 +72,9 @@ void check_cache(const fv_pages* c) {
   aligned(c->refs, 4, "cache refs");
 }
 
-// A strided operand: rows of `row` elements, ld apart.
+// A strided operand: rows of `row` bytes, `ld` bytes apart, from lo to hi.
 struct Span {
-  uintptr_t lo = 0, hi = 0;
+  uintptr_t lo = 0, hi = 0, row = 0, ld = 0;
 };
 Span operand(const void* p, int n, int ld, int row, size_t e, const char* what) {
   aligned(p, 16, what);
@@ -82,10 +82,16 @@ Span operand(const void* p, int n, int ld, int row, size_t e, const char* what) 
     bad(std::string("leading dimension of ") + what + " must be at least " + std::to_string(row) +
         ", at most 2^20 and a multiple of 16 bytes");
   const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
-  return Span{lo, lo + (n > 0 ? ((size_t)(n - 1) * ld + row) * e : 0)};
+  return Span{lo, lo + (n > 0 ? ((size_t)(n - 1) * ld + row) * e : 0), (size_t)row * e, (size_t)ld * e};
 }
+// Columns of one packed matrix are apart though their spans are not.
 void apart(const Span& a, const Span& b, const char* what) {
-  if (a.lo < b.hi && b.lo < a.hi) bad(std::string(what) + " must not overlap");
+  if (a.lo >= b.hi || b.lo >= a.hi) return;
+  if (a.ld == b.ld) {
+    const uintptr_t d = a.lo < b.lo ? (b.lo - a.lo) % a.ld : (a.lo - b.lo) % a.ld;
+    if (a.lo < b.lo ? d >= a.row && d + b.row <= a.ld : d >= b.row && d + a.row <= a.ld) return;
+  }
+  bad(std::string(what) + " must not overlap");
 }
 
 // A launch holds less than 2^32 threads: the bounds of n, n * heads and n_seqs * heads in the

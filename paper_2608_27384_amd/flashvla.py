@@ -617,6 +617,8 @@ class PageCache:
         (and k_out, if given), and stores v."""
         if v is None or seqs is None or at is None:
             _refuse("append needs v, seqs and at")
+        if q.device != self.k.device:
+            _refuse(f"q is on {q.device}, the cache on {self.k.device}")
         self._layer(layer)
         _rope(self.c, layer, q, k, v, pos, seqs, at, sections, theta, q if q_out is None else q_out,
               k_out, stream)

@@ -231,3 +231,23 @@ def test_binding_refuses_what_32_bits_would_lose():
             c.attend(layer, q, seqs, q.clone())
         with pytest.raises(fvb.FlashVLAError, match="layer"):
             c.append(layer, q, k, k, pos, seqs, seqs, (32,))
+
+
+@pytest.mark.parametrize("q_at,k_at,ldk", [(0, 496, 384), (64, 0, 384), (256, 240, 384), (272, 0, 384),
+                                           (512, 384, 384), (0, 512, 392)])
+def test_columns_of_one_matrix_that_overlap(q_at, k_at, ldk):
+    """q_out (4 heads of 64) and k_out (2) from these bytes of one bf16 matrix on, rows of 384
+    elements (768 bytes): columns apart would be taken, these are not."""
+    a = rope_args(q_out=(P << 3) + q_at, k_out=(P << 3) + k_at, ldq_out=384, ldk_out=ldk)
+    refused(fvb.lib().fv_rope_append(ctypes.byref(a), ctypes.byref(cache()), None), "overlap")
+
+
+def test_binding_refuses_a_cache_elsewhere():
+    torch = pytest.importorskip("torch")
+    pool, refs = torch.zeros(2, 10, 2, 16, 64), torch.zeros(10, dtype=torch.int32)
+    table, length = torch.zeros(4, 3, dtype=torch.int32), torch.zeros(4, dtype=torch.int32)
+    c = fvb.PageCache(pool, pool.clone(), table, length, refs)
+    q, k = (torch.empty((3, h, 64), device="meta") for h in (4, 2))
+    seqs, pos = (torch.empty(s, dtype=torch.int32, device="meta") for s in ((3,), (1, 3)))
+    with pytest.raises(fvb.FlashVLAError, match="the cache on cpu"):
+        c.append(0, q, k, k, pos, seqs, seqs, (32,))

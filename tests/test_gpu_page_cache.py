@@ -293,6 +293,25 @@ def test_rotary_rows_far_apart():
     assert q.equal(qo) and k.equal(ko)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_rotary_into_columns_of_one_matrix(dtype):
+    """Queries and keys rotated into their columns of one packed matrix, the other columns left."""
+    torch = cu.torch_mod()
+    from paper_2608_27384_amd.flashvla import rope
+    n, H, G, D = 37, 4, 2, 64
+    qkv = cu.randn(dtype, 5, n, (H + 2 * G) * D)
+    q, k = qkv[:, :H * D].unflatten(1, (H, D)), qkv[:, H * D:(H + G) * D].unflatten(1, (G, D))
+    pos = cu.ints([np.arange(n)])
+    qo, ko = torch.empty_like(q), torch.empty_like(k)
+    rope(q, k, pos, (D // 2,), qo, ko)
+    for order in ((0, H), (G, 0)):  # queries first, keys first
+        packed = torch.full((n, (H + 2 * G) * D), 7.0, dtype=qkv.dtype, device="cuda")
+        heads = packed.unflatten(1, (H + 2 * G, D))
+        rope(q, k, pos, (D // 2,), heads[:, order[0]:order[0] + H], heads[:, order[1]:order[1] + G])
+        assert heads[:, order[0]:order[0] + H].equal(qo) and heads[:, order[1]:order[1] + G].equal(ko)
+        assert (heads[:, H + G:] == 7).all()
+
+
 def test_one_axis_is_the_action_tokens_rotation():
     """Equal positions on every axis turn as one axis does."""
     torch = cu.torch_mod()

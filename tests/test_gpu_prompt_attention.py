@@ -96,6 +96,20 @@ def test_strided_rows_and_rows_behind_the_last_prompt(shape):
     assert (wide[n:] == 7).all() and (wide[:, H * D:] == 7).all()
 
 
+@pytest.mark.parametrize("shape", [SHAPES[1], FULL[5]], ids=str)
+def test_results_beside_the_queries(shape):
+    """out in columns of the matrix that holds q, k and v."""
+    torch = cu.torch_mod()
+    dtype, H, G, D = shape
+    n = 77
+    cols = cu.randn(dtype, 4, n, 2 * H + 2 * G, D)
+    q, k, v, out = cols[:, :H], cols[:, H:H + G], cols[:, H + G:H + 2 * G], cols[:, H + 2 * G:]
+    kept = cols[:, :H + 2 * G].clone()
+    run(q, k, v, [0, 40, n], [0, 40, n], True, out)
+    check(shape, out, q, k, v, [0, 40, n], [0, 40, n], True)
+    assert torch.equal(cols[:, :H + 2 * G], kept)
+
+
 @pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
 @pytest.mark.parametrize("where", ["k", "v"])
 @pytest.mark.parametrize("shape", [SHAPES[0], SHAPES[1], SHAPES[2], SHAPES[3], SHAPES[6], FULL[0], FULL[3],
