@@ -139,7 +139,7 @@ __device__ __forceinline__ int pages_of(int len, int page_len) {
 __device__ __forceinline__ bool is_page(const fv_pages& c, int p) { return p >= 0 && p < c.n_pages; }
 
 // A plan kernel is one workgroup, bound by its trips to memory one after another: 7.4
-// us to fork, 6.2 to grow, 9.7 to compact a cache of 4000 pages.
+// us to fork, 6 to grow, 9.7 to compact a cache of 4000 pages.
 // Exclusive sum over the workgroup; *total is the whole.
 __device__ int block_scan(int x, int* wave_sums, int* total) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
@@ -241,10 +241,16 @@ __device__ __forceinline__ void verdict(int st, int* status, int* work) {
   }
 }
 
-// Entries that a plan kernel can carry out by itself: a launch of its own costs 3.4
-// us of the host and 3 to 4 us of the GPU.
-constexpr int kInline = kPlanThreads;      // requests of a grow
-constexpr int kInlineRows = 8192;          // table entries of a free
+// Entries that a plan kernel carries out by itself: a launch of its own costs 3.4 us of
+// the host.  us on the GPU by itself and with a second launch: grown by a page each, 64
+// sequences 6.0 and 7.9, 1024 8.0 and 9.5; by 51 pages each, 64 sequences 7.7 and 8.6, 512
+// 18 and 14; freed, with 408 table entries 2.2 and 4.0, with 8192 4.9 and 4.0.
+constexpr int kInline = kPlanThreads;  // sequences of a grow or free
+constexpr int kInlineRows = 8192;      // table entries of a free
+__host__ __device__ __forceinline__ bool free_inline(const fv_pages& c, int n) {
+  return n <= kInline && (long long)n * c.max_pages <= kInlineRows;
+}
+constexpr int kBatch = 4;  // entries of a thread under way at a time
 
 // Workspace: [0] the call's status; lists A, B, C of `list` ints each.
 // A: pages taken.  B[i]: how many were taken for the entries before i.
@@ -254,7 +260,8 @@ __global__ __launch_bounds__(kPlanThreads) void grow_plan_kernel(fv_pages c, con
                                                                  int* status, int* work,
                                                                  int list) {
   __shared__ PlanShared sh;
-  __shared__ int first[kInline], place[kInline];  // of a request's pages: in A, in the table
+  __shared__ int first[kInline];       // of a request's pages: in A
+  __shared__ uint32_t place[kInline];  // and in the table
   int* A = work + kPagesHeader;
   int* B = A + list;
   Holders h;
@@ -290,7 +297,7 @@ __global__ __launch_bounds__(kPlanThreads) void grow_plan_kernel(fv_pages c, con
       B[i] = (int)(total + before);
       if (n <= kInline) {
         first[i] = before;
-        place[i] = have;
+        place[i] = (uint32_t)mine * c.max_pages + have;
       }
     }
     total += all;
@@ -301,18 +308,46 @@ __global__ __launch_bounds__(kPlanThreads) void grow_plan_kernel(fv_pages c, con
     return verdict(FV_PAGES_FULL, status, work);
   verdict(FV_PAGES_OK, status, work);
   if (n > kInline) return;
-  for (int t = threadIdx.x; t < (int)total; t += kPlanThreads) {
-    int lo = 0, hi = n;  // the last request whose pages start at t or before
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (first[mid] <= t)
-        lo = mid;
-      else
-        hi = mid;
+  if (total <= kPlanThreads) {  // a page a thread
+    const int t = threadIdx.x;
+    if (t < (int)total) {
+      const int page = A[t];
+      int lo = 0, hi = n;  // the last request whose pages start at t or before
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (first[mid] <= t)
+          lo = mid;
+        else
+          hi = mid;
+      }
+      c.table[(size_t)place[lo] + (t - first[lo])] = page;
+      c.refs[page] = 1;
     }
-    const int page = A[t];
-    c.table[(size_t)seqs[lo] * c.max_pages + place[lo] + t - first[lo]] = page;
-    c.refs[page] = 1;
+  } else {  // 16 lanes a request: no search, which 52 thousand pages would spend 45 us on
+    constexpr int LANES = 16, GROUPS = kPlanThreads / LANES;
+    for (int i0 = threadIdx.x / LANES; i0 < n; i0 += kBatch * GROUPS) {
+      int at[kBatch], end[kBatch], most = 0;
+      uint32_t to[kBatch];
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) {
+        const int i = i0 + u * GROUPS, r = min(i, n - 1);
+        at[u] = first[r];
+        end[u] = i >= n ? at[u] : r + 1 < n ? first[r + 1] : (int)total;
+        to[u] = place[r];
+        most = max(most, end[u] - at[u]);
+      }
+      for (int j = threadIdx.x % LANES; j < most; j += LANES) {
+        int page[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) page[u] = at[u] + j < end[u] ? A[at[u] + j] : -1;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u)
+          if (page[u] >= 0) {
+            c.table[(size_t)to[u] + j] = page[u];
+            c.refs[page[u]] = 1;
+          }
+      }
+    }
   }
   if (mine >= 0) c.len[mine] = now;
 }
@@ -427,23 +462,43 @@ __global__ __launch_bounds__(256) void fork_apply_kernel(fv_pages c, const int* 
 __global__ __launch_bounds__(kPlanThreads) void free_plan_kernel(fv_pages c, const int* seqs, int n,
                                                                  int* status) {
   __shared__ PlanShared sh;
+  __shared__ uint32_t place[kInline];  // of a sequence's table row
+  __shared__ int held[kInline];        // its pages
+  const bool here = free_inline(c, n);
   clear_seen(sh, c.max_seqs);
+  int mine = -1;
   for (int i = threadIdx.x; i < n; i += kPlanThreads) {
     const int s = seqs[i];
-    if (s < 0 || s >= c.max_seqs || mark(sh, s)) sh.bad = 1;
+    if (s < 0 || s >= c.max_seqs || mark(sh, s)) {
+      sh.bad = 1;
+    } else if (here) {
+      mine = s;
+      place[i] = (uint32_t)s * c.max_pages;
+      held[i] = pages_of(min(max(c.len[s], 0), c.max_pages * c.page_len), c.page_len);
+    }
   }
   __syncthreads();
   verdict(sh.bad ? FV_PAGES_BAD : FV_PAGES_OK, status, nullptr);
-  if (sh.bad || (long long)n * c.max_pages > kInlineRows) return;
-  for (int t = threadIdx.x; t < n * c.max_pages; t += kPlanThreads) {
-    const int i = t / c.max_pages, j = t - i * c.max_pages, s = seqs[i];
-    int* at = c.table + (size_t)s * c.max_pages + j;
-    const int p = *at;
-    if (j * c.page_len < c.len[s] && is_page(c, p)) atomicSub(&c.refs[p], 1);
-    *at = -1;
+  if (sh.bad || !here) return;
+  const int rows = n * c.max_pages;
+  for (int t0 = threadIdx.x; t0 < rows; t0 += kBatch * kPlanThreads) {
+    int* at[kBatch];
+    int page[kBatch];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int t = min(t0 + u * kPlanThreads, rows - 1), i = t / c.max_pages, j = t - i * c.max_pages;
+      at[u] = c.table + (size_t)place[i] + j;
+      page[u] = *at[u];
+      if (j >= held[i]) page[u] = -1;
+    }
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u)
+      if (t0 + u * kPlanThreads < rows) {
+        if (is_page(c, page[u])) atomicSub(&c.refs[page[u]], 1);
+        *at[u] = -1;
+      }
   }
-  __syncthreads();  // the lengths have been read
-  for (int i = threadIdx.x; i < n; i += kPlanThreads) c.len[seqs[i]] = 0;
+  if (mine >= 0) c.len[mine] = 0;
 }
 
 __global__ __launch_bounds__(256) void free_apply_kernel(fv_pages c, const int* seqs,
@@ -640,7 +695,7 @@ void launch_pages_fork(const fv_pages& c, const int* parents, const int* childre
 
 void launch_pages_free(const fv_pages& c, const int* seqs, int n, int* status, hipStream_t s) {
   hipLaunchKernelGGL(free_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, c, seqs, n, status);
-  if ((int64_t)n * c.max_pages > kInlineRows)
+  if (!free_inline(c, n))
     hipLaunchKernelGGL(free_apply_kernel, dim3(n), dim3(256), 0, s, c, seqs, status);
 }
 
