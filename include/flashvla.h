@@ -582,8 +582,9 @@ fv_status fv_paged_attention(const fv_paged_args *args, const fv_pages *cache, v
  *  fv_pages_gather   copies sequences out, dense, as fv_set_prefix takes them:
  *                    k_out, v_out [n_layers][n][ld][n_kv_heads][head_dim]; row r of
  *                    entry i is position r of seqs[i], for r < min(len, ld); other
- *                    rows, and those on table entries that are no page, are left as
- *                    they were.  A sequence may occur several times; n <= 65536.
+ *                    rows, those on table entries that are no page and the entries
+ *                    whose seqs is out of range are left as they were.  A sequence
+ *                    may occur several times; n <= 65536.
  * FV_PAGES_FULL: fewer free pages than the call needs.
  * Errors: FV_ERR_INVALID_ARG, FV_ERR_HIP.
  */

@@ -397,3 +397,51 @@ def test_context_of_a_run(dtype):
             assert rel_err(got[b], ref[b]) < tol(w)
     finally:
         case.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_captured_token_step(dtype):
+    """A token step of two layers (room, rotary append where the lengths say, attention) in one
+    graph, replayed over page ends with the eager steps of another cache between."""
+    torch = cu.torch_mod()
+    H, G, D, L, n = 4, 2, 64, 2, 5
+    sections = (D // 2,)
+    runs = []
+    for _ in range(2):
+        cache, _ = fresh(60, 6, 8, 16, layers=L, heads=G, D=D, dtype=dtype, seed=3)
+        cache.grow(cu.ints(range(6)), cu.ints([1, 15, 16, 0, 31, 40]))
+        runs.append(cache)
+    seqs = cu.ints([4, 0, 2, 1, -1])
+    live = seqs.long()[:4]
+    x = [cu.randn(dtype, 20 + i, n, h, D) for i, h in enumerate((H, G, G))]
+
+    def buffers():
+        return dict(q=torch.empty_like(x[0]), out=[torch.zeros_like(x[0]) for _ in range(L)],
+                    at=torch.zeros(n, dtype=torch.int32, device="cuda"),
+                    one=torch.ones(4, dtype=torch.int32, device="cuda"), few=seqs[:4].clone(),
+                    status=torch.empty(1, dtype=torch.int32, device="cuda"))
+
+    def step(cache, b):
+        cache.grow(b["few"], b["one"], b["status"])
+        b["at"][:4].copy_(cache.length.index_select(0, live) - 1)
+        for l in range(L):
+            cache.append(l, x[0], x[1], x[2], b["at"].view(1, n), seqs, b["at"], sections, q_out=b["q"])
+            cache.attend(l, b["q"], seqs, b["out"][l])
+
+    a, b = buffers(), buffers()
+    before = state(runs[0])
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step(runs[0], a)
+    assert unchanged(runs[0], before)
+    for i in range(20):
+        for t, scale in zip(x, (0.9, 1.1, -0.8)):
+            t.mul_(scale)
+        g.replay()
+        step(runs[1], b)
+        torch.cuda.synchronize()
+        assert a["status"].item() == 0 and b["status"].item() == 0
+        assert unchanged(runs[0], state(runs[1]))
+        for l in range(L):
+            assert a["out"][l].equal(b["out"][l]) and (a["out"][l][4] == 0).all()
+    assert runs[0].length.tolist() == [21, 35, 36, 0, 51, 40]
