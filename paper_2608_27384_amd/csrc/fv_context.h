@@ -11,16 +11,33 @@ __host__ __device__ __forceinline__ size_t page_row(int page, int n_kv, int head
   return ((size_t)page * n_kv + head) * page_len;
 }
 
+// Data that no cache holds until it is used again (the last level has 256 MiB) is moved past
+// them: above twice that size a call's loads and stores are marked as streaming.  Paged
+// attention, 192 rows of 1 to 8191 keys, 32/8 heads of 128 (3.2 GB), 569 us, streaming 524;
+// 64 of 500 to 3001, fp32, 8/1 of 256 (0.2 GB), called again and again, 68 and 79.  Gathering
+// 64 sequences of 300 to 816 in 18 layers (1.3 GB moved) 243 and 228.
+constexpr size_t kStreamBytes = (size_t)512 << 20;
+template <bool STREAM, typename V> __device__ __forceinline__ V load_piece(const V* p) {
+  if constexpr (STREAM) return __builtin_nontemporal_load(p);
+  return *p;
+}
+template <bool STREAM, typename V> __device__ __forceinline__ void store_piece(V* p, V x) {
+  if constexpr (STREAM)
+    __builtin_nontemporal_store(x, p);
+  else
+    *p = x;
+}
+
 // The launches take validated arguments.
 template <typename T>
 void launch_rope_append(const fv_rope_args& a, const fv_pages* c, hipStream_t s);
 template <typename T>
 void launch_prompt(const fv_prompt_args& a, hipStream_t s);
 
-// How a paged attention is laid out: chunks of `chunk` keys, at most n_chunks
+// How a paged attention is laid out for up to `keys` keys: chunks of `chunk`, at most n_chunks
 // a sequence, each with one workgroup per kv head and tile of 16 query heads.
 struct PagedPlan {
-  int chunk, n_chunks;
+  int keys, chunk, n_chunks;
   size_t work_bytes;  // partial outputs and softmax statistics; 0 with one chunk
 };
 PagedPlan plan_paged(int n, int n_q_heads, int n_kv_heads, int head_dim, int max_keys, bool bf16);

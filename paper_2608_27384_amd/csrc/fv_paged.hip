@@ -17,7 +17,7 @@
 // head a matrix row stands for is free, and chosen so that this works out.
 //
 // Measured (a read of memory alone reaches 6.2 TB/s): 192 rows of 1 to 8191 keys, heads
-// 32/8 of 128, 569 us (5.7 TB/s); 192 of 1 to 16000, 8/1 of 256, 307 us (5.2); 64 of 816,
+// 32/8 of 128, 524 us (6.2 TB/s); 192 of 1 to 16000, 8/1 of 256, 290 us (5.5); 64 of 816,
 // 14 us, of which the two launches are 7; 1 of 800, 10 us.
 #include "fv_context.h"
 
@@ -59,9 +59,9 @@ __device__ __forceinline__ int length_of(const PagedCall& a, int s) {
 // A V tile in registers, and its matrix operands.  bf16: 32 keys, 8 a lane
 // (4g .. 4g+3 of either half); the head's 128-element blocks 8 elements a lane,
 // a last block of 64 four.  fp32: 16 keys, 4 a lane, blocks of 64, 4 elements.
-template <typename T, int DH> struct VTile;
+template <typename T, int DH, bool STREAM> struct VTile;
 
-template <int DH> struct VTile<bf16_t, DH> {
+template <int DH, bool STREAM> struct VTile<bf16_t, DH, STREAM> {
   static constexpr int B8 = DH / 128, B4 = (DH % 128) / 64;
   u32x4 w[B8 > 0 ? B8 : 1][8];
   u32x2 n[8];
@@ -70,8 +70,8 @@ template <int DH> struct VTile<bf16_t, DH> {
     for (int x = 0; x < 8; ++x) {
       const bf16_t* p = row[x >> 2] + (size_t)(4 * lg + (x & 3)) * DH;
 #pragma unroll
-      for (int b = 0; b < B8; ++b) w[b][x] = *reinterpret_cast<const u32x4*>(p + 128 * b + 8 * l16);
-      if (B4) n[x] = *reinterpret_cast<const u32x2*>(p + 128 * B8 + 4 * l16);
+      for (int b = 0; b < B8; ++b) w[b][x] = load_piece<STREAM>(reinterpret_cast<const u32x4*>(p + 128 * b + 8 * l16));
+      if (B4) n[x] = load_piece<STREAM>(reinterpret_cast<const u32x2*>(p + 128 * B8 + 4 * l16));
     }
   }
   __device__ __forceinline__ void drop(int x) {  // key x of the lane is not there
@@ -93,14 +93,15 @@ template <int DH> struct VTile<bf16_t, DH> {
   }
 };
 
-template <int DH> struct VTile<float, DH> {
+template <int DH, bool STREAM> struct VTile<float, DH, STREAM> {
   u32x4 w[DH / 64][4];
   __device__ __forceinline__ void load(const float* const (&row)[1], int l16, int lg) {
 #pragma unroll
     for (int x = 0; x < 4; ++x)
 #pragma unroll
       for (int b = 0; b < DH / 64; ++b)
-        w[b][x] = *reinterpret_cast<const u32x4*>(row[0] + (size_t)(4 * lg + x) * DH + 64 * b + 4 * l16);
+        w[b][x] = load_piece<STREAM>(
+            reinterpret_cast<const u32x4*>(row[0] + (size_t)(4 * lg + x) * DH + 64 * b + 4 * l16));
   }
   __device__ __forceinline__ void drop(int x) {
 #pragma unroll
@@ -118,7 +119,7 @@ template <typename T, int DH> __device__ __forceinline__ int element_of(int t, i
   return t / 8 < B8 ? 128 * (t / 8) + 8 * i + t % 8 : 128 * B8 + 4 * i + (t - 8 * B8);
 }
 
-template <typename T, int DH>
+template <typename T, int DH, bool STREAM>
 __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_kernel(PagedCall a) {
   constexpr int NH = sizeof(T) == 2 ? 2 : 1;       // 16-key halves of a tile
   constexpr int KT = 16 * NH;                      // keys of a tile
@@ -202,14 +203,15 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_kernel(PagedCall a)
       for (int h = 0; h < NH; ++h)
 #pragma unroll
         for (int b = 0; b < KB; ++b)
-          kf[h][b] = *reinterpret_cast<const u32x4*>(row[h] + (size_t)l16 * DH + EB * b + (EB / 4) * lg);
+          kf[h][b] = load_piece<STREAM>(
+              reinterpret_cast<const u32x4*>(row[h] + (size_t)l16 * DH + EB * b + (EB / 4) * lg));
     };
     load_keys(0);
     for (int it = 0; it < here; ++it) {
       const T* vrow[NH];
       int left[NH];
       rows(it, vp, vrow, left);
-      VTile<T, DH> vt;
+      VTile<T, DH, STREAM> vt;
       vt.load(vrow, l16, lg);
 
       f32x4 sc[NH];
@@ -418,9 +420,12 @@ __global__ __launch_bounds__(64 * WAVES) void paged_join_kernel(PagedCall a) {
 }
 
 template <typename T, int DH>
-void paged_at(const PagedCall& a, hipStream_t s) {
+void paged_at(const PagedCall& a, size_t bytes, hipStream_t s) {
   const int blocks = a.n * a.n_chunks * a.n_kv * a.q_tiles;
-  hipLaunchKernelGGL((paged_kernel<T, DH>), dim3(blocks), dim3(64 * kPagedWaves), 0, s, a);
+  if (bytes > kStreamBytes)
+    hipLaunchKernelGGL((paged_kernel<T, DH, true>), dim3(blocks), dim3(64 * kPagedWaves), 0, s, a);
+  else
+    hipLaunchKernelGGL((paged_kernel<T, DH, false>), dim3(blocks), dim3(64 * kPagedWaves), 0, s, a);
   // us of both kernels with eight waves and with one: 10.3 and 9.6 at 7 chunks, 10.6 and
   // 10.3 at 16, 10.8 and 11.5 at 32, 15 and 28 at 219 (one row, 8/1 of 256).
   if (a.n_chunks > 16)
@@ -448,6 +453,7 @@ PagedPlan plan_paged(int n, int n_q_heads, int n_kv_heads, int head_dim, int max
   int64_t chunks = (max_keys + chunk - 1) / chunk;
   if (chunks < 1) chunks = 1;
   while (chunks > 1 && chunks * cols > 1 << 23) chunks /= 2;  // the grid's limit: longer last chunks
+  p.keys = max_keys;
   p.chunk = (int)chunk;
   p.n_chunks = (int)chunks;
   if (chunks > 1) {
@@ -484,11 +490,15 @@ void launch_paged(const fv_paged_args& x, const fv_pages& c, const PagedPlan& p,
   a.chunk = p.chunk;
   a.n_chunks = p.n_chunks;
   a.scale = x.scale * kLog2e;
+  // what the call may read: the keys and values planned for, which a layer's pages bound
+  const size_t key = 2 * (size_t)c.n_kv_heads * c.head_dim * sizeof(T);
+  const size_t planned = (size_t)x.n * p.keys * key, pages = (size_t)c.n_pages * c.page_len * key;
+  const size_t bytes = planned < pages ? planned : pages;
   switch (c.head_dim) {
-    case 64: return paged_at<T, 64>(a, s);
-    case 128: return paged_at<T, 128>(a, s);
-    case 192: return paged_at<T, 192>(a, s);
-    default: return paged_at<T, 256>(a, s);
+    case 64: return paged_at<T, 64>(a, bytes, s);
+    case 128: return paged_at<T, 128>(a, bytes, s);
+    case 192: return paged_at<T, 192>(a, bytes, s);
+    default: return paged_at<T, 256>(a, bytes, s);
   }
 }
 template void launch_paged<bf16_t>(const fv_paged_args&, const fv_pages&, const PagedPlan&, hipStream_t);

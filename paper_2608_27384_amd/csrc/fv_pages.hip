@@ -579,6 +579,7 @@ __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(fv_pages c, 
 // Blocks (x, 0) rewrite the table; blocks (x, 1 + 2 l + kv) move pages of layer l, a
 // page at a time, which a few hundred kilobytes in flight a CU keep at the rate of a
 // copy: 672 MB in 132 us (5.1 TB/s).
+template <bool STREAM>
 __global__ __launch_bounds__(256) void compact_apply_kernel(fv_pages c, const int* work, int list,
                                                             int row16) {
   const int moves = work[0], tid = threadIdx.x;
@@ -604,13 +605,14 @@ __global__ __launch_bounds__(256) void compact_apply_kernel(fv_pages c, const in
   for (int i = blockIdx.x; i < moves; i += gridDim.x) {
     const u32x4* src = pool + (base + B[i]) * page16;
     u32x4* dst = pool + (base + A[i]) * page16;
-    for (int x = tid; x < page16; x += 256) dst[x] = src[x];
+    for (int x = tid; x < page16; x += 256) store_piece<STREAM>(dst + x, load_piece<STREAM>(src + x));
   }
 }
 
 // Block (page, entry, layer): the rows of one page of one sequence, keys and values.
 // A copy: 5.0 to 5.5 TB/s at 64 sequences of 300 to 816 tokens, 18 layers, heads of 64
 // to 256.
+template <bool STREAM>
 __global__ __launch_bounds__(256) void gather_kernel(fv_pages c, const int* seqs, int n, int ld,
                                                      u32x4* k_out, u32x4* v_out, int row16) {
   const int l = blockIdx.z, pg = blockIdx.x, tid = threadIdx.x;
@@ -629,13 +631,17 @@ __global__ __launch_bounds__(256) void gather_kernel(fv_pages c, const int* seqs
     for (int x = tid; x < rows * wide; x += 256) {
       const int r = x / wide, y = x - r * wide, h = y / row16;
       const int at = (h * c.page_len + r) * row16 + (y - h * row16);
-      k_out[to + x] = k[at];
-      v_out[to + x] = v[at];
+      store_piece<STREAM>(k_out + to + x, load_piece<STREAM>(k + at));
+      store_piece<STREAM>(v_out + to + x, load_piece<STREAM>(v + at));
     }
   }
 }
 
 int row_pieces(const fv_pages& c) { return c.head_dim * (c.dtype == FV_BF16 ? 2 : 4) / 16; }
+// Keys and values of n tokens in every layer.
+size_t token_bytes(const fv_pages& c, size_t n) {
+  return 2 * n * c.n_layers * c.n_kv_heads * row_pieces(c) * 16;
+}
 
 template <typename T, int DH>
 void rope_at(const RopeCall& r, hipStream_t s) {
@@ -703,15 +709,19 @@ void launch_pages_compact(const fv_pages& c, int* used, int* work, hipStream_t s
   const int list = (int)pages_list(c);
   hipLaunchKernelGGL(compact_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, c, used, work, list);
   const int most = c.n_pages / 2 > 1 ? c.n_pages / 2 : 1;  // no more pages than holes can move
-  hipLaunchKernelGGL(compact_apply_kernel, dim3(most < 1024 ? most : 1024, 1 + 2 * c.n_layers),
-                     dim3(256), 0, s, c, work, list, row_pieces(c));
+  // at most half of the pages are read and as many written
+  const bool stream = token_bytes(c, (size_t)c.n_pages * c.page_len) > kStreamBytes;
+  hipLaunchKernelGGL(stream ? compact_apply_kernel<true> : compact_apply_kernel<false>,
+                     dim3(most < 1024 ? most : 1024, 1 + 2 * c.n_layers), dim3(256), 0, s, c, work,
+                     list, row_pieces(c));
 }
 
 void launch_pages_gather(const fv_pages& c, const int* seqs, int n, int ld, void* k_out,
                          void* v_out, hipStream_t s) {
   const int holds = c.max_pages * c.page_len;
   const int pages = ((ld < holds ? ld : holds) + c.page_len - 1) / c.page_len;
-  hipLaunchKernelGGL(gather_kernel, dim3(pages, n < 65535 ? n : 65535, c.n_layers), dim3(256), 0, s,
+  const bool stream = 2 * token_bytes(c, (size_t)n * pages * c.page_len) > kStreamBytes;
+  hipLaunchKernelGGL(stream ? gather_kernel<true> : gather_kernel<false>, dim3(pages, n < 65535 ? n : 65535, c.n_layers), dim3(256), 0, s,
                      c, seqs, n, ld, static_cast<u32x4*>(k_out), static_cast<u32x4*>(v_out),
                      row_pieces(c));
 }

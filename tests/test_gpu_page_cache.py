@@ -190,6 +190,41 @@ def test_gather(page_len, dtype, D):
     assert k.equal(want[0]) and v.equal(want[1])
 
 
+@pytest.mark.parametrize("dtype,D", [("bf16", 64), ("fp32", 192)])
+def test_copies_of_more_than_the_caches_hold(dtype, D):
+    """Gathered and compacted in a pool of more than half a gigabyte."""
+    torch = cu.torch_mod()
+    G, L = 2, 2
+    token = 2 * L * G * D * (2 if dtype == "bf16" else 4)
+    pages = (1 << 29) // (16 * token) + 9
+    cache, model = fresh(pages, 5, pages, layers=L, heads=G, D=D, dtype=dtype)
+    lens = [70, (pages // 2) * 16 - 3, 1, 0, pages * 5 + 1]
+    assert int(cache.grow(cu.ints(range(5)), cu.ints(lens))) == 0
+    model.grow(list(range(5)), lens)
+
+    def gathered(seqs, ld):
+        k, v = (torch.full((L, len(seqs), ld, G, D), 7.0, dtype=cache.k.dtype, device="cuda")
+                for _ in range(2))
+        cache.gather(cu.ints(seqs), k, v)
+        return k, v
+
+    ld = lens[1] + 40
+    got = gathered([4, 1], ld)
+    table = cache.table.long()
+    for out, pool in zip(got, (cache.k, cache.v)):
+        for i, s in enumerate((4, 1)):
+            want = pool[:, table[s, :-(-lens[s] // 16)]].transpose(2, 3).reshape(L, -1, G, D)
+            assert out[:, i, :lens[s]].equal(want[:, :lens[s]]) and bool((out[:, i, lens[s]:] == 7).all())
+    assert int(cache.free(cu.ints([1]))) == 0
+    model.free([1])
+    before = gathered([4, 0, 2], ld)
+    used, _ = model.compact()
+    assert int(cache.compact()) == used
+    same(cache, model)
+    after = gathered([4, 0, 2], ld)
+    assert before[0].equal(after[0]) and before[1].equal(after[1])
+
+
 def test_captured_upkeep():
     """Free, fork, grow and compact in one graph, replayed on bookkeeping that changes."""
     torch = cu.torch_mod()

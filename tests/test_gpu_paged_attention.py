@@ -201,3 +201,26 @@ def test_a_row_does_not_depend_on_the_others():
     cache.length[0] = 3
     cache.attend(0, q, cu.ints([0, 1, 2]), b)
     assert torch.equal(a[1:], b[1:]) and not torch.equal(a[0], b[0])
+
+
+@pytest.mark.parametrize("shape", [(t, 4, 4, D) for t in ("bf16", "fp32") for D in (64, 128, 192, 256)],
+                         ids=str)
+def test_more_than_the_caches_hold(shape):
+    """A layer of more than half a gigabyte, and rows that might read as much: streamed."""
+    torch = cu.torch_mod()
+    from paper_2608_27384_amd.flashvla import PageCache
+    small, q, table = make(shape, LENS, layers=1)
+    key = 2 * shape[2] * shape[3] * q.element_size()
+    pages = (1 << 29) // (16 * key) + 7
+    k, v = (torch.full((1, pages, *x.shape[2:]), float("nan"), dtype=x.dtype, device="cuda")
+            for x in (small.k, small.v))
+    k[:, :small.k.shape[1]], v[:, :small.v.shape[1]] = small.k, small.v
+    wide = np.full((len(LENS), pages), -1)
+    wide[:, :table.shape[1]] = table
+    refs = np.zeros(pages)
+    refs[table[table >= 0]] = 1
+    cache = PageCache(k, v, cu.ints(wide), cu.ints(LENS), cu.ints(refs))
+    for max_len in (0, pages * 16):
+        out = torch.full_like(q, 7.0)
+        cache.attend(0, q, cu.ints(range(len(LENS))), out, max_len=max_len)
+        check(shape, cache, table, LENS, q, out, 0)
