@@ -872,13 +872,22 @@ void prompt_at(PromptCall& a, int form, hipStream_t s) {
 // full.  In fp32, where products are 16 times as long and the loads of few rows no
 // matter, kFew and kTiles take: heads of 256, 81 (207) and 161 (583) at 560, 279 (2592)
 // and 309 (2862) at 2240, 541 (10082) and 527 (10700) at 4480; of 128, 44 (44) and 81
-// (80), 154 (390) and 133 (432), 298 (1425) and 240 (1260).
+// (80), 154 (390) and 133 (432), 298 (1425) and 240 (1260).  Long prompts favour kFew: 16
+// of 4000, heads 4/2 of 192 (8000 tiles), 3376 and 4078; 8 of 2400, 8/1 of 256 (4800),
+// 1668 and 1814; but heads of 64, 16 of 4000 (16000), 2400 and 2250.  So does the causal
+// edge, most at 128: 4 prompts of 800, heads 8/2 (800), 74 and 111, all keys seen 137 and
+// 112.
 int prompt_form(const fv_prompt_args& x) {
   const int64_t tiles = (int64_t)x.n_q * x.n_q_heads / 32;
-  if (x.dtype == FV_FP32) return tiles <= (x.head_dim == 128 ? 2048 : 4096) ? kFew : kTiles;
+  const bool far = x.n_k / x.n_seqs >= 2048;  // long prompts
+  if (x.dtype == FV_FP32) {
+    int most = 4096;
+    if (x.head_dim >= 192 && far) most = 8192;
+    if (x.head_dim == 128 && !far) most = x.causal ? 2048 : 768;
+    return tiles <= most ? kFew : kTiles;
+  }
   if (tiles < 384) return kFew;
-  const bool few_long = x.causal && x.n_k / x.n_seqs >= 2048;
-  return tiles <= (few_long ? 2560 : 1024) ? kHalves : kTiles;
+  return tiles <= (x.causal && far ? 2560 : 1024) ? kHalves : kTiles;
 }
 
 }  // namespace
