@@ -28,6 +28,11 @@ template <bool STREAM, typename V> __device__ __forceinline__ void store_piece(V
     *p = x;
 }
 
+constexpr int kRopeThreads = 256;
+constexpr int kRopeTokens = 8;  // most tokens of a workgroup
+// Tokens of a workgroup that rotates n tokens of `row` bytes to be rotated or stored.
+int rope_tokens(int n, size_t row);
+
 // The launches take validated arguments.
 template <typename T>
 void launch_rope_append(const fv_rope_args& a, const fv_pages* c, hipStream_t s);

@@ -94,9 +94,12 @@ void apart(const Span& a, const Span& b, const char* what) {
   bad(std::string(what) + " must not overlap");
 }
 
-// A launch holds less than 2^32 threads: the bounds of n, n * heads and n_seqs * heads in the
-// calls below keep every grid under that (the largest, 512 threads for each of n * heads
-// joined rows, 2^31).
+// A launch holds less than 2^32 threads in x and 2^16 workgroups in y and z.  The bounds of n,
+// n * heads and n_seqs * heads in the calls below keep x under that: the most are the 256
+// threads of 2^23 + 2^22 row tiles and spare slots of prompt attention, the 512 of 2^22 rows
+// that paged attention joins and the rotary tokens, whose number a workgroup follows n
+// (rope_tokens).  y and z count layers (1024 at most, 2049 with keys and values apart) or are cut
+// to fit.
 void check_launch() {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) fail(FV_ERR_HIP, std::string("kernel launch: ") + hipGetErrorString(e));

@@ -12,9 +12,6 @@ namespace {
 
 // ------------------------------------------------------------ rotary append
 
-constexpr int kRopeThreads = 256;
-constexpr int kRopeTokens = 8;  // most tokens of a workgroup
-
 struct RopeCall {
   fv_rope_args a;
   fv_pages c;
@@ -651,6 +648,20 @@ void rope_at(const RopeCall& r, hipStream_t s) {
 
 }  // namespace
 
+// Angles are shared by a token's heads, so one token a workgroup loses nothing; more
+// of them amortise the 64-bit exponentials once the chip is full, the more the less
+// there is to move.  us with 1 | 2 | 8 tokens a workgroup, heads 8/1 of 256 (5 KB a
+// token): 3.4 | 3.8 | 5.8 at 64 tokens, 10.7 | 8.9 | 9.8 at 4096, 77 | 61 | 57 at
+// 32768; 8/2 of 64 (1.5 KB), 42 | 28 | 18 at 32768; 32/8 of 128 (12 KB), 30.9 | 29.9 |
+// 30.5 at 8192, 130 | 135 | 150 at 32768.
+// From 2^24 workgroups on the grid would have the 2^32 threads that no launch takes.
+int rope_tokens(int n, size_t row) {
+  int tokens = n >= 8192 && row < 6 << 10 ? kRopeTokens : 2;
+  if (n < 2048 || (n >= 16384 && row >= 10 << 10)) tokens = 1;
+  while (((int64_t)n + tokens - 1) / tokens * kRopeThreads >= (int64_t)1 << 32) tokens *= 2;
+  return tokens;
+}
+
 template <typename T>
 void launch_rope_append(const fv_rope_args& a, const fv_pages* c, hipStream_t s) {
   RopeCall r{};
@@ -658,18 +669,8 @@ void launch_rope_append(const fv_rope_args& a, const fv_pages* c, hipStream_t s)
   if (c) r.c = *c;
   r.has_cache = c != nullptr;
   r.log2_theta = log2((double)a.theta);
-  // Angles are shared by a token's heads, so one token a workgroup loses nothing; more
-  // of them amortise the 64-bit exponentials once the chip is full, the more the less
-  // there is to move.  us with 1 | 2 | 8 tokens a workgroup, heads 8/1 of 256 (5 KB a
-  // token): 3.4 | 3.8 | 5.8 at 64 tokens, 10.7 | 8.9 | 9.8 at 4096, 77 | 61 | 57 at
-  // 32768; 8/2 of 64 (1.5 KB), 42 | 28 | 18 at 32768; 32/8 of 128 (12 KB), 30.9 | 29.9 |
-  // 30.5 at 8192, 130 | 135 | 150 at 32768.
   const int heads = a.n_q_heads + (c || a.k_out ? a.n_kv_heads : 0) + (c ? a.n_kv_heads : 0);
-  const size_t row = (size_t)heads * a.head_dim * sizeof(T);
-  if (a.n < 2048 || (a.n >= 16384 && row >= 10 << 10))
-    r.tokens = 1;
-  else
-    r.tokens = a.n >= 8192 && row < 6 << 10 ? kRopeTokens : 2;
+  r.tokens = rope_tokens(a.n, (size_t)heads * a.head_dim * sizeof(T));
   switch (a.head_dim) {
     case 64: return rope_at<T, 64>(r, s);
     case 128: return rope_at<T, 128>(r, s);

@@ -1,0 +1,36 @@
+"""Launch rules of the observation context's operators, on the host: the plan functions are C++
+symbols of the library; calling them needs no GPU."""
+import ctypes
+
+import pytest
+
+from paper_2608_27384_amd import flashvla as fvb
+
+
+def rope_tokens(n, row):
+    f = getattr(fvb.lib(), "_ZN2fv11rope_tokensEim")
+    f.restype, f.argtypes = ctypes.c_int, [ctypes.c_int, ctypes.c_size_t]
+    return f(n, row)
+
+
+# bytes of a token that are rotated or stored: one head of 64 in bf16 to 3072 of 256 in fp32
+ROWS = [128 << i for i in range(15)] + [(6 << 10) - 16, 6 << 10, (10 << 10) - 16, 10 << 10, 12 << 10, 3 << 20]
+COUNTS = [1, 2047, 2048, 16384] + [n + d for n in (1 << 23, 1 << 24, 1 << 25, 1 << 26) for d in (-1, 0, 1)]
+
+
+@pytest.mark.parametrize("n", [n for n in COUNTS if n <= 1 << 26])
+def test_rotary_grids_are_launches(n):
+    """Every count of tokens that is taken has a grid of less than 2^32 threads of 256 a workgroup,
+    which shares its angles among no more than 8 tokens."""
+    for row in ROWS:
+        t = rope_tokens(n, row)
+        assert 1 <= t <= 8
+        assert -(-n // t) * 256 < 1 << 32, (row, t)
+
+
+# (tokens, bytes of one, tokens a workgroup of the fastest)
+@pytest.mark.parametrize("n,row,tokens", [
+    (64, 5120, 1), (4096, 5120, 2), (32768, 5120, 8), (32768, 1536, 8), (8192, 12288, 2),
+    (32768, 12288, 1)])
+def test_rotary_tokens_that_were_faster(n, row, tokens):
+    assert rope_tokens(n, row) == tokens
