@@ -481,7 +481,8 @@ typedef struct {
  *  cache     the pages, or NULL: rotate only (then seqs, at and v are not read)
  * len is neither read nor changed; fv_pages_grow makes room beforehand.
  * q_out may be q and k_out may be k (same leading dimension); otherwise outputs
- * and inputs must not overlap.  n = 0 does nothing; n is at most 2^26.
+ * must not overlap each other, inputs that the call reads, or the layer's pages.
+ * n = 0 does nothing; n is at most 2^26.
  * Errors: FV_ERR_INVALID_ARG, FV_ERR_HIP.
  */
 typedef struct {
@@ -535,8 +536,8 @@ fv_status fv_prompt_attention(const fv_prompt_args *args, void *stream);
  *  work     fv_paged_attention_workspace bytes, overwritten (calls that may run
  *           at the same time need one each); NULL where that is 0
  * Rounding as in fv_prompt_attention; the result does not depend on the other
- * rows' lengths.  out must not overlap q.  n is at most 65536, n * n_q_heads at
- * most 2^22.
+ * rows' lengths.  out must not overlap q, work none of the other operands, and
+ * neither the layer's pages.  n is at most 65536, n * n_q_heads at most 2^22.
  * Errors: FV_ERR_INVALID_ARG, FV_ERR_HIP.
  */
 typedef struct {
@@ -584,7 +585,8 @@ fv_status fv_paged_attention(const fv_paged_args *args, const fv_pages *cache, v
  *                    entry i is position r of seqs[i], for r < min(len, ld); other
  *                    rows, those on table entries that are no page and the entries
  *                    whose seqs is out of range are left as they were.  A sequence
- *                    may occur several times; n <= 65536.
+ *                    may occur several times; n <= 65536.  k_out and v_out must not
+ *                    overlap each other or the cache's pages.
  * FV_PAGES_FULL: fewer free pages than the call needs.
  * Errors: FV_ERR_INVALID_ARG, FV_ERR_HIP.
  */

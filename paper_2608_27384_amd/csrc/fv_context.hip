@@ -94,6 +94,25 @@ void apart(const Span& a, const Span& b, const char* what) {
   bad(std::string(what) + " must not overlap");
 }
 
+// One run of `n` times `bytes` bytes (a size past 64 bits reaches the end of memory).
+Span run_of(const void* p, size_t n, size_t bytes) {
+  const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
+  uintptr_t size, hi;
+  if (__builtin_mul_overflow(n, bytes, &size) || __builtin_add_overflow(lo, size, &hi)) {
+    hi = UINTPTR_MAX;
+    size = hi - lo;
+  }
+  return Span{lo, hi, size, size};
+}
+// The pages of a layer in the pool p, and those of all layers.
+size_t layer_bytes(const fv_pages& c) {
+  return page_row(c.n_pages, c.n_kv_heads, 0, c.page_len) * c.head_dim * type_size(c.dtype);
+}
+Span layer_of(const void* p, const fv_pages& c, int layer) {
+  return run_of(static_cast<const char*>(p) + layer * layer_bytes(c), 1, layer_bytes(c));
+}
+Span pool_of(const void* p, const fv_pages& c) { return run_of(p, c.n_layers, layer_bytes(c)); }
+
 // A launch holds less than 2^32 threads in x and 2^16 workgroups in y and z.  The bounds of n,
 // n * heads and n_seqs * heads in the calls below keep x under that: the most are the 256
 // threads of 2^23 + 2^22 row tiles and spare slots of prompt attention, the 512 of 2^22 rows
@@ -177,21 +196,26 @@ fv_status fv_rope_append(const fv_rope_args* a, const fv_pages* c, void* stream)
     const Span k = operand(a->k, a->n, a->ldk, rk, e, "k");
     const Span v = c ? operand(a->v, a->n, a->ldv, rk, e, "v") : Span{};
     const Span qo = operand(a->q_out, a->n, a->ldq_out, rq, e, "q_out");
+    // an output may be its own input, and nothing else that the call reads or writes
     const bool q_in_place = a->q_out == a->q && a->ldq_out == a->ldq;
-    if (!q_in_place) {
-      apart(qo, q, "q_out and q");
-      apart(qo, k, "q_out and k");
-      apart(qo, v, "q_out and v");
-    }
+    if (!q_in_place) apart(qo, q, "q_out and q");
+    if (!q_in_place || c || a->k_out) apart(qo, k, "q_out and k");
+    apart(qo, v, "q_out and v");
+    Span ko;
     if (a->k_out) {
-      const Span ko = operand(a->k_out, a->n, a->ldk_out, rk, e, "k_out");
-      const bool k_in_place = a->k_out == a->k && a->ldk_out == a->ldk;
-      if (!k_in_place) {
-        apart(ko, q, "k_out and q");
-        apart(ko, k, "k_out and k");
-        apart(ko, v, "k_out and v");
+      ko = operand(a->k_out, a->n, a->ldk_out, rk, e, "k_out");
+      if (!(a->k_out == a->k && a->ldk_out == a->ldk)) apart(ko, k, "k_out and k");
+      apart(ko, q, "k_out and q");
+      apart(ko, v, "k_out and v");
+      apart(ko, qo, "k_out and q_out");
+    }
+    if (c) {
+      const Span pk = layer_of(c->k, *c, a->layer), pv = layer_of(c->v, *c, a->layer);
+      apart(pk, pv, "cache k and v");
+      for (const Span& p : {pk, pv}) {
+        apart(qo, p, "q_out and the cache's pages");
+        apart(ko, p, "k_out and the cache's pages");
       }
-      if (!(q_in_place && k_in_place)) apart(ko, qo, "k_out and q_out");
     }
     aligned(a->pos, 4, "pos");
     if (c) {
@@ -256,8 +280,12 @@ fv_status fv_paged_attention(const fv_paged_args* a, const fv_pages* c, void* st
     if (a->n == 0) return;
     const size_t e = type_size(c->dtype);
     const int row = a->n_q_heads * c->head_dim;
-    apart(operand(a->out, a->n, a->ldo, row, e, "out"), operand(a->q, a->n, a->ldq, row, e, "q"),
-          "out and q");
+    const Span out = operand(a->out, a->n, a->ldo, row, e, "out");
+    const Span q = operand(a->q, a->n, a->ldq, row, e, "q");
+    const Span pk = layer_of(c->k, *c, a->layer), pv = layer_of(c->v, *c, a->layer);
+    apart(out, q, "out and q");
+    apart(out, pk, "out and the cache's pages");
+    apart(out, pv, "out and the cache's pages");
     aligned(a->seqs, 4, "seqs");
     const PagedPlan p = paged_plan(*a, *c);
     if (p.work_bytes) {
@@ -265,6 +293,11 @@ fv_status fv_paged_attention(const fv_paged_args* a, const fv_pages* c, void* st
       if (a->work_bytes < p.work_bytes)
         bad("work holds " + std::to_string(a->work_bytes) + " bytes, " +
             std::to_string(p.work_bytes) + " are needed");
+      const Span w = run_of(a->work, 1, p.work_bytes);
+      apart(w, out, "work and out");
+      apart(w, q, "work and q");
+      apart(w, pk, "work and the cache's pages");
+      apart(w, pv, "work and the cache's pages");
     }
     hipStream_t s = static_cast<hipStream_t>(stream);
     OnStream on(s);
@@ -346,6 +379,15 @@ fv_status fv_pages_gather(const fv_pages* c, const int32_t* seqs, int32_t n, int
     aligned(seqs, 4, "seqs");
     aligned(k_out, 16, "k_out");
     aligned(v_out, 16, "v_out");
+    // bytes of a row, of all heads: at most 2^20
+    const size_t row = (size_t)c->n_kv_heads * c->head_dim * type_size(c->dtype);
+    const size_t rows = (size_t)c->n_layers * n * ld;
+    const Span ko = run_of(k_out, rows, row), vo = run_of(v_out, rows, row);
+    apart(ko, vo, "k_out and v_out");
+    for (const void* pool : {c->k, c->v}) {
+      apart(ko, pool_of(pool, *c), "k_out and the cache's pages");
+      apart(vo, pool_of(pool, *c), "v_out and the cache's pages");
+    }
     hipStream_t s = static_cast<hipStream_t>(stream);
     OnStream on(s);
     launch_pages_gather(*c, seqs, n, ld, k_out, v_out, s);

@@ -251,3 +251,66 @@ def test_binding_refuses_a_cache_elsewhere():
     seqs, pos = (torch.empty(s, dtype=torch.int32, device="meta") for s in ((3,), (1, 3)))
     with pytest.raises(fvb.FlashVLAError, match="the cache on cpu"):
         c.append(0, q, k, k, pos, seqs, seqs, (32,))
+
+
+# Where the operands of rope_args begin; its rows of 256 (queries) and 128 (keys and values) bf16
+Q, K, V, POOL = P, P << 1, P << 2, P << 6
+
+
+@pytest.mark.parametrize("kw", [
+    # queries in place, in a matrix that keys or values have a head of as well
+    dict(q_out=Q, k=Q + 384), dict(q_out=Q, v=Q + 384), dict(q_out=Q, k=Q), dict(q_out=Q, k=Q + 384, k_out=None),
+    # keys in place
+    dict(k_out=K, q=K), dict(k_out=K, v=K + 128), dict(k_out=K, v=K),
+    # both in place
+    dict(q_out=Q, k=Q + 384, k_out=Q + 384), dict(q_out=Q, k=Q, k_out=Q),
+    # columns of one packed matrix, the keys' one head too early
+    dict(q_out=Q, ldq=512, ldq_out=512, k=Q + 384, k_out=Q + 384, ldk=512, ldk_out=512, v=Q + 768, ldv=512)],
+    ids=str)
+def test_rotation_in_place_over_other_operands(kw):
+    a = rope_args(**kw)
+    refused(fvb.lib().fv_rope_append(ctypes.byref(a), ctypes.byref(cache(k=POOL, v=POOL << 1)), None), "overlap")
+
+
+def test_rotation_in_place_without_a_cache():
+    a = rope_args(q_out=Q, k=Q + 384)
+    refused(fvb.lib().fv_rope_append(ctypes.byref(a), None, None), "overlap")
+
+
+# A layer of cache() has 10 pages of 2 heads, 16 rows of 64: 40960 bytes
+LAYER = 10 * 2 * 16 * 64 * 2
+
+
+@pytest.mark.parametrize("pool", ["k", "v"])
+def test_outputs_in_the_pages(pool):
+    L, ref = fvb.lib(), ctypes.byref
+    n = ctypes.c_size_t()
+    for layer, at in ((0, 0), (1, LAYER), (1, 2 * LAYER - 16)):
+        inside = POOL + at
+        c = cache(k=POOL << 1, v=POOL << 1)
+        setattr(c, pool, POOL)
+        for kw in (dict(q_out=inside), dict(k_out=inside)):
+            refused(L.fv_rope_append(ref(rope_args(layer=layer, **kw)), ref(c), None), "pages")
+        refused(L.fv_paged_attention(ref(paged_args(out=inside, layer=layer)), ref(c), None), "pages")
+        for a, b in ((inside, P), (P, inside)):
+            refused(L.fv_pages_gather(ref(c), P, 1, 5, a, b, None), "pages")
+    # keys and values in one pool
+    refused(L.fv_rope_append(ref(rope_args()), ref(cache(k=POOL, v=POOL)), None), "cache k and v")
+
+
+def test_workspace_over_other_operands():
+    L, ref = fvb.lib(), ctypes.byref
+    c, n = cache(max_pages=4000, k=POOL, v=POOL << 1), ctypes.c_size_t()
+    assert L.fv_paged_attention_workspace(ref(paged_args()), ref(c), ref(n)) == 0
+    for work in (P, P << 1, POOL - 16, (POOL << 1) + LAYER - 16):
+        refused(L.fv_paged_attention(ref(paged_args(work=work, work_bytes=n.value)), ref(c), None), "work")
+
+
+def test_gathered_keys_over_gathered_values():
+    L, c = fvb.lib(), cache(k=POOL, v=POOL << 1)
+    out = 2 * 3 * 5 * 2 * 64 * 2  # bytes of 2 layers, 3 entries of 5 rows, 2 heads of 64
+    for k, v in ((P, P), (P, P + out - 16), (P + out - 16, P)):
+        refused(L.fv_pages_gather(ctypes.byref(c), P, 3, 5, k, v, None), "overlap")
+    # sizes that 64 bits do not hold
+    huge = cache(n_layers=1024, n_kv_heads=1024, head_dim=256, dtype=fvb.FV_FP32, k=POOL, v=POOL)
+    refused(L.fv_pages_gather(ctypes.byref(huge), P, 65536, (1 << 31) - 1, P, P << 1, None), "overlap")
