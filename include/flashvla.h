@@ -579,7 +579,7 @@ fv_status fv_paged_attention(const fv_paged_args *args, const fv_pages *cache, v
  *                    i-th lowest page in use from u on moves to the i-th lowest free
  *                    page below u, contents, holders and table entries.  Writes u to
  *                    `used` (int32 in device memory).  Moved-from pages keep their
- *                    contents.
+ *                    contents, entries on pages that nobody holds their numbers.
  *  fv_pages_gather   copies sequences out, dense, as fv_set_prefix takes them:
  *                    k_out, v_out [n_layers][n][ld][n_kv_heads][head_dim]; row r of
  *                    entry i is position r of seqs[i], for r < min(len, ld); other

@@ -513,8 +513,9 @@ __global__ __launch_bounds__(256) void free_apply_kernel(fv_pages c, const int* 
   if (threadIdx.x == 0) c.len[s] = 0;
 }
 
-// Workspace: [0] moves, [1] pages in use; A[i] <- B[i] are the moves and C[B[i]] =
-// A[i] the new number of a page that moves.
+// Workspace: [0] moves, [1] pages in use; A[i] <- B[i] are the moves and C[B[i]] = i.
+// C is written for the pages that move and no others: an entry of it counts where B
+// says that it is that page's.
 __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(fv_pages c, int* used,
                                                                     int* work, int list) {
   __shared__ PlanShared sh;
@@ -562,7 +563,7 @@ __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(fv_pages c, 
   __syncthreads();  // the lists are complete; holes == movers
   for (int i = threadIdx.x; i < movers; i += kPlanThreads) {
     const int src = B[i], dst = A[i];
-    C[src] = dst;
+    C[src] = i;
     c.refs[dst] = c.refs[src];
     c.refs[src] = 0;
   }
@@ -583,13 +584,15 @@ __global__ __launch_bounds__(256) void compact_apply_kernel(fv_pages c, const in
   const int* A = work + kPagesHeader;
   if (blockIdx.y == 0) {
     const int u = work[1];
-    const int* C = A + 2 * (size_t)list;
+    const int *B = A + list, *C = B + list;
     for (int s = blockIdx.x; s < c.max_seqs; s += gridDim.x) {
       int* row = c.table + (size_t)s * c.max_pages;
       const int pages = pages_of(min(max(c.len[s], 0), c.max_pages * c.page_len), c.page_len);
       for (int j = tid; j < pages; j += 256) {
         const int p = row[j];
-        if (p >= u && is_page(c, p)) row[j] = C[p];
+        if (p < u || !is_page(c, p)) continue;
+        const int i = C[p];
+        if (i >= 0 && i < moves && B[i] == p) row[j] = A[i];  // a page that nobody holds stays
       }
     }
     return;

@@ -480,3 +480,29 @@ def test_captured_token_step(dtype):
         for l in range(L):
             assert a["out"][l].equal(b["out"][l]) and (a["out"][l][4] == 0).all()
     assert runs[0].length.tolist() == [21, 35, 36, 0, 51, 40]
+
+
+@pytest.mark.parametrize("poison", [0, 1, 7, 15, 39, -1, 1 << 30])
+@pytest.mark.parametrize("refs", [0, -1])
+def test_compaction_leaves_entries_on_pages_that_nobody_holds(refs, poison):
+    """A live entry whose page has no holder, past the pages in use, keeps its number whatever an
+    earlier call left in the workspace; the others move."""
+    import ctypes
+    from paper_2608_27384_amd import flashvla as fvb
+    torch = cu.torch_mod()
+    cache, model = fresh(40, 4, 12)
+    for s, n in ((0, 160), (1, 80), (2, 76)):
+        assert cache.grow(cu.ints([s]), cu.ints([n])).item() == model.grow([s], [n]) == 0
+    assert cache.free(cu.ints([0])).item() == model.free([0]) == 0
+    lost = int(model.table[1, 2])
+    cache.refs[lost] = refs
+    model.refs[lost] = 0
+    want = model.compact()[0]
+    model.refs[lost] = refs
+    work = torch.full((cache.work_bytes // 4,), poison, dtype=torch.int32, device="cuda")
+    used = torch.empty(1, dtype=torch.int32, device="cuda")
+    st = fvb.lib().fv_pages_compact(ctypes.byref(cache.c), used.data_ptr(), work.data_ptr(),
+                                    torch.cuda.current_stream().cuda_stream)
+    assert st == 0 and used.item() == want == 9
+    assert cache.table[1, 2].item() == lost == 12
+    same(cache, model)
