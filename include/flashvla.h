@@ -535,7 +535,8 @@ fv_status fv_prompt_attention(const fv_prompt_args *args, void *stream);
  *  scale    as above
  *  work     fv_paged_attention_workspace bytes, overwritten (calls that may run
  *           at the same time need one each); NULL where that is 0
- * Rounding as in fv_prompt_attention; the result does not depend on the other
+ * Scores, softmax and sums are fp32; in bf16 the probabilities meet the values in
+ * two parts of bf16, together 16 bits.  The result does not depend on the other
  * rows' lengths.  out must not overlap q, work none of the other operands, and
  * neither the layer's pages.  n is at most 65536, n * n_q_heads at most 2^22.
  * Errors: FV_ERR_INVALID_ARG, FV_ERR_HIP.

@@ -15,6 +15,13 @@
 // its own 8 keys, one 256-byte row per 16 lanes, and turns the 8x8 block over in
 // registers (32 byte permutes, nothing beside the loads); which element of the
 // head a matrix row stands for is free, and chosen so that this works out.
+// bf16 values meet each probability in two parts, its upper 8 bits and what they
+// leave, so that 16 bits count (2^-16 of it is lost, 2^-8 with one part: the error
+// against 64 bits was 1.2 to 1.3 times that of exact probabilities).  A lowest bit
+// that is always set keeps the second part above zero, where an infinite value would
+// lose its infinity to 0 * inf.  Half as many products again, us with one part and with
+// two: 64 rows of 816 keys 14.3 and 14.8, 32 of 1000 to 4000 23.9 and 24.3 (heads 8/1 of
+// 256), 192 of 1 to 8191 522 and 522 (32/8 of 128).
 //
 // Measured (a read of memory alone reaches 6.2 TB/s): 192 rows of 1 to 8191 keys, heads
 // 32/8 of 128, 524 us (6.2 TB/s); 192 of 1 to 16000, 8/1 of 256, 290 us (5.5); 64 of 816,
@@ -42,6 +49,7 @@ struct PagedCall {
   float* part;  // [n][n_chunks][heads][DH] sums, then [n][n_chunks][heads][2] maximum and sum
   float* stat;
   int ldq, ldo, n, heads, n_kv, group, q_tiles, page_len, n_pages, max_seqs, max_pages;
+  uint32_t per_page;  // 2^31 over a page's runs of 16 rows, rounded up
   int chunk, n_chunks;
   float scale;  // of the scores, in log2 units
 };
@@ -144,12 +152,19 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_kernel(PagedCall a)
   if (s < 0 || s >= a.max_seqs) return;
   const int k0 = ch * a.chunk;
   const int* table = a.table + (size_t)s * a.max_pages;
+  // Page number of the 16 keys from `key` on, a multiple of 16 below 2^25: with m = page_len / 16
+  // up to 16, the rounded up quotient is exact while key / 16 * (m - 1) stays below 2^31.
+  auto page_of = [&](int key) __attribute__((always_inline)) { return (int)__umulhi(key >> 3, a.per_page); };
   auto page_at = [&](int key) __attribute__((always_inline)) {
-    const int p = key / a.page_len;
+    const int p = page_of(key);
     return p < a.max_pages ? table[p] : -1;
   };
+  // First key of the half that a lane looks up (below), past that of its wave's tile `base`; in
+  // one register, which the compiler would make two.
+  int ahead = kPagedWaves * (lane / NH) * KT + 16 * (lane % NH);
+  asm volatile("" : "+v"(ahead));
   // the first page numbers are fetched together with the length
-  int page = page_at(k0 + (wave + kPagedWaves * (lane / NH)) * KT + 16 * (lane % NH));
+  int page = page_at(k0 + wave * KT + ahead);
   const int len = length_of(a, s);
   const int chunks = chunks_of(len, a.chunk, a.n_chunks);
   if (ch >= chunks && ch > 0) return;
@@ -179,19 +194,18 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_kernel(PagedCall a)
   // Page numbers 64 halves at a time: lane i holds half i % NH of the wave's tile base + i / NH.
   constexpr int GO = 64 / NH;
   for (int base = wave; base < tiles; base += kPagedWaves * GO) {
-    const int myKey = k0 + (base + kPagedWaves * (lane / NH)) * KT + 16 * (lane % NH);
+    const int myKey = k0 + base * KT + ahead;
     if (base != wave) page = page_at(myKey);
-    if (myKey >= k1 || page < 0 || page >= a.n_pages) page = -1;
-    const int off = page >= 0 ? myKey % a.page_len : 0;
+    // page and row / 16 in one register (a page has at most 256 rows), -1: no keys
+    const int half = myKey >= k1 || page < 0 || page >= a.n_pages ? -1 : page << 4 | (myKey - page_of(myKey) * a.page_len) >> 4;
     const int here = min(GO, (tiles - base + kPagedWaves - 1) / kPagedWaves);
     // first rows of a tile's halves, and how many of their keys are there
     auto rows = [&](int it, const T* pool, const T* (&row)[NH], int (&left)[NH]) __attribute__((always_inline)) {
 #pragma unroll
       for (int h = 0; h < NH; ++h) {
-        const int pg = __builtin_amdgcn_readlane(page, it * NH + h);
-        const int of = __builtin_amdgcn_readlane(off, it * NH + h);
-        left[h] = pg < 0 ? 0 : min(16, k1 - (k0 + (base + kPagedWaves * it) * KT + 16 * h));
-        row[h] = pool + (page_row(pg < 0 ? 0 : pg, a.n_kv, kh, a.page_len) + of) * DH;
+        const int at = __builtin_amdgcn_readlane(half, it * NH + h);
+        left[h] = at < 0 ? 0 : min(16, k1 - (k0 + (base + kPagedWaves * it) * KT + 16 * h));
+        row[h] = pool + (page_row(max(at, 0) >> 4, a.n_kv, kh, a.page_len) + 16 * (max(at, 0) & 15)) * DH;
       }
     };
     u32x4 kf[NH][KB];
@@ -257,18 +271,20 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_kernel(PagedCall a)
         for (int t = 0; t < NT; ++t) o[t] *= f;
       }
       const float ref = m == -INFINITY ? 0.f : m;
-      u32x4 pf;
+      u32x4 pf, rest;
       if constexpr (sizeof(T) == 2) {
-        u16x8 pb;
+        u16x8 pb, rb;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const float p = __builtin_amdgcn_exp2f(sc[h][r] - ref);
-            l += p;
-            pb[4 * h + r] = f32_to_bf16(p);
+            const uint32_t p = __float_as_uint(__builtin_amdgcn_exp2f(sc[h][r] - ref)) | 1;
+            l += __uint_as_float(p);
+            pb[4 * h + r] = (bf16_t)(p >> 16);
+            rb[4 * h + r] = f32_to_bf16(__uint_as_float(p) - __uint_as_float(p & 0xffff0000u));
           }
         pf = __builtin_bit_cast(u32x4, pb);
+        rest = __builtin_bit_cast(u32x4, rb);
       } else {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
@@ -278,7 +294,11 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_kernel(PagedCall a)
         }
       }
 #pragma unroll
-      for (int t = 0; t < NT; ++t) o[t] = mma64(vt.operand(t), pf, o[t], T{});
+      for (int t = 0; t < NT; ++t) {
+        const u32x4 v = vt.operand(t);
+        o[t] = mma64(v, pf, o[t], T{});
+        if constexpr (sizeof(T) == 2) o[t] = mma64(v, rest, o[t], T{});
+      }
     }
   }
 
@@ -484,6 +504,7 @@ void launch_paged(const fv_paged_args& x, const fv_pages& c, const PagedPlan& p,
   a.group = x.n_q_heads / c.n_kv_heads;
   a.q_tiles = (a.group + 15) / 16;
   a.page_len = c.page_len;
+  a.per_page = (uint32_t)(((1ull << 31) + c.page_len / 16 - 1) / (c.page_len / 16));
   a.n_pages = c.n_pages;
   a.max_seqs = c.max_seqs;
   a.max_pages = c.max_pages;

@@ -71,6 +71,19 @@ def check_attention(got, ref, dtype):
                                  float((got.double() - out).abs().max()))
 
 
+def check_attention_wide(got, ref, dtype):
+    """The same where the probabilities of bf16 values are kept in two parts of bf16: of a
+    probability in [1, 2) the first leaves less than 2^-7, which the second holds in steps of
+    2^-15 at most, so half a step is 2^-16; as much of every other, by its exponent: 2^-16 A."""
+    out, size, fp32 = ref
+    tol = EPS[dtype] * out.abs() + fp32 * (1 + EPS[dtype]) + 1e-37
+    if dtype == "bf16":
+        tol = tol + 2.0 ** -16 * size * (1 + EPS["bf16"])
+    bad = ~((got.double() - out).abs() <= tol)
+    assert not bool(bad.any()), (int(bad.sum()), bad.nonzero()[:4].tolist(),
+                                 float((got.double() - out).abs().max()))
+
+
 def rotate(x, pos, sections, theta):
     """x [n, H, D] at positions pos [axes][n]: the 64-bit result, and its own size."""
     torch = torch_mod()

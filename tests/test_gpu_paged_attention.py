@@ -224,3 +224,39 @@ def test_more_than_the_caches_hold(shape):
         out = torch.full_like(q, 7.0)
         cache.attend(0, q, cu.ints(range(len(LENS))), out, max_len=max_len)
         check(shape, cache, table, LENS, q, out, 0)
+
+
+@pytest.mark.parametrize("max_len", [0, 2049])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_probabilities_keep_their_bits(shape, max_len):
+    """bf16 values meet probabilities of 16 bits, not of 8."""
+    torch = cu.torch_mod()
+    cache, q, table = make(shape, LENS)
+    out = torch.full_like(q, 7.0)
+    cache.attend(1, q, cu.ints(np.arange(len(LENS))), out, max_len=max_len)
+    for i, n in enumerate(LENS):
+        k, v = rows(cache, table, i, n, 1)
+        cu.check_attention_wide(out[i:i + 1], cu.attention(q[i:i + 1], k, v, [n]), shape[0])
+
+
+@pytest.mark.parametrize("bad", [np.inf, -np.inf, np.nan])
+@pytest.mark.parametrize("shape", [SHAPES[0], SHAPES[2], SHAPES[5]], ids=str)
+def test_values_that_are_not_finite(shape, bad):
+    """An infinite value of a key that is seen gives that infinity, whatever bits its probability
+    has: all alike (scores of zero) or spread."""
+    torch = cu.torch_mod()
+    lens = [1, 40, 700, 2049]
+    for zero in (True, False):
+        cache, q, table = make(shape, lens, layers=1)
+        if zero:
+            q.zero_()
+        for b, n in enumerate(lens):
+            for at, d in ((0, 3), (n - 1, 5), (n // 2, 7)):
+                cache.v[0, table[b, at // 16], :, at % 16, d] = bad
+        out = torch.full_like(q, 7.0)
+        cache.attend(0, q, cu.ints(range(len(lens))), out)
+        hit = torch.zeros(shape[3], dtype=torch.bool, device="cuda")
+        hit[[3, 5, 7]] = True
+        got = out[..., hit]
+        assert (got.isnan() if np.isnan(bad) else got == bad).all()
+        assert out[..., ~hit].isfinite().all()
