@@ -57,7 +57,7 @@ __device__ __forceinline__ void dma16(u32x4 src, const unsigned char* lds, int o
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(
                    __builtin_amdgcn_readfirstlane((int)to)),
                "v"(off), "s"(src)
-               : "memory");
+               : "m0", "memory");
 }
 
 // 32x32 products over two 16-byte pieces a row (one of each lane half).

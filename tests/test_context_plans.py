@@ -34,3 +34,16 @@ def test_rotary_grids_are_launches(n):
     (32768, 12288, 1)])
 def test_rotary_tokens_that_were_faster(n, row, tokens):
     assert rope_tokens(n, row) == tokens
+
+
+def test_assembly_names_the_registers_that_it_sets():
+    """The compiler keeps m0 over a block that does not say that it sets it."""
+    import os
+    import re
+    csrc = os.path.join(os.path.dirname(os.path.abspath(fvb.__file__)), "csrc")
+    blocks = []
+    for name in sorted(os.listdir(csrc)):
+        with open(os.path.join(csrc, name)) as f:
+            blocks += re.findall(r"asm volatile\(.*?\);", f.read(), re.S)
+    sets = [b for b in blocks if "_b32 m0" in b]
+    assert sets and all('"m0"' in b for b in sets)
