@@ -45,7 +45,8 @@ __device__ __forceinline__ u32x2 read_transposed(const unsigned char* p) {
 
 // A direct-to-LDS load (see lds_dma16) that the compiler does not know of: it waits
 // for all those it knows of before a transposing read, the next tile's among them.
-// Whoever reads the data waits for the loads itself.
+// Whoever reads the data waits for the loads itself.  The place in LDS goes by m0, an
+// operand, so that the compiler knows what that holds.
 __device__ __forceinline__ u32x4 dma_source(const void* base) {
   const uint64_t p = reinterpret_cast<uint64_t>(base);
   return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)p),
@@ -54,10 +55,10 @@ __device__ __forceinline__ u32x4 dma_source(const void* base) {
 __device__ __forceinline__ void dma16(u32x4 src, const unsigned char* lds, int off) {
   const uint32_t to = (uint32_t)reinterpret_cast<uintptr_t>(
       (const __attribute__((address_space(3))) unsigned char*)lds);
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(
+  asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(
                    __builtin_amdgcn_readfirstlane((int)to)),
                "v"(off), "s"(src)
-               : "m0", "memory");
+               : "memory");
 }
 
 // 32x32 products over two 16-byte pieces a row (one of each lane half).
