@@ -435,13 +435,14 @@ def _refuse(message: str):
     raise FlashVLAError(FV_ERR_INVALID_ARG, message)
 
 
-_torch = None
+_torch = _new_version = None
 
 
 def _tmod():
-    global _torch
+    global _torch, _new_version
     if _torch is None:
         import torch
+        _new_version = torch._C._increment_version
         _torch = torch
     return _torch
 
@@ -455,11 +456,12 @@ def _dtype(t, what: str) -> int:
     return FV_FP32
 
 
-def _rows(t, what: str, dtype, device, shape=None) -> int:
-    """Leading dimension of a [tokens, heads, head_dim] tensor whose heads lie side by side."""
+def _rows(t, what: str, dtype, gpu: int, shape=None) -> int:
+    """Leading dimension of a [tokens, heads, head_dim] tensor whose heads lie side by side.
+    gpu: the number of the call's GPU (-1: none, which the call refuses)."""
     got = t.shape
-    if t.dtype is not dtype or t.device != device:
-        _refuse(f"{what} must have dtype {dtype} on {device}")
+    if t.dtype is not dtype or t.get_device() != gpu:
+        _refuse(f"{what} must have dtype {dtype} on the call's GPU: {t.dtype} on {t.device}")
     if len(got) != 3 or (shape is not None and got != shape):
         _refuse(f"{what} has shape {tuple(got)}" + (f", not {tuple(shape)}" if shape else ""))
     n, h, d = got
@@ -471,13 +473,27 @@ def _rows(t, what: str, dtype, device, shape=None) -> int:
     return ld if n > 1 else h * d
 
 
-def _int32(t, what: str, device, shape=None) -> int:
+def _int32(t, what: str, gpu: int, shape=None) -> int:
     """Pointer of a dense int32 tensor."""
-    if t.dtype is not _tmod().int32 or t.device != device or not t.is_contiguous():
-        _refuse(f"{what} must be a contiguous int32 tensor on {device}")
+    if t.dtype is not _torch.int32 or t.get_device() != gpu or not t.is_contiguous():
+        _refuse(f"{what} must be contiguous int32 on the call's GPU: {t.dtype} on {t.device}")
     if shape is not None and t.shape != shape:
         _refuse(f"{what} has shape {tuple(t.shape)}, not {tuple(shape)}")
     return t.data_ptr()
+
+
+def _no_gradient(*tensors) -> None:
+    """Refuses, in grad mode, tensors that a gradient would have to pass: the calls form none."""
+    if _torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                _refuse("a tensor requires a gradient, which the call does not form "
+                        "(torch.no_grad() takes it)")
+
+
+def _wrote(*tensors) -> None:
+    """What autograd kept of these tensors for a backward pass is no longer there."""
+    _new_version(tensors)
 
 
 class _On:
@@ -524,11 +540,13 @@ def prompt_attention(q, k, v, cu_q, cu_k, out, causal: bool = True, scale: Optio
                      stream=None) -> None:
     """fv_prompt_attention on torch tensors: q and out [tokens, heads, head_dim], k and v
     [keys, kv heads, head_dim] (rows may be strided), cu_q and cu_k int32 [prompts + 1].
-    `scale` defaults to 1/sqrt(head_dim)."""
-    dtype, t, dev, shape = _dtype(q, "q"), q.dtype, q.device, q.shape
-    ldq, ldo = _rows(q, "q", t, dev), _rows(out, "out", t, dev, shape)
-    ldk = _rows(k, "k", t, dev)
-    ldv = _rows(v, "v", t, dev, k.shape)
+    `scale` defaults to 1/sqrt(head_dim).  As every call here it forms no gradient: in grad
+    mode tensors that require one are refused, and what is written counts as modified."""
+    dtype, t, gpu, shape = _dtype(q, "q"), q.dtype, q.get_device(), q.shape
+    _no_gradient(q, k, v, out)
+    ldq, ldo = _rows(q, "q", t, gpu), _rows(out, "out", t, gpu, shape)
+    ldk = _rows(k, "k", t, gpu)
+    ldv = _rows(v, "v", t, gpu, k.shape)
     n_q, heads, dh = shape
     n_k, kv_heads, dk = k.shape
     if dk != dh:
@@ -537,11 +555,12 @@ def prompt_attention(q, k, v, cu_q, cu_k, out, causal: bool = True, scale: Optio
     if len(prompts) != 1 or prompts[0] < 1:
         _refuse("cu_q must have prompts + 1 entries")
     args = FvPromptArgs(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), ldq, ldk, ldv, ldo,
-                        _int32(cu_q, "cu_q", dev), _int32(cu_k, "cu_k", dev, prompts),
+                        _int32(cu_q, "cu_q", gpu), _int32(cu_k, "cu_k", gpu, prompts),
                         prompts[0] - 1, n_q, n_k, heads, kv_heads, dh, dtype, 1 if causal else 0,
                         dh ** -0.5 if scale is None else scale)
-    with _On(dev, stream) as on:
+    with _On(q.device, stream) as on:
         _check_context(lib().fv_prompt_attention(byref(args), on.raw), "fv_prompt_attention")
+    _wrote(out)
 
 
 def rope(q, k, pos, sections: Sequence[int], q_out, k_out=None, theta: float = 10000.0,
@@ -550,9 +569,10 @@ def rope(q, k, pos, sections: Sequence[int], q_out, k_out=None, theta: float = 1
     _rope(None, 0, q, k, None, pos, None, None, sections, theta, q_out, k_out, stream)
 
 
-def _rope(cache, layer, q, k, v, pos, seqs, at, sections, theta, q_out, k_out, stream) -> None:
-    dtype, t, dev = _dtype(q, "q"), q.dtype, q.device
-    ldq, ldk = _rows(q, "q", t, dev), _rows(k, "k", t, dev)
+def _rope(cache, layer, q, k, v, pos, seqs, at, sections, theta, q_out, k_out, stream, *pools) -> None:
+    dtype, t, gpu = _dtype(q, "q"), q.dtype, q.get_device()
+    _no_gradient(q, k, v, q_out, k_out)
+    ldq, ldk = _rows(q, "q", t, gpu), _rows(k, "k", t, gpu)
     n, heads, dh = q.shape
     nk, kv_heads, dk = k.shape
     if nk != n or dk != dh:
@@ -561,16 +581,17 @@ def _rope(cache, layer, q, k, v, pos, seqs, at, sections, theta, q_out, k_out, s
     if not 1 <= axes <= 4:
         _refuse("sections must have 1 to 4 entries")
     args = FvRopeArgs(q.data_ptr(), k.data_ptr(), _ptr(v), q_out.data_ptr(), _ptr(k_out), ldq, ldk,
-                      _rows(v, "v", t, dev, k.shape) if v is not None else 0,
-                      _rows(q_out, "q_out", t, dev, q.shape),
-                      _rows(k_out, "k_out", t, dev, k.shape) if k_out is not None else 0,
-                      _int32(pos, "pos", dev, (axes, n)),
-                      _int32(seqs, "seqs", dev, (n,)) if seqs is not None else None,
-                      _int32(at, "at", dev, (n,)) if at is not None else None, n, heads, kv_heads,
+                      _rows(v, "v", t, gpu, k.shape) if v is not None else 0,
+                      _rows(q_out, "q_out", t, gpu, q.shape),
+                      _rows(k_out, "k_out", t, gpu, k.shape) if k_out is not None else 0,
+                      _int32(pos, "pos", gpu, (axes, n)),
+                      _int32(seqs, "seqs", gpu, (n,)) if seqs is not None else None,
+                      _int32(at, "at", gpu, (n,)) if at is not None else None, n, heads, kv_heads,
                       dh, dtype, layer, axes, tuple(sections), theta)
-    with _On(dev, stream) as on:
+    with _On(q.device, stream) as on:
         _check_context(lib().fv_rope_append(byref(args), None if cache is None else byref(cache),
                                             on.raw), "fv_rope_append")
+    _wrote(q_out, *pools) if k_out is None else _wrote(q_out, k_out, *pools)
 
 
 class PageCache:
@@ -589,12 +610,13 @@ class PageCache:
         if table.dim() != 2:
             _refuse("table must be [sequences, pages of a sequence]")
         layers, pages, heads, page_len, dh = k.shape
-        dev = k.device
+        gpu = k.get_device()
+        _no_gradient(k, v)
         self.k, self.v, self.table, self.length, self.refs = k, v, table, length, refs
         self.c = FvPages(dtype, layers, heads, dh, page_len, pages, table.shape[0], table.shape[1],
-                         k.data_ptr(), v.data_ptr(), _int32(table, "table", dev),
-                         _int32(length, "length", dev, table.shape[:1]),
-                         _int32(refs, "refs", dev, (pages,)))
+                         k.data_ptr(), v.data_ptr(), _int32(table, "table", gpu),
+                         _int32(length, "length", gpu, table.shape[:1]),
+                         _int32(refs, "refs", gpu, (pages,)))
         need = c_size_t()
         _check_context(lib().fv_pages_workspace(byref(self.c), byref(need)), "PageCache")
         self.work_bytes = need.value  # of the upkeep's calls
@@ -621,20 +643,21 @@ class PageCache:
             _refuse(f"q is on {q.device}, the cache on {self.k.device}")
         self._layer(layer)
         _rope(self.c, layer, q, k, v, pos, seqs, at, sections, theta, q if q_out is None else q_out,
-              k_out, stream)
+              k_out, stream, self.k, self.v)
 
     def attend(self, layer: int, q, seqs, out, scale: Optional[float] = None, max_len: int = 0,
                stream=None) -> None:
         """fv_paged_attention: q and out [rows, heads, head_dim], seqs int32 [rows]."""
-        t, dev = self.k.dtype, self.k.device
-        ldq = _rows(q, "q", t, dev)
-        ldo = _rows(out, "out", t, dev, q.shape)
+        t, dev, gpu = self.k.dtype, self.k.device, self.k.get_device()
+        _no_gradient(q, out)
+        ldq = _rows(q, "q", t, gpu)
+        ldo = _rows(out, "out", t, gpu, q.shape)
         n, heads, dh = q.shape
         cache = byref(self.c)
         self._layer(layer)
         if dh != self.c.head_dim:
             _refuse(f"head_dim of q is {dh}, of the cache {self.c.head_dim}")
-        args = FvPagedArgs(q.data_ptr(), out.data_ptr(), ldq, ldo, _int32(seqs, "seqs", dev, (n,)), n,
+        args = FvPagedArgs(q.data_ptr(), out.data_ptr(), ldq, ldo, _int32(seqs, "seqs", gpu, (n,)), n,
                            heads, layer, max_len, dh ** -0.5 if scale is None else scale, None, 0)
         with _On(dev, stream) as on:
             need, L, a = c_size_t(), lib(), byref(args)
@@ -643,25 +666,30 @@ class PageCache:
                 work = _work(need.value, dev)
                 args.work, args.work_bytes = work.data_ptr(), need.value
             _check_context(L.fv_paged_attention(a, cache, on.raw), "fv_paged_attention")
+        _wrote(out)
 
     def _layer(self, layer: int) -> None:
         if not 0 <= layer < self.c.n_layers:
             _refuse(f"layer {layer} of {self.c.n_layers}")
 
-    def _upkeep(self, name: str, stream, *lists, status=None, work=True):
-        dev = self.k.device
+    def _upkeep(self, name: str, stream, *lists, status=None, work=True, pages=False):
+        dev, gpu = self.k.device, self.k.get_device()
         n = lists[0].shape[0] if lists else 0
-        args = [byref(self.c), *[_int32(t, name + " list", dev, (n,)) for t in lists]]
+        args = [byref(self.c), *[_int32(t, name + " list", gpu, (n,)) for t in lists]]
         if lists:
             args.append(n)
         with _On(dev, stream) as on:
             if status is None:
                 status = _tmod().empty(1, dtype=_tmod().int32, device=dev)
-            args.append(_int32(status, "status", dev, (1,)))
+            args.append(_int32(status, "status", gpu, (1,)))
             if work:
                 buf = _work(self.work_bytes, dev)
                 args.append(buf.data_ptr())
             _check_context(getattr(lib(), name)(*args, on.raw), name)
+        if pages:
+            _wrote(self.table, self.length, self.refs, status, self.k, self.v)
+        else:
+            _wrote(self.table, self.length, self.refs, status)
         return status
 
     def grow(self, seqs, add, status=None, stream=None):
@@ -670,7 +698,7 @@ class PageCache:
 
     def fork(self, parents, children, status=None, stream=None):
         """fv_pages_fork; returns the status tensor."""
-        return self._upkeep("fv_pages_fork", stream, parents, children, status=status)
+        return self._upkeep("fv_pages_fork", stream, parents, children, status=status, pages=True)
 
     def free(self, seqs, status=None, stream=None):
         """fv_pages_free; returns the status tensor."""
@@ -678,12 +706,13 @@ class PageCache:
 
     def compact(self, used=None, stream=None):
         """fv_pages_compact; returns the number of pages in use (int32 [1])."""
-        return self._upkeep("fv_pages_compact", stream, status=used)
+        return self._upkeep("fv_pages_compact", stream, status=used, pages=True)
 
     def gather(self, seqs, k_out, v_out, stream=None) -> None:
         """fv_pages_gather: k_out and v_out [layers, entries, ld, kv heads, head_dim], as
         Expert.set_prefix takes them."""
         c, dev = self.c, self.k.device
+        _no_gradient(k_out, v_out)
         for t, what in ((k_out, "k_out"), (v_out, "v_out")):
             if t.dim() != 5 or t.dtype != self.k.dtype or t.device != dev or not t.is_contiguous():
                 _refuse(f"{what} must be contiguous [layers, entries, ld, kv heads, head_dim]")
@@ -692,6 +721,8 @@ class PageCache:
         if k_out.shape != v_out.shape:
             _refuse("k_out and v_out must have the same shape")
         with _On(dev, stream) as on:
-            _check_context(lib().fv_pages_gather(byref(c), _int32(seqs, "seqs", dev, k_out.shape[1:2]),
-                                                 k_out.shape[1], k_out.shape[2], k_out.data_ptr(),
-                                                 v_out.data_ptr(), on.raw), "fv_pages_gather")
+            ids = _int32(seqs, "seqs", self.k.get_device(), k_out.shape[1:2])
+            _check_context(lib().fv_pages_gather(byref(c), ids, k_out.shape[1], k_out.shape[2],
+                                                 k_out.data_ptr(), v_out.data_ptr(), on.raw),
+                           "fv_pages_gather")
+        _wrote(k_out, v_out)

@@ -314,3 +314,37 @@ def test_gathered_keys_over_gathered_values():
     # sizes that 64 bits do not hold
     huge = cache(n_layers=1024, n_kv_heads=1024, head_dim=256, dtype=fvb.FV_FP32, k=POOL, v=POOL)
     refused(L.fv_pages_gather(ctypes.byref(huge), P, 65536, (1 << 31) - 1, P, P << 1, None), "overlap")
+
+
+def test_binding_refuses_what_would_need_a_gradient():
+    """The calls form none and write through pointers: in grad mode such tensors are refused, under
+    no_grad they are taken (and then refused for not being on a GPU)."""
+    torch = pytest.importorskip("torch")
+    pool, refs = torch.zeros(2, 10, 2, 16, 64), torch.zeros(10, dtype=torch.int32)
+    table, length = torch.zeros(4, 3, dtype=torch.int32), torch.zeros(4, dtype=torch.int32)
+    seqs, pos = torch.zeros(3, dtype=torch.int32), torch.zeros(1, 3, dtype=torch.int32)
+    cum = torch.tensor([0, 3], dtype=torch.int32)
+
+    def calls(i):
+        """Every call with its i-th floating tensor requiring a gradient."""
+        def t(j, *shape):
+            return torch.zeros(*shape, requires_grad=i == j)
+        c = fvb.PageCache(t(9, 2, 10, 2, 16, 64), t(9, 2, 10, 2, 16, 64), table, length, refs)
+        yield (0, 1), lambda: (fvb.PageCache(t(0, 2, 10, 2, 16, 64), t(1, 2, 10, 2, 16, 64), table, length, refs),
+                               c.attend(0, t(9, 3, 4, 64), seqs, t(9, 3, 4, 64)))
+        yield (0, 1, 2, 3), lambda: fvb.prompt_attention(t(0, 3, 4, 64), t(1, 3, 2, 64), t(2, 3, 2, 64), cum,
+                                                         cum, t(3, 3, 4, 64))
+        yield (0, 1, 2, 3), lambda: fvb.rope(t(0, 3, 4, 64), t(1, 3, 2, 64), pos, (32,), t(2, 3, 4, 64),
+                                             t(3, 3, 2, 64))
+        yield range(5), lambda: c.append(0, t(0, 3, 4, 64), t(1, 3, 2, 64), t(2, 3, 2, 64), pos, seqs, seqs,
+                                         (32,), q_out=t(3, 3, 4, 64), k_out=t(4, 3, 2, 64))
+        yield (0, 1), lambda: c.attend(0, t(0, 3, 4, 64), seqs, t(1, 3, 4, 64))
+        yield (0, 1), lambda: c.gather(seqs, t(0, 2, 3, 5, 2, 64), t(1, 2, 3, 5, 2, 64))
+
+    for i in range(5):
+        for takes, call in calls(i):
+            with pytest.raises(fvb.FlashVLAError, match="gradient" if i in takes else "GPU") as e:
+                call()
+            assert e.value.status == fvb.FV_ERR_INVALID_ARG
+            with torch.no_grad(), pytest.raises(fvb.FlashVLAError, match="on a GPU"):
+                call()

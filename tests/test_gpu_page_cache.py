@@ -506,3 +506,45 @@ def test_compaction_leaves_entries_on_pages_that_nobody_holds(refs, poison):
     assert st == 0 and used.item() == want == 9
     assert cache.table[1, 2].item() == lost == 12
     same(cache, model)
+
+
+def test_written_tensors_move_their_versions():
+    """A tensor that autograd keeps for a backward pass and a call then overwrites is noticed."""
+    torch = cu.torch_mod()
+    from paper_2608_27384_amd.flashvla import prompt_attention, rope
+    cache, _ = fresh(20, 4, 4)
+    q, k, v = (cu.randn("bf16", i, 5, h, 64) for i, h in enumerate((4, 2, 2)))
+    out, ko = torch.empty_like(q), torch.empty_like(k)
+    at, seqs, cum = cu.ints(range(5)), cu.ints([0] * 5), cu.ints([0, 5])
+    kd, vd = (torch.empty(2, 1, 5, 2, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    st = torch.empty(1, dtype=torch.int32, device="cuda")
+    books, pools = [cache.table, cache.length, cache.refs, st], [cache.k, cache.v]
+    every = books + pools + [q, k, v, out, ko, kd, vd, at, seqs, cum]
+
+    def moved(call):
+        before = [t._version for t in every]
+        call()
+        return [t for t, b in zip(every, before) if t._version != b]
+
+    def same(got, want):
+        assert [t.data_ptr() for t in got] == [t.data_ptr() for t in every if any(t is w for w in want)]
+
+    same(moved(lambda: cache.grow(cu.ints([0]), cu.ints([5]), st)), books)
+    same(moved(lambda: cache.append(0, q, k, v, at[None], seqs, at, (32,))), pools + [q])
+    same(moved(lambda: cache.append(1, q, k, v, at[None], seqs, at, (32,), q_out=out, k_out=ko)), pools + [out, ko])
+    same(moved(lambda: rope(q, k, at[None], (32,), out)), [out])
+    same(moved(lambda: prompt_attention(q, k, v, cum, cum, out)), [out])
+    same(moved(lambda: cache.attend(0, q, seqs, out)), [out])
+    same(moved(lambda: cache.fork(cu.ints([0]), cu.ints([1]), st)), books + pools)
+    same(moved(lambda: cache.gather(cu.ints([0]), kd, vd)), [kd, vd])
+    same(moved(lambda: cache.compact(st)), books + pools)
+    same(moved(lambda: cache.free(cu.ints([0]), st)), books)
+    w = torch.ones(4, 64, dtype=torch.bfloat16, device="cuda", requires_grad=True)
+    y = (q * w).sum()  # keeps q
+    cache.append(0, q, k, v, at[None], seqs, at, (32,))
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+    with torch.inference_mode():  # tensors without versions
+        z = torch.empty_like(q)
+        prompt_attention(q, k, v, cum, cum, z)
+        assert z.isfinite().all()
