@@ -36,6 +36,9 @@ int rope_tokens(int n, size_t row);
 // The launches take validated arguments.
 template <typename T>
 void launch_rope_append(const fv_rope_args& a, const fv_pages* c, hipStream_t s);
+// The kernel of a prompt attention: few rows, halved keys or whole tiles.
+enum { kFew, kHalves, kTiles };
+int prompt_form(const fv_prompt_args& a);
 template <typename T>
 void launch_prompt(const fv_prompt_args& a, hipStream_t s);
 

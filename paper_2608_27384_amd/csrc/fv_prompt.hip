@@ -848,8 +848,6 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void prompt_few_kernel(PromptCal
   }
 }
 
-enum { kFew, kHalves, kTiles };
-
 template <typename T, int DH>
 void prompt_at(PromptCall& a, int form, hipStream_t s) {
   const int R = form == kFew ? 32 : 128;
@@ -862,6 +860,8 @@ void prompt_at(PromptCall& a, int form, hipStream_t s) {
   else if constexpr (sizeof(T) == 2)
     hipLaunchKernelGGL((prompt_kernel<T, DH, 2>), grid, dim3(512), 0, s, a);
 }
+
+}  // namespace
 
 // Which kernel, by the 32-row tiles of the call (256 CUs; a CU holds one or two
 // workgroups).  us at prompts of 560 tokens (one prompt), heads 8/1 of 256: kFew 17
@@ -890,8 +890,6 @@ int prompt_form(const fv_prompt_args& x) {
   if (tiles < 384) return kFew;
   return tiles <= (x.causal && far ? 2560 : 1024) ? kHalves : kTiles;
 }
-
-}  // namespace
 
 template <typename T>
 void launch_prompt(const fv_prompt_args& x, hipStream_t s) {

@@ -61,6 +61,22 @@ def attention(q, k, v, limits, scale=None):
     return out, size, size * soft
 
 
+FEW, HALVES, TILES = range(3)
+
+
+def prompt_form(dtype, n_q, n_k, prompts, heads, kv_heads, head_dim, causal):
+    """The kernel that such a call of prompt attention takes (a C++ function of the library)."""
+    import ctypes
+    from paper_2608_27384_amd import flashvla as fvb
+    torch_mod()  # its HIP runtime is the process's, if the library is not loaded before it
+    f = getattr(fvb.lib(), "_ZN2fv11prompt_formERK14fv_prompt_args")
+    f.restype, f.argtypes = ctypes.c_int, [ctypes.POINTER(fvb.FvPromptArgs)]
+    a = fvb.FvPromptArgs(n_seqs=prompts, n_q=n_q, n_k=n_k, n_q_heads=heads, n_kv_heads=kv_heads,
+                         head_dim=head_dim, dtype=fvb.FV_BF16 if dtype == "bf16" else fvb.FV_FP32,
+                         causal=int(causal))
+    return f(ctypes.byref(a))
+
+
 def check_attention(got, ref, dtype):
     out, size, fp32 = ref
     tol = EPS[dtype] * out.abs() + fp32 * (1 + EPS[dtype]) + 1e-37

@@ -4,6 +4,7 @@ import ctypes
 
 import pytest
 
+import context_util as cu
 from paper_2608_27384_amd import flashvla as fvb
 
 
@@ -34,6 +35,25 @@ def test_rotary_grids_are_launches(n):
     (32768, 12288, 1)])
 def test_rotary_tokens_that_were_faster(n, row, tokens):
     assert rope_tokens(n, row) == tokens
+
+
+# Both sides of every threshold: (type, 32-row tiles of 8 heads, mean keys, head dim, causal, kernel)
+@pytest.mark.parametrize("dtype,tiles,keys,D,causal,form", [
+    ("bf16", 383, 560, 256, True, cu.FEW), ("bf16", 384, 560, 256, True, cu.HALVES),
+    ("bf16", 383, 9000, 64, False, cu.FEW), ("bf16", 384, 9000, 64, False, cu.HALVES),
+    ("bf16", 1024, 2047, 128, True, cu.HALVES), ("bf16", 1025, 2047, 128, True, cu.TILES),
+    ("bf16", 1025, 2048, 128, True, cu.HALVES), ("bf16", 2560, 2048, 192, True, cu.HALVES),
+    ("bf16", 2561, 2048, 192, True, cu.TILES), ("bf16", 1024, 2048, 128, False, cu.HALVES),
+    ("bf16", 1025, 2048, 128, False, cu.TILES), ("fp32", 4096, 500, 64, True, cu.FEW),
+    ("fp32", 4097, 500, 64, True, cu.TILES), ("fp32", 4096, 2048, 64, True, cu.FEW),
+    ("fp32", 4097, 2048, 64, True, cu.TILES), ("fp32", 4096, 2047, 192, True, cu.FEW),
+    ("fp32", 4097, 2047, 256, True, cu.TILES), ("fp32", 8192, 2048, 192, False, cu.FEW),
+    ("fp32", 8193, 2048, 256, True, cu.TILES), ("fp32", 2048, 2047, 128, True, cu.FEW),
+    ("fp32", 2049, 2047, 128, True, cu.TILES), ("fp32", 768, 2047, 128, False, cu.FEW),
+    ("fp32", 769, 2047, 128, False, cu.TILES), ("fp32", 4096, 2048, 128, False, cu.FEW),
+    ("fp32", 4097, 2048, 128, True, cu.TILES)])
+def test_prompt_kernels(dtype, tiles, keys, D, causal, form):
+    assert cu.prompt_form(dtype, 4 * tiles, 3 * keys, 3, 8, 1, D, causal) == form
 
 
 def test_direct_loads_take_their_address_register_as_an_operand():

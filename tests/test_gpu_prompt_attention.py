@@ -281,3 +281,113 @@ def test_replayed_graph_and_other_stream(shape):
     prompt_attention(q, k, v, dq, dk, out, stream=s)
     s.synchronize()
     assert torch.equal(out, want)
+
+
+# Prompts of more than 2000 keys on average, one of them longer: (queries, keys)
+FAR = [(33, 2700), (900, 2400)]
+# (type, heads, kv heads, head dim, causal, the kernel that FAR takes)
+FAR_CASES = [("bf16", H, G, D, c, form) for D in (64, 128, 192, 256) for H, G, c, form in (
+    (8, 1, True, cu.FEW), (8, 1, False, cu.FEW), (64, 4, True, cu.HALVES), (32, 2, False, cu.HALVES),
+    (128, 8, True, cu.TILES), (64, 4, False, cu.TILES))]
+FAR_CASES += [("fp32", 128, 8, D, c, cu.FEW) for D in (64, 128, 192, 256) for c in (True, False)]
+FAR_CASES += [("fp32", 256, 16, 64, True, cu.TILES), ("fp32", 256, 16, 128, False, cu.TILES),
+              ("fp32", 256, 16, 192, True, cu.FEW), ("fp32", 256, 16, 256, False, cu.FEW),
+              ("fp32", 288, 18, 192, True, cu.TILES), ("fp32", 288, 18, 256, True, cu.TILES)]
+
+
+def takes(shape, lens, causal):
+    return cu.prompt_form(shape[0], sum(a for a, _ in lens), sum(b for _, b in lens), len(lens),
+                          *shape[1:], causal)
+
+
+def check_some(shape, out, q, k, v, cq, ck, causal, seed=0):
+    """Some rows of every prompt, the first and the last ones among them, and some heads."""
+    dtype, H, G, D = shape
+    rng = np.random.default_rng(seed)
+    heads = sorted({0, H // 2, H - 1, *rng.integers(0, H, 2).tolist()})
+    kv = [h * G // H for h in heads]
+    for b in range(len(cq) - 1):
+        nq, nk = int(cq[b + 1] - cq[b]), int(ck[b + 1] - ck[b])
+        if nq == 0:
+            continue
+        rows = sorted({0, 1, 31, 32, 127, 128, nq // 2, nq - 33, nq - 2, nq - 1,
+                       *rng.integers(0, nq, 10).tolist()} & set(range(nq)))
+        lim = limits(nq, nk, causal)
+        at = [int(cq[b]) + r for r in rows]
+        ref = cu.attention(q[at][:, heads], k[ck[b]:ck[b + 1]][:, kv], v[ck[b]:ck[b + 1]][:, kv],
+                           [lim[r] for r in rows])
+        cu.check_attention(out[at][:, heads], ref, dtype)
+
+
+@pytest.mark.parametrize("case", FAR_CASES, ids=lambda c: "x".join(map(str, c)))
+def test_long_prompts(case):
+    """Prompts on the far side of the kernels' choice, some rows against the 64-bit form."""
+    shape, causal, form = case[:4], case[4], case[5]
+    assert takes(shape, FAR, causal) == form
+    q, k, v, cq, ck = make(shape, FAR)
+    check_some(shape, run(q, k, v, cq, ck, causal), q, k, v, cq, ck, causal)
+
+
+@pytest.mark.parametrize("case", FAR_CASES, ids=lambda c: "x".join(map(str, c)))
+def test_every_key_counts_once(case):
+    """With queries of zero every probability is one, and the value of key j in kv head g a one at
+    element j + g: a row's result is, times the keys that it sees, how many of them fall on each
+    element.  Sums of ones are exact; the quotient's three roundings and the result's own (bf16 2^-8,
+    fp32 2^-24) leave less than half a key where an element has at most 43."""
+    torch = cu.torch_mod()
+    (dtype, H, G, D), causal, form = case[:4], case[4], case[5]
+    assert takes(case[:4], FAR, causal) == form
+    q, k, v, cq, ck = make(case[:4], FAR)
+    q.zero_()
+    v.zero_()
+    for b in range(2):
+        j = torch.arange(FAR[b][1], device="cuda")[:, None]
+        g = torch.arange(G, device="cuda")[None]
+        v[ck[b]:ck[b + 1]].scatter_(2, ((j + g) % D)[..., None], 1.0)
+    out = run(q, k, v, cq, ck, causal)
+    d, g = torch.arange(D, device="cuda")[None, None], (torch.arange(H, device="cuda") * G // H)[None, :, None]
+    for b, (nq, nk) in enumerate(FAR):
+        lim = torch.tensor(limits(nq, nk, causal), device="cuda")[:, None, None]
+        want = torch.div(lim - (d - g) % D + D - 1, D, rounding_mode="floor").clamp(min=0)  # keys j = d - g mod D
+        assert int(want.max()) <= 43
+        got = out[cq[b]:cq[b + 1]].double() * lim
+        assert bool(((got - want).abs() <= want * (cu.EPS[dtype] + 2.0 ** -20)).all())
+
+
+@pytest.mark.parametrize("shape,causal", [(("bf16", 8, 1, 256), False), (("bf16", 8, 1, 256), True),
+                                          (("bf16", 16, 4, 128), True), (("fp32", 32, 8, 64), True)], ids=str)
+def test_prompts_in_any_order(shape, causal):
+    """More row tiles than the chip holds, the longest prompt first, last and anywhere: a prompt's
+    result does not depend on its place."""
+    torch = cu.torch_mod()
+    up = [(300 + 516 * i // 63, 300 + 516 * i // 63) for i in range(64)]
+    assert takes(shape, up, causal) == cu.TILES and sum(a for a, _ in up) * shape[1] // 128 > 512
+    q, k, v, cq, ck = make(shape, up)
+    want = run(q, k, v, cq, ck, causal)
+    check_some(shape, want, q, k, v, cq[:3], ck[:3], causal)
+    check_some(shape, want[cq[62]:], q[cq[62]:], k[ck[62]:], v[ck[62]:], cq[62:] - cq[62], ck[62:] - ck[62], causal)
+    rng = np.random.default_rng(1)
+    for order in (np.arange(64)[::-1], rng.permutation(64)):
+        at = torch.from_numpy(np.concatenate([np.arange(cq[i], cq[i + 1]) for i in order])).cuda()
+        edges = np.cumsum([0] + [up[i][0] for i in order])
+        assert torch.equal(run(q[at], k[at], v[at], edges, edges, causal), want[at])
+
+
+@pytest.mark.parametrize("shape", [("bf16", 128, 16, 64), ("bf16", 128, 16, 128), ("bf16", 128, 16, 192),
+                                   ("bf16", 128, 16, 256), ("fp32", 512, 32, 64), ("fp32", 512, 32, 128),
+                                   ("fp32", 512, 32, 256)], ids=lambda s: "x".join(map(str, s)))
+def test_strided_rows_of_whole_tiles(shape):
+    """The kernel of whole tiles on columns of one matrix, its results into columns of another."""
+    torch = cu.torch_mod()
+    dtype, H, G, D = shape
+    n = 300
+    cq = np.array([0, 171, n])
+    assert takes(shape, [(171, 171), (129, 129)], True) == cu.TILES
+    qkv = cu.randn(dtype, 3, n, (H + 2 * G) * D + 32)
+    q, k, v = (qkv[:, a * D:b * D].unflatten(1, (-1, D)) for a, b in ((0, H), (H, H + G), (H + G, H + 2 * G)))
+    wide = torch.full((n + 5, H * D + 16), 7.0, dtype=q.dtype, device="cuda")
+    out = wide[:n, :H * D].unflatten(1, (H, D))
+    run(q, k, v, cq, cq, True, out)
+    check_some(shape, out, q, k, v, cq, cq, True)
+    assert (wide[n:] == 7).all() and (wide[:, H * D:] == 7).all()
+    assert torch.equal(out, run(*(x.contiguous() for x in (q, k, v)), cq, cq, True))
