@@ -260,3 +260,31 @@ def test_values_that_are_not_finite(shape, bad):
         got = out[..., hit]
         assert (got.isnan() if np.isnan(bad) else got == bad).all()
         assert out[..., ~hit].isfinite().all()
+
+
+@pytest.mark.parametrize("max_len", [0, 4900, 40])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_every_key_counts_once(shape, max_len):
+    """With queries of zero every probability is one, and the value of position p in kv head g a one
+    at element p + g: a row's result is, times its length, how many positions fall on each element.
+    Ones are 1 + 2^-23 in bf16, whose sums of 77 and, for the denominator, of a lane's 20 by 64 lanes
+    and 39 chunks, each addition off by 2^-24, stay within 2^-16; with the result's own rounding
+    (2^-8) that leaves less than half a key where an element has at most 77."""
+    torch = cu.torch_mod()
+    dtype, H, G, D = shape
+    lens = [1, 16, 127, 128, 129, 1000, 2048, 3333, 4900]
+    cache, q, table = make(shape, lens, 48, layers=1)
+    q.zero_()
+    cache.v.masked_fill_(~cache.v.isnan(), 0.0)
+    g = torch.arange(G, device="cuda")[:, None]
+    for b, n in enumerate(lens):
+        for j in range(-(-n // 48)):
+            p = torch.arange(48 * j, min(48 * j + 48, n), device="cuda")[None]
+            cache.v[0, table[b, j], :, :p.shape[1]].scatter_(2, ((p + g) % D)[..., None], 1.0)
+    out = torch.full_like(q, 7.0)
+    cache.attend(0, q, cu.ints(range(len(lens))), out, max_len=max_len)
+    n = torch.tensor(lens, device="cuda")[:, None, None]
+    d, h = torch.arange(D, device="cuda")[None, None], (torch.arange(H, device="cuda") * G // H)[None, :, None]
+    want = torch.div(n - (d - h) % D + D - 1, D, rounding_mode="floor").clamp(min=0)
+    assert int(want.max()) <= 77
+    assert bool(((out.double() * n - want).abs() <= want * (cu.EPS[dtype] + 2.0 ** -16)).all())
