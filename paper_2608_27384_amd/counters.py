@@ -54,7 +54,8 @@ ATTN_SRC = ("csrc/fv_attn.hip", "csrc/fv_internal.h")
 MISC_SRC = ("csrc/fv_misc.hip", "csrc/fv_internal.h")
 ALL_SRC = ("csrc/fv_gemm.hip", "csrc/fv_few.hip", "csrc/fv_attn.hip", "csrc/fv_misc.hip",
            "csrc/fv_runtime.hip", "csrc/fv_internal.h", "csrc/fv_context.hip", "csrc/fv_pages.hip",
-           "csrc/fv_paged.hip", "csrc/fv_prompt.hip")
+           "csrc/fv_paged.hip", "csrc/fv_prompt.hip", "csrc/fv_context.h", "csrc/fv_error.h",
+           "csrc/fv_pack.h")
 
 # kernel key (substring of its name in a trace) -> source files that define it
 KERNELS: Dict[str, Tuple[str, ...]] = {

@@ -13,8 +13,8 @@ __host__ __device__ __forceinline__ size_t page_row(int page, int n_kv, int head
 
 // Data that no cache holds until it is used again (the last level has 256 MiB) is moved past
 // them: above twice that size a call's loads and stores are marked as streaming.  Paged
-// attention, 192 rows of 1 to 8191 keys, 32/8 heads of 128 (3.2 GB), 569 us, streaming 524;
-// 64 of 500 to 3001, fp32, 8/1 of 256 (0.2 GB), called again and again, 68 and 79.  Gathering
+// attention, 192 rows of 1 to 8191 keys, 32/8 heads of 128 (3.2 GB), 574 us, streaming 526;
+// 64 of 500 to 3001, fp32, 8/1 of 256 (0.2 GB), called again and again, 65 and 79.  Gathering
 // 64 sequences of 300 to 816 in 18 layers (1.3 GB moved) 243 and 228.
 constexpr size_t kStreamBytes = (size_t)512 << 20;
 template <bool STREAM, typename V> __device__ __forceinline__ V load_piece(const V* p) {

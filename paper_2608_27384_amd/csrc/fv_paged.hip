@@ -25,7 +25,7 @@
 //
 // Measured (a read of memory alone reaches 6.2 TB/s): 192 rows of 1 to 8191 keys, heads
 // 32/8 of 128, 524 us (6.2 TB/s); 192 of 1 to 16000, 8/1 of 256, 290 us (5.5); 64 of 816,
-// 14 us, of which the two launches are 7; 1 of 800, 10 us.
+// 14 us; 1 of 816, 11 us, as a caller sees them.
 #include "fv_context.h"
 
 namespace fv {
@@ -459,12 +459,12 @@ void paged_at(const PagedCall& a, size_t bytes, hipStream_t s) {
 PagedPlan plan_paged(int n, int n_q_heads, int n_kv_heads, int head_dim, int max_keys, bool bf16) {
   PagedPlan p{};
   const int64_t cols = (int64_t)n * n_kv_heads * ((n_q_heads / n_kv_heads + 15) / 16);
-  // 2048 workgroups fill the chip (two to four a CU at a time) and leave room
-  // for ragged lengths: 64 rows of 1 to 8000 keys, heads 4/2 of 192, 83 us, with 1024
-  // of them 91; 64 of 500 to 3001, fp32, 8/1 of 256, 68 and 77.  A chunk is at least
-  // one tile of each wave and at most 2048 keys, where its partial result is below a
-  // hundredth of its keys: 192 rows of 1 to 8191 keys, 32/8 of 128, 569 us, with at
-  // most 1024 keys 569, with 512 591.
+  // 2048 workgroups fill the chip (two to four a CU at a time) and leave room for ragged
+  // lengths: 64 rows of 1 to 8000 keys, heads 4/2 of 192, 83 us, with 1024 of them 91; 64 of 500
+  // to 3001, fp32, 8/1 of 256, 65 and 76; 192 of 1 to 16000, 292 and 335; alike lengths want fewer
+  // (256 of 8000 362 and 336).  A chunk is at least one tile of each wave and at most 2048 keys:
+  // 192 rows of 1 to 8191 keys, 32/8 of 128, 526 us, with at most 512, 1024 and 4096 keys 564,
+  // 551 and 657; 192 of 1 to 16000, 8/1 of 256, 292, and 320, 296 and 292.
   const int least = kPagedWaves * (bf16 ? 32 : 16);
   int64_t chunk = ((int64_t)max_keys * cols + 2047) / 2048;
   chunk = (chunk + least - 1) / least * least;

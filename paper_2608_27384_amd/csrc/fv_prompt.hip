@@ -174,7 +174,12 @@ __device__ __forceinline__ f32x16 product(u32x4 v, const f32x16&, const u32x4 (&
 __device__ __forceinline__ f32x16 product(float v, const f32x16& p, const u32x4 (&)[2], int c, f32x16 o) {
   return __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[c], o, 0, 0, 0);
 }
-// bf16 operands of 32 probabilities.
+// bf16 operands of 32 probabilities, each rounded once (2^-8 at most), as the result is
+// afterwards; their sum is of the unrounded ones.  The error against 64 bits is 1.2 to 1.4
+// times that of exact probabilities.  Operands of 16 bits, in two parts, make half as
+// many products again, which here nothing hides: us with one part and with two, one prompt
+// of 560, heads 8/1 of 256, 15.6 and 17.0; 64 of 300 to 816 196 and 258; one of 28672 2634
+// and 3770; 7 of 1 to 4111, 32/8 of 128, 599 and 857.
 __device__ __forceinline__ void as_operands(const f32x16& p, u32x4 (&pf)[2]) {
 #pragma unroll
   for (int c = 0; c < 2; ++c) {
@@ -305,7 +310,8 @@ struct Rows {
     wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     l32 = lane & 31;
     lh = lane >> 5;
-    // the heaviest tiles of a causal prompt, its last ones, go first
+    // within a causal prompt the heaviest tiles, its last ones, go first; the prompts go in
+    // the reverse of the caller's order
     const int slot = a.n_slots - 1 - (int)(blockIdx.x / a.n_kv);
     kh = blockIdx.x % a.n_kv;
     int first;
@@ -878,6 +884,11 @@ void prompt_at(PromptCall& a, int form, hipStream_t s) {
 // 1668 and 1814; but heads of 64, 16 of 4000 (16000), 2400 and 2250.  So does the causal
 // edge, most at 128: 4 prompts of 800, heads 8/2 (800), 74 and 111, all keys seen 137 and
 // 112.
+// Swept again over 122 calls (head dims 64 to 256, 140 to 8000 tiles, prompts of 128 to
+// 16000): the kernel taken is the fastest or within 6 % of it in 114; the others are bf16
+// heads of 64 at 560 to 600 tiles (one prompt of 2400: 28 and 22 with kFew; four of 560: 11.0 and
+// 10.3) and of 128 with prompts under 200 (11.4 and 9.6 with kTiles), fp32 heads of 64 at
+// 4050 to 7800 tiles (142 and 125, 817 and 752) and of 128, every key seen (287 and 262).
 int prompt_form(const fv_prompt_args& x) {
   const int64_t tiles = (int64_t)x.n_q * x.n_q_heads / 32;
   const bool far = x.n_k / x.n_seqs >= 2048;  // long prompts
