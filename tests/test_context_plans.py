@@ -68,3 +68,16 @@ def test_direct_loads_take_their_address_register_as_an_operand():
             blocks += re.findall(r"asm volatile\(.*?\);", f.read(), re.S)
     loads = [b for b in blocks if "m0" in b or "offen lds" in b]
     assert loads and all('"{m0}"' in b and "_b32 m0" not in b for b in loads)
+
+
+def test_the_gpu_tests_reach_every_prompt_kernel():
+    """The shapes of the GPU tests run the kernels that they are there for, by today's choice."""
+    import test_gpu_prompt_attention as t
+    few = {(s[0], s[3], t.takes(s, t.LENS["ragged"], True)) for s in t.SHAPES}
+    assert {f for _, _, f in few} == {cu.FEW} and {d for _, d, _ in few} == {64, 128, 192, 256}
+    full = {(s[0], s[3], t.takes(s, t.LENS["ragged"], c)) for s in t.FULL for c in (True, False)}
+    assert full == {(d, D, f) for d, fs in (("bf16", (cu.HALVES, cu.TILES)), ("fp32", (cu.TILES,)))
+                    for D in (64, 128, 192, 256) for f in fs}
+    far = {(c[0], c[3], c[5]) for c in t.FAR_CASES}
+    assert far == {(d, D, f) for d, fs in (("bf16", (cu.FEW, cu.HALVES, cu.TILES)), ("fp32", (cu.FEW, cu.TILES)))
+                   for D in (64, 128, 192, 256) for f in fs}
