@@ -136,7 +136,7 @@ __device__ __forceinline__ int pages_of(int len, int page_len) {
 __device__ __forceinline__ bool is_page(const fv_pages& c, int p) { return p >= 0 && p < c.n_pages; }
 
 // A plan kernel is one workgroup, bound by its trips to memory one after another: 7.4
-// us to fork, 6 to grow, 9.7 to compact a cache of 4000 pages.
+// us to fork and 6.7 to grow by 32 children, 10.3 to compact a cache of 4564 pages.
 // Exclusive sum over the workgroup; *total is the whole.
 __device__ int block_scan(int x, int* wave_sums, int* total) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;

@@ -232,9 +232,10 @@ __device__ __forceinline__ void softmax(f32x16& sc, bool edge, int key0, int lh,
 // everything again.  `minus`: minus the reference, kNoRef for a row without one,
 // against which any visible score is infinite and a hidden one still nothing.
 // Leaves the scores as they are, which takes 16 more registers: for head dims up to
-// 192.  The vector unit bounds the loop at 128 (740 of 850 cycles a step, the
-// products 512): 16 maxima less, and the kept load offsets, brought eight prompts of
-// 2000 tokens, heads 32/8 of 128, from 519 to 485 us (1.08 PFLOP/s).
+// 192.  At 128 the vector unit is busy 58 % of the time and the matrix unit 62 %, and a
+// wave uses one after the other: 16 maxima less, and the kept load offsets, brought eight
+// prompts of 2000 tokens, every key seen, heads 32/8 of 128, from 519 to 485 us (1.08
+// PFLOP/s).
 constexpr float kLimit = 1024.0f;  // sums stay within 2^10 of the largest value's size
 constexpr float kNoRef = 3.402823466e38f;
 template <typename Rescale>
@@ -406,7 +407,7 @@ struct Walk : Rows<T, DH, 128> {
   }
   // Direct loads of key tile kt: slot u, 16 bytes, is piece u % PIECES of row u / PIECES.
   // offs: the offsets of a whole tile (Offsets), which the narrower heads have the
-  // registers to keep; the vector unit is what their loop is bound by.
+  // registers to keep, and whose vector instructions they have few products to hide behind.
   static constexpr bool KEEP = E == 2 && DH <= 128;
   struct Offsets {
     int k[KEEP ? NI : 1], v[KEEP ? NI : 1];
