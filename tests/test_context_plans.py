@@ -14,7 +14,7 @@ def rope_tokens(n, row):
     return f(n, row)
 
 
-# bytes of a token that are rotated or stored: one head of 64 in bf16 to 3072 of 256 in fp32
+# bytes of a token that are rotated or stored: a head of 64 in bf16 to three times 1024 of 256 in fp32
 ROWS = [128 << i for i in range(15)] + [(6 << 10) - 16, 6 << 10, (10 << 10) - 16, 10 << 10, 12 << 10, 3 << 20]
 COUNTS = [1, 2047, 2048, 16384] + [n + d for n in (1 << 23, 1 << 24, 1 << 25, 1 << 26) for d in (-1, 0, 1)]
 
