@@ -288,3 +288,42 @@ def test_every_key_counts_once(shape, max_len):
     want = torch.div(n - (d - h) % D + D - 1, D, rounding_mode="floor").clamp(min=0)
     assert int(want.max()) <= 77
     assert bool(((out.double() * n - want).abs() <= want * (cu.EPS[dtype] + 2.0 ** -16)).all())
+
+
+@pytest.mark.parametrize("page_len", range(16, 257, 16))
+@pytest.mark.parametrize("shape", [SHAPES[2], SHAPES[5]], ids=str)
+def test_every_page_length(shape, page_len):
+    torch = cu.torch_mod()
+    lens = [0, 1, page_len - 1, page_len, page_len + 1, 3 * page_len + 17, 16 * page_len, 4000 + page_len]
+    cache, q, table = make(shape, lens, page_len, extra=2)
+    for max_len in (0, 100):
+        out = torch.full_like(q, 7.0)
+        cache.attend(1, q, cu.ints(range(len(lens))), out, max_len=max_len)
+        check(shape, cache, table, lens, q, out, 1)
+
+
+@pytest.mark.parametrize("max_len", [0, 1 << 20])
+def test_longest_row_of_a_table(max_len):
+    """65536 pages of 256 rows, sixteen pages each named 4096 times: the result over every key once.
+    Of a chunk's 2048 keys a lane adds 128, and of 8192 chunks a wave 1024, a shorter chain of additions
+    than the 4096 of the definition's bound; planned for 2^20 keys the last chunk has the other 2^24,
+    of which a lane adds one in 16 (four waves, tiles of 32 keys of which a lane has 8)."""
+    from paper_2608_27384_amd.flashvla import PageCache
+    torch = cu.torch_mod()
+    shape = ("bf16", 8, 1, 64)
+    pl, pages, width = 256, 16, 65536
+    k, v = (cu.randn("bf16", i, 1, pages, 1, pl, 64) for i in (1, 2))
+    ids = np.random.default_rng(0).permutation(np.repeat(np.arange(pages), width // pages))
+    n = width * pl
+    cache = PageCache(k, v, cu.ints([ids]), cu.ints([n]), cu.ints([width // pages] * pages))
+    q = cu.randn("bf16", 3, 1, 8, 64)
+    out = torch.full_like(q, 7.0)
+    cache.attend(0, q, cu.ints([0]), out, max_len=max_len)
+    want, size, soft = cu.attention(q, k[0].reshape(-1, 1, 64), v[0].reshape(-1, 1, 64), [pages * pl])
+    if max_len:
+        soft = soft + size * (n // 16 * 2.0 ** -24)
+    cu.check_attention_wide(out, (want, size, soft), "bf16")
+    cache.length.fill_(n - 1)  # one key fewer moves nothing by more than its weight
+    again = torch.full_like(q, 7.0)
+    cache.attend(0, q, cu.ints([0]), again, max_len=max_len)
+    cu.check_attention_wide(again, (want, size, soft + size * 2.0 ** -8), "bf16")
