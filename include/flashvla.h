@@ -508,7 +508,9 @@ fv_status fv_rope_append(const fv_rope_args *args, const fv_pages *cache, void *
  * nk) gives zeros.  Rows past cu_q[n_seqs] are left as they were.  What a query
  * does not see has no influence on its result, also where it is infinite or NaN.
  * Scores, softmax and sums are fp32; in bf16 the probabilities are rounded to
- * bf16 before they meet the values.  out must not overlap q, k or v.
+ * bf16 before they meet the values.  Values are summed before they are divided by
+ * the weights' sum, with weights of up to 2^10: sizes from 2^117 / nk on may leave
+ * the range of fp32 on the way.  out must not overlap q, k or v.
  * Errors: FV_ERR_INVALID_ARG (a size below 0, n_seqs > 65536, n_q * n_q_heads >
  * 2^30, n_seqs * n_kv_heads > 2^22, strides, pointers), FV_ERR_HIP.
  */
@@ -536,9 +538,10 @@ fv_status fv_prompt_attention(const fv_prompt_args *args, void *stream);
  *  work     fv_paged_attention_workspace bytes, overwritten (calls that may run
  *           at the same time need one each); NULL where that is 0
  * Scores, softmax and sums are fp32; in bf16 the probabilities meet the values in
- * two parts of bf16, together 16 bits.  The result does not depend on the other
- * rows' lengths.  out must not overlap q, work none of the other operands, and
- * neither the layer's pages.  n is at most 65536, n * n_q_heads at most 2^22.
+ * two parts of bf16, together 16 bits, and weights are at most 1 while values are
+ * summed.  The result does not depend on the other rows' lengths.  out must not
+ * overlap q, work none of the other operands, and neither the layer's pages.  n is
+ * at most 65536, n * n_q_heads at most 2^22.
  * Errors: FV_ERR_INVALID_ARG, FV_ERR_HIP.
  */
 typedef struct {
