@@ -606,6 +606,127 @@ fv_status fv_pages_compact(const fv_pages *cache, int32_t *used, void *work, voi
 fv_status fv_pages_gather(const fv_pages *cache, const int32_t *seqs, int32_t n, int32_t ld,
                           void *k_out, void *v_out, void *stream);
 
+/*
+ * ---------------------------------------------------------------------------
+ * The cache in 8 bits: the same operators over pages of e4m3 numbers (sign, 4
+ * bits of exponent, 3 of mantissa; largest 448; the bytes 127 and 255 are NaN),
+ * with a power of two as the scale of each block.  A block is 16 positions of a
+ * sequence, p to p + 15 with p a multiple of 16, in one layer and kv head, keys
+ * and values apart: its scale is one byte b, and a code stands for code *
+ * 2^(b - 127).  Every such number is a bf16 number, so that only the quantising
+ * rounds.  The conventions of the observation context hold; sequences, pages and
+ * the bookkeeping are those of fv_pages.
+ * ---------------------------------------------------------------------------
+ */
+
+/*
+ *  dtype  FV_BF16 or FV_FP32: of the queries, keys, values and results of the calls
+ *  k, v   [n_layers][n_pages][n_kv_heads][page_len / 16] blocks of 16 * head_dim
+ *         bytes.  With d = 64 s + 16 c + i (c < 4, i < 16), byte of position t and
+ *         element d in a block of keys: 1024 s + 64 t + 16 c + i; of values:
+ *         1024 s + 256 (t / 4) + 16 i + 4 c + t % 4, as the matrix unit takes them.
+ *  k_scale, v_scale  uint8 [n_layers][n_pages][n_kv_heads][page_len / 16]: the bytes
+ *         b, from 10 to 246 where fv_quant_append wrote them.  One outside counts
+ *         as the nearer end of this range.
+ *  table, len, refs, and the requirements on sizes: as in fv_pages
+ */
+typedef struct {
+  int32_t dtype, n_layers, n_kv_heads, head_dim, page_len, n_pages, max_seqs, max_pages;
+  void *k, *v, *k_scale, *v_scale;
+  int32_t *table, *len, *refs;
+} fv_quant_pages;
+
+/*
+ * fv_quant_append -- fv_rope_append into a cache in 8 bits, which is not NULL.
+ * Arguments, rotation, q_out and k_out are those of fv_rope_append (k_out: the
+ * rotated keys in the dtype); keys are quantised from the rotation's fp32 result.
+ * The tokens of one block stand side by side in the list, at rising positions.
+ * With a = m 2^k (1 <= m < 2) the largest size among their finite elements, they ask
+ * for the scale 2^e, e = k - 8 for m <= 1.75, else k - 7, at least -117, at most 119.
+ *  - From the block's first position on, the block starts anew: its scale is 2^e,
+ *    and its other positions hold zeros.
+ *  - From another position on, the scale is the larger of 2^e and the block's own,
+ *    and the other positions keep what they hold, rounded again where the scale grew
+ *    (which changes only what falls below 2^-6 of it).
+ * Elements are rounded to the nearest code, ties to even, and saturate at 448 times
+ * the scale; what is infinite or NaN becomes NaN and has no part in a.
+ * A block whose tokens stand in several places of the list holds codes of either
+ * and a scale of either: the caller appends them by several calls.
+ * Errors: FV_ERR_INVALID_ARG, FV_ERR_HIP.
+ */
+fv_status fv_quant_append(const fv_rope_args *args, const fv_quant_pages *cache, void *stream);
+
+/*
+ * fv_quant_attention -- fv_paged_attention over a cache in 8 bits: attention of one
+ * new token a sequence.  Arguments and conventions are those of fv_paged_attention,
+ * work is fv_quant_attention_workspace bytes.  The probabilities meet the values in
+ * two parts of bf16, together 16 bits, in fp32 in three, 24 bits; scores are products
+ * of the exact queries and codes.
+ * Errors: FV_ERR_INVALID_ARG, FV_ERR_HIP.
+ */
+fv_status fv_quant_attention_workspace(const fv_paged_args *args, const fv_quant_pages *cache,
+                                       size_t *bytes);
+fv_status fv_quant_attention(const fv_paged_args *args, const fv_quant_pages *cache, void *stream);
+
+/*
+ * fv_quant_part_attention -- attention of several new tokens a sequence over one
+ * layer of a cache in 8 bits: parts of prompts, chunks (the tokens' own keys and
+ * values are in the cache already).
+ *  q, out   [n_q][n_q_heads][head_dim], ldq, ldo
+ *  cu_q     int32 [n_seqs + 1], ascending from 0: entry i has the query rows
+ *           cu_q[i] .. cu_q[i+1], the last ones of sequence seqs[i]
+ *  seqs     int32 [n_seqs].  Rows of an entry whose seqs is out of range are left as
+ *           they were.  A sequence may occur several times.
+ *  causal   1: query j of nq sees the positions up to len - nq + j; 0: all of them.
+ *           A query that sees none gives zeros.  Table entries that are no page hold
+ *           no keys.  What a query does not see has no influence on its result.
+ *  max_len  a bound of the lengths that only plans the work, as above
+ *  scale    of the scores, positive and finite
+ *  work     fv_quant_part_workspace bytes, overwritten (calls that may run at the same
+ *           time need one each); NULL where that is 0
+ * Rows past cu_q[n_seqs] are left as they were.  Scores, softmax and sums are fp32; in
+ * bf16 the probabilities are rounded to bf16 before they meet the values, in fp32 they
+ * keep 24 bits; sums may leave the range of fp32 as in fv_prompt_attention.  out must
+ * not overlap q, work none of the other operands, and neither the layer's pages.
+ * Errors: FV_ERR_INVALID_ARG (a size below 0, n_seqs > 65536, n_q * n_q_heads > 2^28,
+ * n_seqs * n_kv_heads > 2^22, strides, pointers), FV_ERR_HIP.
+ */
+typedef struct {
+  const void *q;
+  void *out;
+  int32_t ldq, ldo;
+  const int32_t *cu_q, *seqs;
+  int32_t n_seqs, n_q, n_q_heads, layer, max_len, causal;
+  float scale;
+  void *work;
+  size_t work_bytes;
+} fv_part_args;
+fv_status fv_quant_part_workspace(const fv_part_args *args, const fv_quant_pages *cache,
+                                  size_t *bytes);
+fv_status fv_quant_part_attention(const fv_part_args *args, const fv_quant_pages *cache,
+                                  void *stream);
+
+/*
+ * The upkeep of a cache in 8 bits: fv_pages_grow, _fork, _free, _compact and _gather
+ * on it, with the same arguments, statuses and conventions; work is
+ * fv_quant_workspace bytes.  fv_quant_fork copies the blocks of a part-filled last
+ * page that hold positions in use, whole and with their scales; fv_quant_compact
+ * moves the scales with the pages.  fv_quant_gather reads back: k_out and v_out are
+ * of the cache's dtype and hold what the codes stand for, exactly.
+ * Errors: FV_ERR_INVALID_ARG, FV_ERR_HIP.
+ */
+fv_status fv_quant_workspace(const fv_quant_pages *cache, size_t *bytes);
+fv_status fv_quant_grow(const fv_quant_pages *cache, const int32_t *seqs, const int32_t *add,
+                        int32_t n, int32_t *status, void *work, void *stream);
+fv_status fv_quant_fork(const fv_quant_pages *cache, const int32_t *parents,
+                        const int32_t *children, int32_t n, int32_t *status, void *work,
+                        void *stream);
+fv_status fv_quant_free(const fv_quant_pages *cache, const int32_t *seqs, int32_t n,
+                        int32_t *status, void *stream);
+fv_status fv_quant_compact(const fv_quant_pages *cache, int32_t *used, void *work, void *stream);
+fv_status fv_quant_gather(const fv_quant_pages *cache, const int32_t *seqs, int32_t n, int32_t ld,
+                          void *k_out, void *v_out, void *stream);
+
 /* Message of the calling thread's last failed call of the observation context
  * ("" if its last one succeeded), valid until the thread's next one. */
 const char *fv_context_error(void);

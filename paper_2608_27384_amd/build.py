@@ -16,7 +16,8 @@ ROOT = os.path.dirname(HERE)
 OUT = os.path.join(HERE, "libflashvla.so")
 BUILD_DIR = os.path.join(ROOT, "_build")
 SOURCES = ["fv_runtime.hip", "fv_gemm.hip", "fv_attn.hip", "fv_few.hip", "fv_misc.hip",
-           "fv_context.hip", "fv_pages.hip", "fv_paged.hip", "fv_prompt.hip"]
+           "fv_context.hip", "fv_pages.hip", "fv_paged.hip", "fv_prompt.hip",
+           "fv_quant.hip", "fv_quant_attn.hip", "fv_quant_part.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -55,7 +55,8 @@ MISC_SRC = ("csrc/fv_misc.hip", "csrc/fv_internal.h")
 ALL_SRC = ("csrc/fv_gemm.hip", "csrc/fv_few.hip", "csrc/fv_attn.hip", "csrc/fv_misc.hip",
            "csrc/fv_runtime.hip", "csrc/fv_internal.h", "csrc/fv_context.hip", "csrc/fv_pages.hip",
            "csrc/fv_paged.hip", "csrc/fv_prompt.hip", "csrc/fv_context.h", "csrc/fv_error.h",
-           "csrc/fv_pack.h")
+           "csrc/fv_pack.h", "csrc/fv_paged.h", "csrc/fv_prompt.h", "csrc/fv_quant.h",
+           "csrc/fv_quant.hip", "csrc/fv_quant_attn.hip", "csrc/fv_quant_part.hip")
 
 # kernel key (substring of its name in a trace) -> source files that define it
 KERNELS: Dict[str, Tuple[str, ...]] = {

@@ -6,6 +6,8 @@
 
 namespace fv {
 
+constexpr float kLog2e = 1.4426950408889634f;
+
 // First of the `group` kv heads' rows: the pools are [layer][page][kv head][row][dh].
 __host__ __device__ __forceinline__ size_t page_row(int page, int n_kv, int head, int page_len) {
   return ((size_t)page * n_kv + head) * page_len;
@@ -27,6 +29,34 @@ template <bool STREAM, typename V> __device__ __forceinline__ void store_piece(V
   else
     *p = x;
 }
+
+// The angles of a thread of kRopeThreads: pair i turns by pos * theta^(-2i/DH), taken in turns
+// (over 2 pi) in 64 bits, of which only the fraction is rounded to fp32.
+template <int DH> struct RopeAngles {
+  static constexpr int HALF = DH / 2, STEP = 256 / HALF;  // tokens a pass
+  const int* pos;  // of the pair's axis
+  double turns;
+  int i, at;  // the pair, the first token of the thread
+  __device__ __forceinline__ RopeAngles(const fv_rope_args& a, double log2_theta) {
+    i = threadIdx.x % HALF;
+    at = threadIdx.x < STEP * HALF ? threadIdx.x / HALF : 1 << 30;
+    int axis = 0, end = a.sections[0];
+    while (axis < a.n_axes - 1 && i >= end) end += a.sections[++axis];
+    pos = a.pos + (size_t)axis * a.n;
+    turns = exp2(-log2_theta * (2.0 * i / DH)) * 0.15915494309189535;
+  }
+  // Of the tokens from `from` to `to` behind t0.
+  __device__ __forceinline__ void form(int t0, int from, int to, float (*cs)[HALF], float (*sn)[HALF]) const {
+    for (int t = from + at; t < to; t += STEP) {
+      double x = (double)pos[t0 + t] * turns;
+      x -= rint(x);
+      float s, c;
+      sincospif(2.0f * (float)x, &s, &c);
+      cs[t][i] = c;
+      sn[t][i] = s;
+    }
+  }
+};
 
 constexpr int kRopeThreads = 256;
 constexpr int kRopeTokens = 8;  // most tokens of a workgroup
@@ -58,12 +88,16 @@ inline size_t pages_list(const fv_pages& c) {
   return (size_t)(c.n_pages > c.max_seqs ? c.n_pages : c.max_seqs);
 }
 inline size_t pages_work_ints(const fv_pages& c) { return kPagesHeader + 3 * pages_list(c); }
+// The scales of a cache in 8 bits, whose pages then hold a byte an element; none otherwise.
+struct Scales {
+  uint8_t *k = nullptr, *v = nullptr;
+};
 void launch_pages_grow(const fv_pages& c, const int* seqs, const int* add, int n, int* status,
                        int* work, hipStream_t s);
 void launch_pages_fork(const fv_pages& c, const int* parents, const int* children, int n,
-                       int* status, int* work, hipStream_t s);
+                       int* status, int* work, hipStream_t s, const Scales& q = {});
 void launch_pages_free(const fv_pages& c, const int* seqs, int n, int* status, hipStream_t s);
-void launch_pages_compact(const fv_pages& c, int* used, int* work, hipStream_t s);
+void launch_pages_compact(const fv_pages& c, int* used, int* work, hipStream_t s, const Scales& q = {});
 void launch_pages_gather(const fv_pages& c, const int* seqs, int n, int ld, void* k_out,
                          void* v_out, hipStream_t s);
 

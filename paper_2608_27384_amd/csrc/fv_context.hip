@@ -1,6 +1,7 @@
 // The C boundary of the observation context's operators: what the host can see
 // of a call is checked here, before anything is enqueued.
 #include "fv_context.h"
+#include "fv_quant.h"
 
 #include <cmath>
 #include <exception>
@@ -70,6 +71,10 @@ void check_cache(const fv_pages* c) {
   aligned(c->table, 4, "cache table");
   aligned(c->len, 4, "cache len");
   aligned(c->refs, 4, "cache refs");
+}
+
+void check_layer(int layer, int n_layers) {
+  if (layer < 0 || layer >= n_layers) bad("layer out of range");
 }
 
 // A strided operand: rows of `row` bytes, `ld` bytes apart, from lo to hi.
@@ -146,7 +151,7 @@ void check_paged(const fv_paged_args* a, const fv_pages* c) {
   if (a->n < 0 || a->n > 65536) bad("n must be 0 to 65536");
   if ((int64_t)a->n * a->n_q_heads > 1 << 22) bad("n * n_q_heads must be at most 2^22");
   if (a->max_len < 0) bad("max_len must not be negative");
-  if (a->layer < 0 || a->layer >= c->n_layers) bad("layer out of range");
+  check_layer(a->layer, c->n_layers);
 }
 
 PagedPlan paged_plan(const fv_paged_args& a, const fv_pages& c) {
@@ -161,6 +166,118 @@ void check_list(const fv_pages* c, const void* p, int n, const char* what) {
   if (n) aligned(p, 4, what);
 }
 
+// The rotary append into c (or none), which holds `held` for the layer; whether there is work.
+bool check_rope(const fv_rope_args* a, const fv_pages* c, const Span* held, int n_held) {
+  need(a, "args");
+  const size_t e = type_size(a->dtype);
+  check_heads(a->n_q_heads, a->n_kv_heads, a->head_dim);
+  if (a->n < 0 || a->n > 1 << 26) bad("n must be 0 to 2^26");
+  if (a->n_axes < 1 || a->n_axes > 4) bad("n_axes must be 1 to 4");
+  int64_t pairs = 0;
+  for (int i = 0; i < a->n_axes; ++i) {
+    if (a->sections[i] < 0) bad("sections must not be negative");
+    pairs += a->sections[i];
+  }
+  if (pairs != a->head_dim / 2) bad("sections must add up to head_dim/2");
+  if (!(a->theta > 0.f) || !std::isfinite(a->theta)) bad("theta must be positive and finite");
+  if (c) {
+    check_cache(c);
+    if (c->dtype != a->dtype || c->head_dim != a->head_dim || c->n_kv_heads != a->n_kv_heads)
+      bad("the cache has another dtype, head_dim or n_kv_heads");
+    if (a->layer < 0 || a->layer >= c->n_layers) bad("layer out of range");
+  }
+  if (a->n == 0) return false;
+  const int rq = a->n_q_heads * a->head_dim, rk = a->n_kv_heads * a->head_dim;
+  const Span q = operand(a->q, a->n, a->ldq, rq, e, "q");
+  const Span k = operand(a->k, a->n, a->ldk, rk, e, "k");
+  const Span v = c ? operand(a->v, a->n, a->ldv, rk, e, "v") : Span{};
+  const Span qo = operand(a->q_out, a->n, a->ldq_out, rq, e, "q_out");
+  // an output may be its own input, and nothing else that the call reads or writes
+  const bool q_in_place = a->q_out == a->q && a->ldq_out == a->ldq;
+  if (!q_in_place) apart(qo, q, "q_out and q");
+  if (!q_in_place || c || a->k_out) apart(qo, k, "q_out and k");
+  apart(qo, v, "q_out and v");
+  Span ko;
+  if (a->k_out) {
+    ko = operand(a->k_out, a->n, a->ldk_out, rk, e, "k_out");
+    if (!(a->k_out == a->k && a->ldk_out == a->ldk)) apart(ko, k, "k_out and k");
+    apart(ko, q, "k_out and q");
+    apart(ko, v, "k_out and v");
+    apart(ko, qo, "k_out and q_out");
+  }
+  for (int i = 0; i < n_held; ++i) {
+    apart(qo, held[i], "q_out and the cache's pages");
+    apart(ko, held[i], "k_out and the cache's pages");
+    for (int j = 0; j < i; ++j) apart(held[i], held[j], "cache k and v");
+  }
+  aligned(a->pos, 4, "pos");
+  if (c) {
+    aligned(a->seqs, 4, "seqs");
+    aligned(a->at, 4, "at");
+  }
+  return true;
+}
+
+// A cache in 8 bits: what it has in common with pages of the dtype.
+fv_pages check_quant(const fv_quant_pages* c) {
+  need(c, "cache");
+  const fv_pages p = as_pages(*c);
+  check_cache(&p);
+  need(c->k_scale, "cache k_scale");
+  need(c->v_scale, "cache v_scale");
+  return p;
+}
+// The codes and scales of a layer, or of n_layers from it on: keys, values, their scales.
+struct Held {
+  Span at[4];
+  Held(const fv_quant_pages& c, int layer, int layers) {
+    const size_t blocks = block_of(c.n_pages, c.n_kv_heads, 0, c.page_len, 0);
+    void* const of[4] = {c.k, c.v, c.k_scale, c.v_scale};
+    for (int i = 0; i < 4; ++i) {
+      const size_t bytes = blocks * (i < 2 ? kBlock * c.head_dim : 1);
+      at[i] = run_of(static_cast<const char*>(of[i]) + layer * bytes, layers, bytes);
+    }
+  }
+};
+
+// Outputs of an attention over a cache, its workspace and what it reads.
+void check_apart(const Span& out, const Span& q, const Span* held, int n_held, const void* work,
+                 size_t work_bytes, size_t needs) {
+  apart(out, q, "out and q");
+  for (int i = 0; i < n_held; ++i) apart(out, held[i], "out and the cache's pages");
+  if (!needs) return;
+  aligned(work, 16, "work");
+  if (work_bytes < needs)
+    bad("work holds " + std::to_string(work_bytes) + " bytes, " + std::to_string(needs) + " are needed");
+  const Span w = run_of(work, 1, needs);
+  apart(w, out, "work and out");
+  apart(w, q, "work and q");
+  for (int i = 0; i < n_held; ++i) apart(w, held[i], "work and the cache's pages");
+}
+
+int keys_planned(int max_len, const fv_quant_pages& c) {
+  const int holds = c.max_pages * c.page_len;
+  return max_len > 0 && max_len < holds ? max_len : holds;
+}
+PagedPlan quant_plan(const fv_paged_args& a, const fv_quant_pages& c) {
+  return plan_quant(a.n, a.n_q_heads, c.n_kv_heads, c.head_dim, keys_planned(a.max_len, c));
+}
+
+// Whether there is work.
+bool check_part(const fv_part_args* a, const fv_quant_pages* c) {
+  need(a, "args");
+  check_quant(c);
+  check_heads(a->n_q_heads, c->n_kv_heads, c->head_dim);
+  if (a->n_seqs < 0 || a->n_seqs > 65536) bad("n_seqs must be 0 to 65536");
+  if (a->n_q < 0) bad("n_q must not be negative");
+  if ((int64_t)a->n_q * a->n_q_heads > 1 << 28) bad("n_q * n_q_heads must be at most 2^28");
+  if ((int64_t)a->n_seqs * c->n_kv_heads > 1 << 22) bad("n_seqs * n_kv_heads must be at most 2^22");
+  if (a->max_len < 0) bad("max_len must not be negative");
+  if (a->causal != 0 && a->causal != 1) bad("causal must be 0 or 1");
+  check_layer(a->layer, c->n_layers);
+  return a->n_seqs > 0 && a->n_q > 0;
+}
+
 }  // namespace
 }  // namespace fv
 
@@ -173,55 +290,14 @@ const char* fv_context_error(void) { return context_error.c_str(); }
 fv_status fv_rope_append(const fv_rope_args* a, const fv_pages* c, void* stream) {
   return guarded([&] {
     need(a, "args");
-    const size_t e = type_size(a->dtype);
-    check_heads(a->n_q_heads, a->n_kv_heads, a->head_dim);
-    if (a->n < 0 || a->n > 1 << 26) bad("n must be 0 to 2^26");
-    if (a->n_axes < 1 || a->n_axes > 4) bad("n_axes must be 1 to 4");
-    int64_t pairs = 0;
-    for (int i = 0; i < a->n_axes; ++i) {
-      if (a->sections[i] < 0) bad("sections must not be negative");
-      pairs += a->sections[i];
-    }
-    if (pairs != a->head_dim / 2) bad("sections must add up to head_dim/2");
-    if (!(a->theta > 0.f) || !std::isfinite(a->theta)) bad("theta must be positive and finite");
+    Span held[2];
     if (c) {
       check_cache(c);
-      if (c->dtype != a->dtype || c->head_dim != a->head_dim || c->n_kv_heads != a->n_kv_heads)
-        bad("the cache has another dtype, head_dim or n_kv_heads");
-      if (a->layer < 0 || a->layer >= c->n_layers) bad("layer out of range");
+      check_layer(a->layer, c->n_layers);
+      held[0] = layer_of(c->k, *c, a->layer);
+      held[1] = layer_of(c->v, *c, a->layer);
     }
-    if (a->n == 0) return;
-    const int rq = a->n_q_heads * a->head_dim, rk = a->n_kv_heads * a->head_dim;
-    const Span q = operand(a->q, a->n, a->ldq, rq, e, "q");
-    const Span k = operand(a->k, a->n, a->ldk, rk, e, "k");
-    const Span v = c ? operand(a->v, a->n, a->ldv, rk, e, "v") : Span{};
-    const Span qo = operand(a->q_out, a->n, a->ldq_out, rq, e, "q_out");
-    // an output may be its own input, and nothing else that the call reads or writes
-    const bool q_in_place = a->q_out == a->q && a->ldq_out == a->ldq;
-    if (!q_in_place) apart(qo, q, "q_out and q");
-    if (!q_in_place || c || a->k_out) apart(qo, k, "q_out and k");
-    apart(qo, v, "q_out and v");
-    Span ko;
-    if (a->k_out) {
-      ko = operand(a->k_out, a->n, a->ldk_out, rk, e, "k_out");
-      if (!(a->k_out == a->k && a->ldk_out == a->ldk)) apart(ko, k, "k_out and k");
-      apart(ko, q, "k_out and q");
-      apart(ko, v, "k_out and v");
-      apart(ko, qo, "k_out and q_out");
-    }
-    if (c) {
-      const Span pk = layer_of(c->k, *c, a->layer), pv = layer_of(c->v, *c, a->layer);
-      apart(pk, pv, "cache k and v");
-      for (const Span& p : {pk, pv}) {
-        apart(qo, p, "q_out and the cache's pages");
-        apart(ko, p, "k_out and the cache's pages");
-      }
-    }
-    aligned(a->pos, 4, "pos");
-    if (c) {
-      aligned(a->seqs, 4, "seqs");
-      aligned(a->at, 4, "at");
-    }
+    if (!check_rope(a, c, held, c ? 2 : 0)) return;
     hipStream_t s = static_cast<hipStream_t>(stream);
     OnStream on(s);
     if (a->dtype == FV_BF16)
@@ -282,23 +358,10 @@ fv_status fv_paged_attention(const fv_paged_args* a, const fv_pages* c, void* st
     const int row = a->n_q_heads * c->head_dim;
     const Span out = operand(a->out, a->n, a->ldo, row, e, "out");
     const Span q = operand(a->q, a->n, a->ldq, row, e, "q");
-    const Span pk = layer_of(c->k, *c, a->layer), pv = layer_of(c->v, *c, a->layer);
-    apart(out, q, "out and q");
-    apart(out, pk, "out and the cache's pages");
-    apart(out, pv, "out and the cache's pages");
+    const Span held[2] = {layer_of(c->k, *c, a->layer), layer_of(c->v, *c, a->layer)};
     aligned(a->seqs, 4, "seqs");
     const PagedPlan p = paged_plan(*a, *c);
-    if (p.work_bytes) {
-      aligned(a->work, 16, "work");
-      if (a->work_bytes < p.work_bytes)
-        bad("work holds " + std::to_string(a->work_bytes) + " bytes, " +
-            std::to_string(p.work_bytes) + " are needed");
-      const Span w = run_of(a->work, 1, p.work_bytes);
-      apart(w, out, "work and out");
-      apart(w, q, "work and q");
-      apart(w, pk, "work and the cache's pages");
-      apart(w, pv, "work and the cache's pages");
-    }
+    check_apart(out, q, held, 2, a->work, a->work_bytes, p.work_bytes);
     hipStream_t s = static_cast<hipStream_t>(stream);
     OnStream on(s);
     if (c->dtype == FV_BF16)
@@ -391,6 +454,177 @@ fv_status fv_pages_gather(const fv_pages* c, const int32_t* seqs, int32_t n, int
     hipStream_t s = static_cast<hipStream_t>(stream);
     OnStream on(s);
     launch_pages_gather(*c, seqs, n, ld, k_out, v_out, s);
+    check_launch();
+  });
+}
+
+// ------------------------------------------------------------ the cache in 8 bits
+
+fv_status fv_quant_append(const fv_rope_args* a, const fv_quant_pages* c, void* stream) {
+  return guarded([&] {
+    need(a, "args");
+    const fv_pages p = check_quant(c);
+    check_layer(a->layer, c->n_layers);
+    const Held held(*c, a->layer, 1);
+    if (!check_rope(a, &p, held.at, 4)) return;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    OnStream on(s);
+    if (a->dtype == FV_BF16)
+      launch_quant_append<bf16_t>(*a, *c, s);
+    else
+      launch_quant_append<float>(*a, *c, s);
+    check_launch();
+  });
+}
+
+fv_status fv_quant_attention_workspace(const fv_paged_args* a, const fv_quant_pages* c, size_t* bytes) {
+  return guarded([&] {
+    need(bytes, "bytes");
+    const fv_pages p = check_quant(c);
+    check_paged(a, &p);
+    *bytes = a->n ? quant_plan(*a, *c).work_bytes : 0;
+  });
+}
+
+fv_status fv_quant_attention(const fv_paged_args* a, const fv_quant_pages* c, void* stream) {
+  return guarded([&] {
+    const fv_pages pages = check_quant(c);
+    check_paged(a, &pages);
+    if (!(a->scale > 0.f) || !std::isfinite(a->scale)) bad("scale must be positive and finite");
+    if (a->n == 0) return;
+    const size_t e = type_size(c->dtype);
+    const int row = a->n_q_heads * c->head_dim;
+    const Span out = operand(a->out, a->n, a->ldo, row, e, "out");
+    const Span q = operand(a->q, a->n, a->ldq, row, e, "q");
+    aligned(a->seqs, 4, "seqs");
+    const PagedPlan p = quant_plan(*a, *c);
+    check_apart(out, q, Held(*c, a->layer, 1).at, 4, a->work, a->work_bytes, p.work_bytes);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    OnStream on(s);
+    if (c->dtype == FV_BF16)
+      launch_quant_paged<bf16_t>(*a, *c, p, s);
+    else
+      launch_quant_paged<float>(*a, *c, p, s);
+    check_launch();
+  });
+}
+
+fv_status fv_quant_part_workspace(const fv_part_args* a, const fv_quant_pages* c, size_t* bytes) {
+  return guarded([&] {
+    need(bytes, "bytes");
+    *bytes = check_part(a, c) ? plan_part(*a, *c, keys_planned(a->max_len, *c)).work_bytes : 0;
+  });
+}
+
+fv_status fv_quant_part_attention(const fv_part_args* a, const fv_quant_pages* c, void* stream) {
+  return guarded([&] {
+    const bool work = check_part(a, c);
+    if (!(a->scale > 0.f) || !std::isfinite(a->scale)) bad("scale must be positive and finite");
+    if (!work) return;
+    const size_t e = type_size(c->dtype);
+    const int row = a->n_q_heads * c->head_dim;
+    const Span out = operand(a->out, a->n_q, a->ldo, row, e, "out");
+    const Span q = operand(a->q, a->n_q, a->ldq, row, e, "q");
+    aligned(a->cu_q, 4, "cu_q");
+    aligned(a->seqs, 4, "seqs");
+    const PartPlan p = plan_part(*a, *c, keys_planned(a->max_len, *c));
+    check_apart(out, q, Held(*c, a->layer, 1).at, 4, a->work, a->work_bytes, p.work_bytes);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    OnStream on(s);
+    if (c->dtype == FV_BF16)
+      launch_quant_part<bf16_t>(*a, *c, p, s);
+    else
+      launch_quant_part<float>(*a, *c, p, s);
+    check_launch();
+  });
+}
+
+fv_status fv_quant_workspace(const fv_quant_pages* c, size_t* bytes) {
+  return guarded([&] {
+    need(bytes, "bytes");
+    *bytes = pages_work_ints(check_quant(c)) * 4;
+  });
+}
+
+fv_status fv_quant_grow(const fv_quant_pages* c, const int32_t* seqs, const int32_t* add, int32_t n,
+                        int32_t* status, void* work, void* stream) {
+  return guarded([&] {
+    const fv_pages p = check_quant(c);
+    check_list(&p, seqs, n, "seqs");
+    if (n) aligned(add, 4, "add");
+    aligned(status, 4, "status");
+    aligned(work, 16, "work");
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    OnStream on(s);
+    launch_pages_grow(p, seqs, add, n, status, static_cast<int*>(work), s);
+    check_launch();
+  });
+}
+
+fv_status fv_quant_fork(const fv_quant_pages* c, const int32_t* parents, const int32_t* children,
+                        int32_t n, int32_t* status, void* work, void* stream) {
+  return guarded([&] {
+    const fv_pages p = check_quant(c);
+    check_list(&p, parents, n, "parents");
+    if (n) aligned(children, 4, "children");
+    aligned(status, 4, "status");
+    aligned(work, 16, "work");
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    OnStream on(s);
+    launch_pages_fork(p, parents, children, n, status, static_cast<int*>(work), s, scales_of(*c));
+    check_launch();
+  });
+}
+
+fv_status fv_quant_free(const fv_quant_pages* c, const int32_t* seqs, int32_t n, int32_t* status,
+                        void* stream) {
+  return guarded([&] {
+    const fv_pages p = check_quant(c);
+    check_list(&p, seqs, n, "seqs");
+    aligned(status, 4, "status");
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    OnStream on(s);
+    launch_pages_free(p, seqs, n, status, s);
+    check_launch();
+  });
+}
+
+fv_status fv_quant_compact(const fv_quant_pages* c, int32_t* used, void* work, void* stream) {
+  return guarded([&] {
+    const fv_pages p = check_quant(c);
+    aligned(used, 4, "used");
+    aligned(work, 16, "work");
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    OnStream on(s);
+    launch_pages_compact(p, used, static_cast<int*>(work), s, scales_of(*c));
+    check_launch();
+  });
+}
+
+fv_status fv_quant_gather(const fv_quant_pages* c, const int32_t* seqs, int32_t n, int32_t ld,
+                          void* k_out, void* v_out, void* stream) {
+  return guarded([&] {
+    check_quant(c);
+    if (n < 0 || n > 65536) bad("n must be 0 to 65536");
+    if (ld < 0) bad("ld must not be negative");
+    if (n == 0 || ld == 0) return;
+    aligned(seqs, 4, "seqs");
+    aligned(k_out, 16, "k_out");
+    aligned(v_out, 16, "v_out");
+    const size_t row = (size_t)c->n_kv_heads * c->head_dim * type_size(c->dtype);
+    const size_t rows = (size_t)c->n_layers * n * ld;
+    const Span ko = run_of(k_out, rows, row), vo = run_of(v_out, rows, row);
+    apart(ko, vo, "k_out and v_out");
+    for (const Span& held : Held(*c, 0, c->n_layers).at) {
+      apart(ko, held, "k_out and the cache's pages");
+      apart(vo, held, "v_out and the cache's pages");
+    }
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    OnStream on(s);
+    if (c->dtype == FV_BF16)
+      launch_quant_gather<bf16_t>(*c, seqs, n, ld, k_out, v_out, s);
+    else
+      launch_quant_gather<float>(*c, seqs, n, ld, k_out, v_out, s);
     check_launch();
   });
 }

@@ -26,43 +26,10 @@
 // Measured (a read of memory alone reaches 6.2 TB/s): 192 rows of 1 to 8191 keys, heads
 // 32/8 of 128, 524 us (6.2 TB/s); 192 of 1 to 16000, 8/1 of 256, 290 us (5.5); 64 of 816,
 // 14 us; 1 of 816, 11 us, as a caller sees them.
-#include "fv_context.h"
+#include "fv_paged.h"
 
 namespace fv {
 namespace {
-
-constexpr int kPagedWaves = 4;
-constexpr float kLog2e = 1.4426950408889634f;
-
-// Largest of the lanes l, l ^ 16, l ^ 32, l ^ 48.
-__device__ __forceinline__ float max_xor16_32(float x) {
-  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  const float y = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(y), __float_as_uint(y), false, false);
-  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-
-struct PagedCall {
-  const void *q, *k, *v;  // the pools of the layer
-  void* out;
-  const int *seqs, *table, *len;
-  float* part;  // [n][n_chunks][heads][DH] sums, then [n][n_chunks][heads][2] maximum and sum
-  float* stat;
-  int ldq, ldo, n, heads, n_kv, group, q_tiles, page_len, n_pages, max_seqs, max_pages;
-  uint32_t per_page;  // 2^31 over a page's runs of 16 rows, rounded up
-  int chunk, n_chunks;
-  float scale;  // of the scores, in log2 units
-};
-
-// Chunks of a sequence that hold keys.  The last workgroup takes what lies past
-// the planned bound, should a sequence be longer.
-__device__ __forceinline__ int chunks_of(int len, int chunk, int n_chunks) {
-  const int c = (len + chunk - 1) / chunk;
-  return c < n_chunks ? c : n_chunks;
-}
-__device__ __forceinline__ int length_of(const PagedCall& a, int s) {
-  return min(max(a.len[s], 0), a.max_pages * a.page_len);
-}
 
 // A V tile in registers, and its matrix operands.  bf16: 32 keys, 8 a lane
 // (4g .. 4g+3 of either half); the head's 128-element blocks 8 elements a lane,
@@ -364,7 +331,7 @@ __global__ __launch_bounds__(64 * WAVES) void paged_join_kernel(PagedCall a) {
   __shared__ __attribute__((aligned(16))) float so[WAVES][DH];
   const int row = blockIdx.x / a.heads, qh = blockIdx.x - row * a.heads;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int s = a.seqs[row];
+  const int s = a.cu ? 0 : a.seqs[row];
   const size_t at = (size_t)row * a.n_chunks * a.heads + qh;  // of chunk 0; the next is `heads` on
   const int d = 4 * lane < DH ? 4 * lane : 0;
   auto part = [&](int c) __attribute__((always_inline)) {
@@ -373,8 +340,13 @@ __global__ __launch_bounds__(64 * WAVES) void paged_join_kernel(PagedCall a) {
   f32x4 x[FIRST];
 #pragma unroll
   for (int i = 0; i < FIRST; ++i) x[i] = part(min(wave + i * WAVES, a.n_chunks - 1));
-  if (s < 0 || s >= a.max_seqs) return;
-  const int chunks = max(1, chunks_of(length_of(a, s), a.chunk, a.n_chunks));
+  int chunks = a.n_chunks;
+  if (a.cu) {  // rows of no entry, and of one that names no sequence, are left as they were
+    if (row < a.cu[0] || row >= a.cu[a.n_entries] || a.stat[2 * at + 1] == kNoEntry) return;
+  } else {
+    if (s < 0 || s >= a.max_seqs) return;
+    chunks = max(1, chunks_of(length_of(a, s), a.chunk, a.n_chunks));
+  }
   const int mine = (chunks - wave + WAVES - 1) / WAVES;  // chunks of this wave, may be none
 
   float m = -INFINITY, l = -1.f;  // a sum of -1: no key
@@ -440,18 +412,23 @@ __global__ __launch_bounds__(64 * WAVES) void paged_join_kernel(PagedCall a) {
 }
 
 template <typename T, int DH>
-void paged_at(const PagedCall& a, size_t bytes, hipStream_t s) {
-  const int blocks = a.n * a.n_chunks * a.n_kv * a.q_tiles;
-  if (bytes > kStreamBytes)
-    hipLaunchKernelGGL((paged_kernel<T, DH, true>), dim3(blocks), dim3(64 * kPagedWaves), 0, s, a);
-  else
-    hipLaunchKernelGGL((paged_kernel<T, DH, false>), dim3(blocks), dim3(64 * kPagedWaves), 0, s, a);
+void join_at(const PagedCall& a, hipStream_t s) {
   // us of both kernels with eight waves and with one: 10.3 and 9.6 at 7 chunks, 10.6 and
   // 10.3 at 16, 10.8 and 11.5 at 32, 15 and 28 at 219 (one row, 8/1 of 256).
   if (a.n_chunks > 16)
     hipLaunchKernelGGL((paged_join_kernel<T, DH, 8>), dim3(a.n * a.heads), dim3(512), 0, s, a);
   else if (a.n_chunks > 1)
     hipLaunchKernelGGL((paged_join_kernel<T, DH, 1>), dim3(a.n * a.heads), dim3(64), 0, s, a);
+}
+
+template <typename T, int DH>
+void paged_at(const PagedCall& a, size_t bytes, hipStream_t s) {
+  const int blocks = a.n * a.n_chunks * a.n_kv * a.q_tiles;
+  if (bytes > kStreamBytes)
+    hipLaunchKernelGGL((paged_kernel<T, DH, true>), dim3(blocks), dim3(64 * kPagedWaves), 0, s, a);
+  else
+    hipLaunchKernelGGL((paged_kernel<T, DH, false>), dim3(blocks), dim3(64 * kPagedWaves), 0, s, a);
+  join_at<T, DH>(a, s);
 }
 
 }  // namespace
@@ -483,13 +460,9 @@ PagedPlan plan_paged(int n, int n_q_heads, int n_kv_heads, int head_dim, int max
   return p;
 }
 
-template <typename T>
-void launch_paged(const fv_paged_args& x, const fv_pages& c, const PagedPlan& p, hipStream_t s) {
+PagedCall paged_call(const fv_paged_args& x, const fv_pages& c, const PagedPlan& p) {
   PagedCall a{};
-  const size_t layer = (size_t)x.layer * page_row(c.n_pages, c.n_kv_heads, 0, c.page_len) * c.head_dim;
   a.q = x.q;
-  a.k = static_cast<const T*>(c.k) + layer;
-  a.v = static_cast<const T*>(c.v) + layer;
   a.out = x.out;
   a.seqs = x.seqs;
   a.table = c.table;
@@ -511,6 +484,27 @@ void launch_paged(const fv_paged_args& x, const fv_pages& c, const PagedPlan& p,
   a.chunk = p.chunk;
   a.n_chunks = p.n_chunks;
   a.scale = x.scale * kLog2e;
+  return a;
+}
+
+template <typename T>
+void launch_paged_join(const PagedCall& a, int head_dim, hipStream_t s) {
+  switch (head_dim) {
+    case 64: return join_at<T, 64>(a, s);
+    case 128: return join_at<T, 128>(a, s);
+    case 192: return join_at<T, 192>(a, s);
+    default: return join_at<T, 256>(a, s);
+  }
+}
+template void launch_paged_join<bf16_t>(const PagedCall&, int, hipStream_t);
+template void launch_paged_join<float>(const PagedCall&, int, hipStream_t);
+
+template <typename T>
+void launch_paged(const fv_paged_args& x, const fv_pages& c, const PagedPlan& p, hipStream_t s) {
+  PagedCall a = paged_call(x, c, p);
+  const size_t layer = (size_t)x.layer * page_row(c.n_pages, c.n_kv_heads, 0, c.page_len) * c.head_dim;
+  a.k = static_cast<const T*>(c.k) + layer;
+  a.v = static_cast<const T*>(c.v) + layer;
   // what the call may read: the keys and values planned for, which a layer's pages bound
   const size_t key = 2 * (size_t)c.n_kv_heads * c.head_dim * sizeof(T);
   const size_t planned = (size_t)x.n * p.keys * key, pages = (size_t)c.n_pages * c.page_len * key;

@@ -20,17 +20,14 @@ struct RopeCall {
 };
 
 // A workgroup first forms the cosines and sines of its tokens, once for all
-// heads: pair i turns by pos * theta^(-2i/DH), taken in turns (over 2 pi) in 64
-// bits, of which only the fraction is rounded to fp32.  Then each thread takes
-// 16 bytes of a head's first half and the 16 that they are paired with.  Memory bounds
-// it: 38 thousand tokens, heads 8/1 of 256, 78 us (388 MB, 4.9 TB/s, as a copy has);
+// heads (RopeAngles).  Then each thread takes 16 bytes of a head's first half and
+// the 16 that they are paired with.  Memory bounds it: 38 thousand tokens, heads 8/1 of 256, 78 us (388 MB, 4.9 TB/s, as a copy has);
 // 64 tokens 3.8 us, a launch and one trip to memory.
 template <typename T, int DH>
 __global__ __launch_bounds__(kRopeThreads) void rope_append_kernel(RopeCall r) {
   constexpr int HALF = DH / 2;
   constexpr int VE = 16 / (int)sizeof(T);
   constexpr int PIECES = HALF / VE;           // 16-byte pieces of half a head
-  constexpr int TP = kRopeThreads / HALF;     // tokens per pass over the angles
   __shared__ __attribute__((aligned(16))) float cs[kRopeTokens][HALF], sn[kRopeTokens][HALF];
   __shared__ long long slot[kRopeTokens];     // row of the token's place for kv head 0, or -1
 
@@ -49,21 +46,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_append_kernel(RopeCall r) {
     }
     slot[tid] = row;
   }
-  {
-    const int i = tid % HALF;
-    int axis = 0, end = a.sections[0];
-    while (axis < a.n_axes - 1 && i >= end) end += a.sections[++axis];
-    const double turns = exp2(-r.log2_theta * (2.0 * i / DH)) * 0.15915494309189535;
-    if (tid < TP * HALF)
-      for (int t = tid / HALF; t < nt; t += TP) {
-        double x = (double)a.pos[(size_t)axis * a.n + t0 + t] * turns;
-        x -= rint(x);
-        float s, c;
-        sincospif(2.0f * (float)x, &s, &c);
-        cs[t][i] = c;
-        sn[t][i] = s;
-      }
-  }
+  RopeAngles<DH>(a, r.log2_theta).form(t0, 0, nt, cs, sn);
   __syncthreads();
 
   const int hk = a.n_q_heads, hv = hk + a.n_kv_heads;
@@ -414,10 +397,11 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(fv_pages c, con
 }
 
 // Block (i, 0) writes the child's bookkeeping; blocks (i, 1 + 2 l + kv) copy the
-// rows in use of the parent's part-filled last page, in layer l.
+// rows in use of the parent's part-filled last page, in layer l: in 8 bits the blocks of
+// 16 that hold them, and their scales.
 __global__ __launch_bounds__(256) void fork_apply_kernel(fv_pages c, const int* parents,
                                                          const int* children, const int* work,
-                                                         int list, int row16) {
+                                                         int list, int row16, Scales q) {
   if (work[0] != FV_PAGES_OK) return;
   const int i = blockIdx.x, tid = threadIdx.x;
   const int ps = parents[i], len = c.len[ps];
@@ -446,13 +430,21 @@ __global__ __launch_bounds__(256) void fork_apply_kernel(fv_pages c, const int* 
   u32x4* pool = static_cast<u32x4*>((blockIdx.y - 1) & 1 ? c.v : c.k);
   const size_t base = (size_t)l * c.n_pages;
   const size_t page16 = (size_t)c.n_kv_heads * c.page_len * row16;  // 16-byte pieces of a page
-  const u32x4* src = pool + (base + from[full]) * page16;
-  u32x4* dst = pool + (base + A[A[list + i]]) * page16;
-  const int run = part * row16;  // pieces in use of one head
+  const size_t src_page = base + from[full], dst_page = base + A[A[list + i]];
+  const u32x4* src = pool + src_page * page16;
+  u32x4* dst = pool + dst_page * page16;
+  const int blocks = (part + 15) / 16;
+  const int run = (q.k ? 16 * blocks : part) * row16;  // pieces in use of one head
   for (int x = tid; x < run * c.n_kv_heads; x += 256) {
     const int h = x / run;
     const size_t at = (size_t)h * c.page_len * row16 + (x - h * run);
     dst[at] = src[at];
+  }
+  if (q.k) {
+    uint8_t* scales = (blockIdx.y - 1) & 1 ? q.v : q.k;
+    const int per = c.page_len / 16, all = c.n_kv_heads * per;
+    for (int x = tid; x < all; x += 256)
+      if (x % per < blocks) scales[dst_page * all + x] = scales[src_page * all + x];
   }
 }
 
@@ -579,7 +571,7 @@ __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(fv_pages c, 
 // copy: 672 MB in 132 us (5.1 TB/s).
 template <bool STREAM>
 __global__ __launch_bounds__(256) void compact_apply_kernel(fv_pages c, const int* work, int list,
-                                                            int row16) {
+                                                            int row16, Scales q) {
   const int moves = work[0], tid = threadIdx.x;
   const int* A = work + kPagesHeader;
   if (blockIdx.y == 0) {
@@ -606,6 +598,11 @@ __global__ __launch_bounds__(256) void compact_apply_kernel(fv_pages c, const in
     const u32x4* src = pool + (base + B[i]) * page16;
     u32x4* dst = pool + (base + A[i]) * page16;
     for (int x = tid; x < page16; x += 256) store_piece<STREAM>(dst + x, load_piece<STREAM>(src + x));
+    if (q.k) {
+      uint8_t* scales = (blockIdx.y - 1) & 1 ? q.v : q.k;
+      const int all = c.n_kv_heads * (c.page_len / 16);
+      for (int x = tid; x < all; x += 256) scales[(base + A[i]) * all + x] = scales[(base + B[i]) * all + x];
+    }
   }
 }
 
@@ -637,10 +634,12 @@ __global__ __launch_bounds__(256) void gather_kernel(fv_pages c, const int* seqs
   }
 }
 
-int row_pieces(const fv_pages& c) { return c.head_dim * (c.dtype == FV_BF16 ? 2 : 4) / 16; }
+int row_pieces(const fv_pages& c, const Scales& q = {}) {
+  return c.head_dim * (q.k ? 1 : c.dtype == FV_BF16 ? 2 : 4) / 16;
+}
 // Keys and values of n tokens in every layer.
-size_t token_bytes(const fv_pages& c, size_t n) {
-  return 2 * n * c.n_layers * c.n_kv_heads * row_pieces(c) * 16;
+size_t token_bytes(const fv_pages& c, size_t n, const Scales& q = {}) {
+  return 2 * n * c.n_layers * c.n_kv_heads * row_pieces(c, q) * 16;
 }
 
 template <typename T, int DH>
@@ -694,13 +693,13 @@ void launch_pages_grow(const fv_pages& c, const int* seqs, const int* add, int n
 }
 
 void launch_pages_fork(const fv_pages& c, const int* parents, const int* children, int n,
-                       int* status, int* work, hipStream_t s) {
+                       int* status, int* work, hipStream_t s, const Scales& q) {
   const int list = (int)pages_list(c);
   hipLaunchKernelGGL(fork_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, c, parents, children, n,
                      status, work, list);
   if (n)
     hipLaunchKernelGGL(fork_apply_kernel, dim3(n, 1 + 2 * c.n_layers), dim3(256), 0, s, c, parents,
-                       children, work, list, row_pieces(c));
+                       children, work, list, row_pieces(c, q), q);
 }
 
 void launch_pages_free(const fv_pages& c, const int* seqs, int n, int* status, hipStream_t s) {
@@ -709,15 +708,15 @@ void launch_pages_free(const fv_pages& c, const int* seqs, int n, int* status, h
     hipLaunchKernelGGL(free_apply_kernel, dim3(n), dim3(256), 0, s, c, seqs, status);
 }
 
-void launch_pages_compact(const fv_pages& c, int* used, int* work, hipStream_t s) {
+void launch_pages_compact(const fv_pages& c, int* used, int* work, hipStream_t s, const Scales& q) {
   const int list = (int)pages_list(c);
   hipLaunchKernelGGL(compact_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, c, used, work, list);
   const int most = c.n_pages / 2 > 1 ? c.n_pages / 2 : 1;  // no more pages than holes can move
   // at most half of the pages are read and as many written
-  const bool stream = token_bytes(c, (size_t)c.n_pages * c.page_len) > kStreamBytes;
+  const bool stream = token_bytes(c, (size_t)c.n_pages * c.page_len, q) > kStreamBytes;
   hipLaunchKernelGGL(stream ? compact_apply_kernel<true> : compact_apply_kernel<false>,
                      dim3(most < 1024 ? most : 1024, 1 + 2 * c.n_layers), dim3(256), 0, s, c, work,
-                     list, row_pieces(c));
+                     list, row_pieces(c, q), q);
 }
 
 void launch_pages_gather(const fv_pages& c, const int* seqs, int n, int ld, void* k_out,

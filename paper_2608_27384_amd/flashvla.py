@@ -37,6 +37,9 @@ EXPORTED = (
     "fv_rope_append", "fv_prompt_attention", "fv_paged_attention_workspace", "fv_paged_attention",
     "fv_pages_workspace", "fv_pages_grow", "fv_pages_fork", "fv_pages_free", "fv_pages_compact",
     "fv_pages_gather", "fv_context_error",
+    "fv_quant_append", "fv_quant_attention_workspace", "fv_quant_attention",
+    "fv_quant_part_workspace", "fv_quant_part_attention", "fv_quant_workspace", "fv_quant_grow",
+    "fv_quant_fork", "fv_quant_free", "fv_quant_compact", "fv_quant_gather",
 )
 
 
@@ -79,6 +82,19 @@ class FvPagedArgs(ctypes.Structure):
     _fields_ = [("q", c_void_p), ("out", c_void_p), ("ldq", c_int32), ("ldo", c_int32),
                 ("seqs", c_void_p)] + [
         (n, c_int32) for n in ("n", "n_q_heads", "layer", "max_len")] + [
+        ("scale", c_float), ("work", c_void_p), ("work_bytes", c_size_t)]
+
+
+class FvQuantPages(ctypes.Structure):
+    _fields_ = [(n, c_int32) for n in ("dtype", "n_layers", "n_kv_heads", "head_dim", "page_len",
+                                       "n_pages", "max_seqs", "max_pages")] + [
+        (n, c_void_p) for n in ("k", "v", "k_scale", "v_scale", "table", "len", "refs")]
+
+
+class FvPartArgs(ctypes.Structure):
+    _fields_ = [("q", c_void_p), ("out", c_void_p), ("ldq", c_int32), ("ldo", c_int32),
+                ("cu_q", c_void_p), ("seqs", c_void_p)] + [
+        (n, c_int32) for n in ("n_seqs", "n_q", "n_q_heads", "layer", "max_len", "causal")] + [
         ("scale", c_float), ("work", c_void_p), ("work_bytes", c_size_t)]
 
 
@@ -145,6 +161,22 @@ def lib() -> ctypes.CDLL:
             "fv_pages_gather": ([POINTER(FvPages), c_void_p, c_int32, c_int32, c_void_p, c_void_p,
                                  c_void_p], S),
             "fv_context_error": ([], c_char_p),
+            "fv_quant_append": ([POINTER(FvRopeArgs), POINTER(FvQuantPages), c_void_p], S),
+            "fv_quant_attention_workspace": ([POINTER(FvPagedArgs), POINTER(FvQuantPages),
+                                              POINTER(c_size_t)], S),
+            "fv_quant_attention": ([POINTER(FvPagedArgs), POINTER(FvQuantPages), c_void_p], S),
+            "fv_quant_part_workspace": ([POINTER(FvPartArgs), POINTER(FvQuantPages),
+                                         POINTER(c_size_t)], S),
+            "fv_quant_part_attention": ([POINTER(FvPartArgs), POINTER(FvQuantPages), c_void_p], S),
+            "fv_quant_workspace": ([POINTER(FvQuantPages), POINTER(c_size_t)], S),
+            "fv_quant_grow": ([POINTER(FvQuantPages), c_void_p, c_void_p, c_int32, c_void_p,
+                               c_void_p, c_void_p], S),
+            "fv_quant_fork": ([POINTER(FvQuantPages), c_void_p, c_void_p, c_int32, c_void_p,
+                               c_void_p, c_void_p], S),
+            "fv_quant_free": ([POINTER(FvQuantPages), c_void_p, c_int32, c_void_p, c_void_p], S),
+            "fv_quant_compact": ([POINTER(FvQuantPages), c_void_p, c_void_p, c_void_p], S),
+            "fv_quant_gather": ([POINTER(FvQuantPages), c_void_p, c_int32, c_int32, c_void_p,
+                                 c_void_p, c_void_p], S),
         }
         for name, (args, res) in sig.items():
             fn = getattr(L, name)
@@ -566,10 +598,10 @@ def prompt_attention(q, k, v, cu_q, cu_k, out, causal: bool = True, scale: Optio
 def rope(q, k, pos, sections: Sequence[int], q_out, k_out=None, theta: float = 10000.0,
          stream=None) -> None:
     """fv_rope_append without a cache: rotates q into q_out and, if given, k into k_out."""
-    _rope(None, 0, q, k, None, pos, None, None, sections, theta, q_out, k_out, stream)
+    _rope("fv_rope_append", None, 0, q, k, None, pos, None, None, sections, theta, q_out, k_out, stream)
 
 
-def _rope(cache, layer, q, k, v, pos, seqs, at, sections, theta, q_out, k_out, stream, *pools) -> None:
+def _rope(name, cache, layer, q, k, v, pos, seqs, at, sections, theta, q_out, k_out, stream, *pools) -> None:
     dtype, t, gpu = _dtype(q, "q"), q.dtype, q.get_device()
     _no_gradient(q, k, v, q_out, k_out)
     ldq, ldk = _rows(q, "q", t, gpu), _rows(k, "k", t, gpu)
@@ -589,8 +621,8 @@ def _rope(cache, layer, q, k, v, pos, seqs, at, sections, theta, q_out, k_out, s
                       _int32(at, "at", gpu, (n,)) if at is not None else None, n, heads, kv_heads,
                       dh, dtype, layer, axes, tuple(sections), theta)
     with _On(q.device, stream) as on:
-        _check_context(lib().fv_rope_append(byref(args), None if cache is None else byref(cache),
-                                            on.raw), "fv_rope_append")
+        _check_context(getattr(lib(), name)(byref(args), None if cache is None else byref(cache),
+                                            on.raw), name)
     _wrote(q_out, *pools) if k_out is None else _wrote(q_out, k_out, *pools)
 
 
@@ -601,8 +633,14 @@ class PageCache:
     holds the tensors and nothing else; every call is stream-ordered and may be
     captured into a HIP graph."""
 
+    _APPEND, _ATTEND, _UPKEEP = "fv_rope_append", "fv_paged_attention", "fv_pages_"
+
     def __init__(self, k, v, table, length, refs):
         dtype = _dtype(k, "k")
+        self.dtype = k.dtype
+        self._hold(FvPages, dtype, k, v, (), table, length, refs)
+
+    def _hold(self, struct, dtype, k, v, scales, table, length, refs):
         if k.dim() != 5 or not k.is_contiguous():
             _refuse("k must be contiguous [layers, pages, kv heads, page_len, head_dim]")
         if v.shape != k.shape or v.dtype != k.dtype or v.device != k.device or not v.is_contiguous():
@@ -611,14 +649,16 @@ class PageCache:
             _refuse("table must be [sequences, pages of a sequence]")
         layers, pages, heads, page_len, dh = k.shape
         gpu = k.get_device()
-        _no_gradient(k, v)
+        self.pools = (k, v) + scales  # what an append writes
+        _no_gradient(*self.pools)
         self.k, self.v, self.table, self.length, self.refs = k, v, table, length, refs
-        self.c = FvPages(dtype, layers, heads, dh, page_len, pages, table.shape[0], table.shape[1],
-                         k.data_ptr(), v.data_ptr(), _int32(table, "table", gpu),
-                         _int32(length, "length", gpu, table.shape[:1]),
-                         _int32(refs, "refs", gpu, (pages,)))
+        self.c = struct(dtype, layers, heads, dh, page_len, pages, table.shape[0], table.shape[1],
+                        *(t.data_ptr() for t in self.pools), _int32(table, "table", gpu),
+                        _int32(length, "length", gpu, table.shape[:1]),
+                        _int32(refs, "refs", gpu, (pages,)))
         need = c_size_t()
-        _check_context(lib().fv_pages_workspace(byref(self.c), byref(need)), "PageCache")
+        name = self._UPKEEP + "workspace"
+        _check_context(getattr(lib(), name)(byref(self.c), byref(need)), type(self).__name__)
         self.work_bytes = need.value  # of the upkeep's calls
 
     @classmethod
@@ -642,30 +682,39 @@ class PageCache:
         if q.device != self.k.device:
             _refuse(f"q is on {q.device}, the cache on {self.k.device}")
         self._layer(layer)
-        _rope(self.c, layer, q, k, v, pos, seqs, at, sections, theta, q if q_out is None else q_out,
-              k_out, stream, self.k, self.v)
+        _rope(self._APPEND, self.c, layer, q, k, v, pos, seqs, at, sections, theta,
+              q if q_out is None else q_out, k_out, stream, *self.pools)
 
     def attend(self, layer: int, q, seqs, out, scale: Optional[float] = None, max_len: int = 0,
                stream=None) -> None:
         """fv_paged_attention: q and out [rows, heads, head_dim], seqs int32 [rows]."""
-        t, dev, gpu = self.k.dtype, self.k.device, self.k.get_device()
+        ldq, ldo = self._queries(layer, q, out)
+        n, heads, dh = q.shape
+        args = FvPagedArgs(q.data_ptr(), out.data_ptr(), ldq, ldo,
+                           _int32(seqs, "seqs", self.k.get_device(), (n,)), n, heads, layer, max_len,
+                           dh ** -0.5 if scale is None else scale, None, 0)
+        self._attend(self._ATTEND, self._ATTEND + "_workspace", args, out, stream)
+
+    def _queries(self, layer: int, q, out):
+        """Checks an attention's queries and results; their leading dimensions."""
+        t, gpu = self.dtype, self.k.get_device()
         _no_gradient(q, out)
         ldq = _rows(q, "q", t, gpu)
         ldo = _rows(out, "out", t, gpu, q.shape)
-        n, heads, dh = q.shape
-        cache = byref(self.c)
         self._layer(layer)
-        if dh != self.c.head_dim:
-            _refuse(f"head_dim of q is {dh}, of the cache {self.c.head_dim}")
-        args = FvPagedArgs(q.data_ptr(), out.data_ptr(), ldq, ldo, _int32(seqs, "seqs", gpu, (n,)), n,
-                           heads, layer, max_len, dh ** -0.5 if scale is None else scale, None, 0)
+        if q.shape[2] != self.c.head_dim:
+            _refuse(f"head_dim of q is {q.shape[2]}, of the cache {self.c.head_dim}")
+        return ldq, ldo
+
+    def _attend(self, name: str, workspace: str, args, out, stream) -> None:
+        dev, cache = self.k.device, byref(self.c)
         with _On(dev, stream) as on:
             need, L, a = c_size_t(), lib(), byref(args)
-            _check_context(L.fv_paged_attention_workspace(a, cache, byref(need)), "fv_paged_attention")
+            _check_context(getattr(L, workspace)(a, cache, byref(need)), name)
             if need.value:
                 work = _work(need.value, dev)
                 args.work, args.work_bytes = work.data_ptr(), need.value
-            _check_context(L.fv_paged_attention(a, cache, on.raw), "fv_paged_attention")
+            _check_context(getattr(L, name)(a, cache, on.raw), name)
         _wrote(out)
 
     def _layer(self, layer: int) -> None:
@@ -673,6 +722,7 @@ class PageCache:
             _refuse(f"layer {layer} of {self.c.n_layers}")
 
     def _upkeep(self, name: str, stream, *lists, status=None, work=True, pages=False):
+        name = self._UPKEEP + name
         dev, gpu = self.k.device, self.k.get_device()
         n = lists[0].shape[0] if lists else 0
         args = [byref(self.c), *[_int32(t, name + " list", gpu, (n,)) for t in lists]]
@@ -687,26 +737,26 @@ class PageCache:
                 args.append(buf.data_ptr())
             _check_context(getattr(lib(), name)(*args, on.raw), name)
         if pages:
-            _wrote(self.table, self.length, self.refs, status, self.k, self.v)
+            _wrote(self.table, self.length, self.refs, status, *self.pools)
         else:
             _wrote(self.table, self.length, self.refs, status)
         return status
 
     def grow(self, seqs, add, status=None, stream=None):
         """fv_pages_grow; returns the status tensor (int32 [1]: FV_PAGES_*)."""
-        return self._upkeep("fv_pages_grow", stream, seqs, add, status=status)
+        return self._upkeep("grow", stream, seqs, add, status=status)
 
     def fork(self, parents, children, status=None, stream=None):
         """fv_pages_fork; returns the status tensor."""
-        return self._upkeep("fv_pages_fork", stream, parents, children, status=status, pages=True)
+        return self._upkeep("fork", stream, parents, children, status=status, pages=True)
 
     def free(self, seqs, status=None, stream=None):
         """fv_pages_free; returns the status tensor."""
-        return self._upkeep("fv_pages_free", stream, seqs, status=status, work=False)
+        return self._upkeep("free", stream, seqs, status=status, work=False)
 
     def compact(self, used=None, stream=None):
         """fv_pages_compact; returns the number of pages in use (int32 [1])."""
-        return self._upkeep("fv_pages_compact", stream, status=used, pages=True)
+        return self._upkeep("compact", stream, status=used, pages=True)
 
     def gather(self, seqs, k_out, v_out, stream=None) -> None:
         """fv_pages_gather: k_out and v_out [layers, entries, ld, kv heads, head_dim], as
@@ -714,7 +764,7 @@ class PageCache:
         c, dev = self.c, self.k.device
         _no_gradient(k_out, v_out)
         for t, what in ((k_out, "k_out"), (v_out, "v_out")):
-            if t.dim() != 5 or t.dtype != self.k.dtype or t.device != dev or not t.is_contiguous():
+            if t.dim() != 5 or t.dtype != self.dtype or t.device != dev or not t.is_contiguous():
                 _refuse(f"{what} must be contiguous [layers, entries, ld, kv heads, head_dim]")
             if t.shape[0] != c.n_layers or tuple(t.shape[3:]) != (c.n_kv_heads, c.head_dim):
                 _refuse(f"{what} has shape {tuple(t.shape)}")
@@ -722,7 +772,64 @@ class PageCache:
             _refuse("k_out and v_out must have the same shape")
         with _On(dev, stream) as on:
             ids = _int32(seqs, "seqs", self.k.get_device(), k_out.shape[1:2])
-            _check_context(lib().fv_pages_gather(byref(c), ids, k_out.shape[1], k_out.shape[2],
-                                                 k_out.data_ptr(), v_out.data_ptr(), on.raw),
-                           "fv_pages_gather")
+            name = self._UPKEEP + "gather"
+            _check_context(getattr(lib(), name)(byref(c), ids, k_out.shape[1], k_out.shape[2],
+                                                k_out.data_ptr(), v_out.data_ptr(), on.raw), name)
         _wrote(k_out, v_out)
+
+
+class QuantCache(PageCache):
+    """A paged cache in 8 bits (fv_quant_pages): k, v float8_e4m3fn [layers, pages, kv heads,
+    page_len, head_dim], which hold their blocks in the order that the header states, and
+    k_scale, v_scale float8_e8m0fnu [layers, pages, kv heads, page_len / 16], a power of two for
+    each block of 16 positions.  dtype: of the queries, keys, values and results of its calls
+    (bfloat16 or float32).  The calls are PageCache's: append quantises as it writes, gather
+    reads back exactly what the codes stand for, and attend_part takes several new tokens a
+    sequence."""
+
+    _APPEND, _ATTEND, _UPKEEP = "fv_quant_append", "fv_quant_attention", "fv_quant_"
+
+    def __init__(self, k, v, k_scale, v_scale, table, length, refs, dtype=None):
+        torch = _tmod()
+        self.dtype = torch.bfloat16 if dtype is None else dtype
+        if self.dtype not in (torch.bfloat16, torch.float32):
+            _refuse(f"dtype must be bfloat16 or float32, not {self.dtype}")
+        if k.dtype is not torch.float8_e4m3fn:
+            _refuse(f"k must be float8_e4m3fn, not {k.dtype}")
+        blocks = (*k.shape[:3], k.shape[3] // 16) if k.dim() == 5 else None
+        for t, what in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+            if t.dtype is not torch.float8_e8m0fnu or t.device != k.device or not t.is_contiguous():
+                _refuse(f"{what} must be contiguous float8_e8m0fnu on the pages' device: {t.dtype} on {t.device}")
+            if blocks is not None and tuple(t.shape) != blocks:
+                _refuse(f"{what} has shape {tuple(t.shape)}, not {blocks}")
+        self.k_scale, self.v_scale = k_scale, v_scale
+        self._hold(FvQuantPages, FV_BF16 if self.dtype is torch.bfloat16 else FV_FP32, k, v,
+                   (k_scale, v_scale), table, length, refs)
+
+    @classmethod
+    def empty(cls, n_layers: int, n_kv_heads: int, head_dim: int, n_pages: int, max_seqs: int,
+              max_pages: int, page_len: int = 16, dtype=None, device="cuda"):
+        """A fresh cache: uninitialised pages, no sequences."""
+        torch = _tmod()
+        shape = (n_layers, n_pages, n_kv_heads, page_len, head_dim)
+        k, v = (torch.empty(shape, dtype=torch.float8_e4m3fn, device=device) for _ in range(2))
+        ks, vs = (torch.empty((*shape[:3], page_len // 16), dtype=torch.float8_e8m0fnu, device=device)
+                  for _ in range(2))
+        i32 = dict(dtype=torch.int32, device=device)
+        return cls(k, v, ks, vs, torch.full((max_seqs, max_pages), -1, **i32),
+                   torch.zeros(max_seqs, **i32), torch.zeros(n_pages, **i32), dtype=dtype)
+
+    def attend_part(self, layer: int, q, cu_q, seqs, out, causal: bool = True,
+                    scale: Optional[float] = None, max_len: int = 0, stream=None) -> None:
+        """fv_quant_part_attention: q and out [rows, heads, head_dim], cu_q int32 [entries + 1],
+        seqs int32 [entries]; entry i's rows are the last tokens of sequence seqs[i]."""
+        ldq, ldo = self._queries(layer, q, out)
+        n, heads, dh = q.shape
+        gpu, entries = self.k.get_device(), cu_q.shape
+        if len(entries) != 1 or entries[0] < 1:
+            _refuse("cu_q must have entries + 1 entries")
+        args = FvPartArgs(q.data_ptr(), out.data_ptr(), ldq, ldo, _int32(cu_q, "cu_q", gpu),
+                          _int32(seqs, "seqs", gpu, (entries[0] - 1,)), entries[0] - 1, n, heads,
+                          layer, max_len, 1 if causal else 0, dh ** -0.5 if scale is None else scale,
+                          None, 0)
+        self._attend("fv_quant_part_attention", "fv_quant_part_workspace", args, out, stream)
