@@ -14,6 +14,8 @@
 #include "fv_prompt.h"
 #include "fv_quant.h"
 
+#include <type_traits>
+
 namespace fv {
 namespace {
 
@@ -34,6 +36,103 @@ struct PartCall {
 __device__ __forceinline__ uint32_t nans(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 __device__ __forceinline__ uint32_t without(uint32_t w, uint32_t n) { return w & ~(n | (n - (n >> 7))); }
 
+// What a workgroup of R rows knows of its entry, and of the chunk of keys that is its own.
+template <int R> struct PartRows {
+  const PartCall& a;
+  int lane, wave, l32, lh, kh, ch, q0, nq, nk, rows, row0, k0, k1;
+  bool named;  // the entry names a sequence
+  const int* table;
+
+  __device__ __forceinline__ explicit PartRows(const PartCall& call) : a(call) {
+    lane = threadIdx.x & 63;
+    wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    l32 = lane & 31;
+    lh = lane >> 5;
+    // the heaviest tiles of a causal part, its last ones, go first
+    int id = blockIdx.x;
+    ch = id % a.n_chunks;
+    id /= a.n_chunks;
+    kh = id % a.n_kv;
+    const int slot = a.n_slots - 1 - id / a.n_kv;
+    int first;
+    const int entry = prompt_of<R>(a, slot, &first);
+    q0 = clamped(a.cu_q, entry, a.n_q);
+    nq = max(0, clamped(a.cu_q, entry + 1, a.n_q) - q0);
+    rows = nq * a.group;
+    row0 = (slot - first) * R;
+    const int s = a.seqs[entry];
+    named = s >= 0 && s < a.max_seqs;
+    nk = named ? min(max(a.len[s], 0), a.max_pages * a.page_len) : 0;
+    table = a.table + (size_t)(named ? s : 0) * a.max_pages;
+    k0 = ch * a.chunk;
+    k1 = min(ch == a.n_chunks - 1 ? nk : min(nk, k0 + a.chunk), limit(row0 + R - 1));
+  }
+  // False: a spare slot, or one that no entry has (offsets that do not ascend from 0).
+  __device__ __forceinline__ bool any() const { return row0 >= 0 && row0 < rows; }
+  // A row sees the keys [0, limit), which do not fall from one row to the next.
+  __device__ __forceinline__ int limit(int row) const {
+    return a.causal ? min(max(nk - nq + 1 + min(row, rows - 1) / a.group, 0), nk) : nk;
+  }
+  // Token and query head of a row.
+  __device__ __forceinline__ void of(int row, int& tok, int& head) const {
+    row = min(row, rows - 1);
+    tok = row / a.group;
+    head = kh * a.group + row - tok * a.group;
+  }
+  __device__ __forceinline__ size_t partial(int tok, int head) const {
+    return ((size_t)(q0 + tok) * a.n_chunks + ch) * a.heads + head;
+  }
+  __device__ __forceinline__ void state(int tok, int head, float m, float l) const {
+    const size_t at = partial(tok, head);
+    a.stat[2 * at] = m;
+    a.stat[2 * at + 1] = l;
+  }
+  // The chunk has keys for no row: says so, where there are several.
+  __device__ __forceinline__ bool idle() const {
+    if (k1 > k0 || (a.n_chunks == 1 && named)) return false;
+    if (a.n_chunks > 1)
+      for (int r = threadIdx.x; r < R; r += blockDim.x)
+        if (row0 + r < rows) {
+          int tok, head;
+          of(row0 + r, tok, head);
+          state(tok, head, -INFINITY, named ? kNoKey : kNoEntry);
+        }
+    return true;
+  }
+  // The pool's block of the 16 keys from `key` on (page and its block), or -1.
+  __device__ __forceinline__ int block_at(int key) const {
+    if (key >= k1) return -1;
+    const int p = (int)__umulhi(key >> 3, a.per_page);
+    const int page = p < a.max_pages ? table[p] : -1;
+    return page < 0 || page >= a.n_pages ? -1 : page << 4 | (key - p * a.page_len) >> 4;
+  }
+  __device__ __forceinline__ size_t place(int at) const {
+    return block_of(max(at, 0) >> 4, a.n_kv, kh, a.page_len, max(at, 0) & 15);
+  }
+  // Whether the value of position `key` is NaN at element d of the head.
+  __device__ __forceinline__ bool is_nan(size_t block, int key, int d, int DH) const {
+    const unsigned char* p = a.v + block * (16 * DH) + 256 * (key % 16 / 4) + key % 4;
+    return (p[1024 * (d / 64) + 16 * (d % 16) + 4 * (d % 64 / 16)] & 127) == 127;
+  }
+};
+
+// 16 probabilities as bf16 operands, in PARTS parts.
+template <int PARTS>
+__device__ __forceinline__ void probabilities(const f32x16& p, u32x4 (&pf)[2][PARTS]) {
+  u16x8 w[2][PARTS];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    bf16_t at[PARTS];
+    split<PARTS>(p[r], at);
+#pragma unroll
+    for (int x = 0; x < PARTS; ++x) w[r / 8][x][r % 8] = at[x];
+  }
+#pragma unroll
+  for (int c = 0; c < 2; ++c)
+#pragma unroll
+    for (int x = 0; x < PARTS; ++x) pf[c][x] = __builtin_bit_cast(u32x4, w[c][x]);
+}
+
 constexpr int kPartWaves = 4;
 
 // 32 rows a workgroup, whose waves share a chunk's keys out, straight from memory into registers,
@@ -45,46 +144,17 @@ __global__ __launch_bounds__(64 * kPartWaves, 1) void quant_part_kernel(PartCall
   __shared__ float sm[kPartWaves][32], sl[kPartWaves][32];
   __shared__ int seen_by[kPartWaves][32];
   __shared__ __attribute__((aligned(16))) float so[kPartWaves][32 * PITCH];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int l32 = lane & 31, lh = lane >> 5;
-  // the heaviest tiles of a causal part, its last ones, go first
-  int id = blockIdx.x;
-  const int ch = id % a.n_chunks;
-  id /= a.n_chunks;
-  const int kh = id % a.n_kv, slot = a.n_slots - 1 - id / a.n_kv;
-  int first;
-  const int entry = prompt_of<32>(a, slot, &first);
-  const int q0 = clamped(a.cu_q, entry, a.n_q), nq = max(0, clamped(a.cu_q, entry + 1, a.n_q) - q0);
-  const int rows = nq * a.group, row0 = (slot - first) * 32;
-  if (row0 < 0 || row0 >= rows) return;
-  const int s = a.seqs[entry];
-  const bool named = s >= 0 && s < a.max_seqs;
-  const int nk = named ? min(max(a.len[s], 0), a.max_pages * a.page_len) : 0;
-  // A row sees the keys [0, limit), which do not fall from one row to the next.
-  auto limit = [&](int row) __attribute__((always_inline)) {
-    return a.causal ? min(max(nk - nq + 1 + min(row, rows - 1) / a.group, 0), nk) : nk;
-  };
-  const int k0 = ch * a.chunk;
-  const int k1 = min(ch == a.n_chunks - 1 ? nk : min(nk, k0 + a.chunk), limit(row0 + 31));
+  const PartRows<32> b(a);
+  if (!b.any() || b.idle()) return;
+  const int lane = b.lane, wave = b.wave, l32 = b.l32, lh = b.lh, row0 = b.row0, rows = b.rows, k0 = b.k0, k1 = b.k1;
   const int steps = max(0, (k1 - k0 + 31) / 32);
-  const int row = min(row0 + l32, rows - 1), tok = row / a.group, head = kh * a.group + row - tok * a.group;
-  const bool here = row0 + l32 < rows;
-  if (steps == 0 && a.n_chunks > 1) {  // of these keys no row sees any
-    if (wave == 0 && lh == 0 && here) {
-      const size_t at = ((size_t)(q0 + tok) * a.n_chunks + ch) * a.heads + head;
-      a.stat[2 * at] = -INFINITY;
-      a.stat[2 * at + 1] = named ? kNoKey : kNoEntry;
-    }
-    return;
-  }
-  if (!named) return;
-
-  const int* table = a.table + (size_t)s * a.max_pages;
-  const int lim = limit(row);
-  const int whole = limit(row0);  // keys that every row of the tile sees
+  int tok, head;
+  b.of(row0 + l32, tok, head);
+  const int lim = b.limit(row0 + l32);
+  const int whole = b.limit(row0);  // keys that every row of the tile sees
   u32x4 qf[NK][PARTS];
   {
-    const T* q = static_cast<const T*>(a.q) + (size_t)(q0 + tok) * a.ldq + head * DH;
+    const T* q = static_cast<const T*>(a.q) + (size_t)(b.q0 + tok) * a.ldq + head * DH;
 #pragma unroll
     for (int p = 0; p < NK; ++p) query8(q + 64 * (p / 4) + 32 * (p / 2 % 2) + 16 * lh + 8 * (p % 2), qf[p]);
   }
@@ -93,21 +163,11 @@ __global__ __launch_bounds__(64 * kPartWaves, 1) void quant_part_kernel(PartCall
   for (int d = 0; d < ND; ++d) o[d] = zeros16();
   float m = -INFINITY, l = 0.f;  // l over the lane half's keys only
   bool unruly = false, seen = false;
-  // the pool's block number of the 16 keys from `key` on, or -1
-  auto block_at = [&](int key) __attribute__((always_inline)) {
-    if (key >= k1) return -1;
-    const int p = (int)__umulhi(key >> 3, a.per_page);
-    const int page = p < a.max_pages ? table[p] : -1;
-    return page < 0 || page >= a.n_pages ? -1 : page << 4 | (key - p * a.page_len) >> 4;
-  };
-  auto place = [&](int at) __attribute__((always_inline)) {
-    return block_of(max(at, 0) >> 4, a.n_kv, kh, a.page_len, max(at, 0) & 15);
-  };
   for (int i = wave; i < steps; i += kPartWaves) {
     const int key0 = k0 + 32 * i;
-    const int at0 = __builtin_amdgcn_readfirstlane(block_at(key0));
-    const int at1 = __builtin_amdgcn_readfirstlane(block_at(key0 + 16));
-    const size_t p0 = place(at0), p1 = place(at1);
+    const int at0 = __builtin_amdgcn_readfirstlane(b.block_at(key0));
+    const int at1 = __builtin_amdgcn_readfirstlane(b.block_at(key0 + 16));
+    const size_t p0 = b.place(at0), p1 = b.place(at1);
     const bool edge = key0 + 32 > whole || key0 + 32 > k1 || at0 < 0 || at1 < 0;
     const size_t mine = l32 < 16 ? p0 : p1;  // of the lane's key
     const unsigned char* kp = a.k + mine * (16 * DH) + 64 * (l32 & 15) + 16 * lh;
@@ -161,14 +221,8 @@ __global__ __launch_bounds__(64 * kPartWaves, 1) void quant_part_kernel(PartCall
                      for (int d = 0; d < ND; ++d) o[d] *= f;
                    },
                    [](int) {});
-    u16x8 pf[2][PARTS];
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      bf16_t at[PARTS];
-      split<PARTS>(sc[r], at);
-#pragma unroll
-      for (int x = 0; x < PARTS; ++x) pf[r / 8][x][r % 8] = at[x];
-    }
+    u32x4 pf[2][PARTS];
+    probabilities<PARTS>(sc, pf);
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
@@ -177,7 +231,7 @@ __global__ __launch_bounds__(64 * kPartWaves, 1) void quant_part_kernel(PartCall
         const u32x4 v = u32x4{to_bf16<false>(lo, vs[c]), to_bf16<true>(lo, vs[c]), to_bf16<false>(hi, vs[c]),
                               to_bf16<true>(hi, vs[c])};
 #pragma unroll
-        for (int x = 0; x < PARTS; ++x) o[d] = mma32(v, __builtin_bit_cast(u32x4, pf[c][x]), o[d], bf16_t{});
+        for (int x = 0; x < PARTS; ++x) o[d] = mma32(v, pf[c][x], o[d], bf16_t{});
       }
   }
 
@@ -217,11 +271,10 @@ __global__ __launch_bounds__(64 * kPartWaves, 1) void quant_part_kernel(PartCall
     for (int i = wave; i < steps; i += kPartWaves) {
       const int from = k0 + 32 * i;
       for (int key = from; key < min(from + 32, k1); ++key) {
-        const int at = __builtin_amdgcn_readfirstlane(block_at(key & ~15));
+        const int at = __builtin_amdgcn_readfirstlane(b.block_at(key & ~15));
         if (at < 0 || (from + 32 <= whole && from + 32 <= k1)) continue;
-        const unsigned char* vp = a.v + place(at) * (16 * DH) + 256 * (key % 16 / 4) + key % 4;
         for (int d = lane; d < DH; d += 64) {
-          const bool odd = (vp[1024 * (d / 64) + 16 * (d % 16) + 4 * (d % 64 / 16)] & 127) == 127;
+          const bool odd = b.is_nan(b.place(at), key, d, DH);
           if (!__any(odd)) continue;
           for (int r = 0; r < 32; ++r)
             if (key < __shfl(lim, r) && odd) mine[r * PITCH + d] = __builtin_nanf("");
@@ -236,23 +289,274 @@ __global__ __launch_bounds__(64 * kPartWaves, 1) void quant_part_kernel(PartCall
     f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < kPartWaves; ++w) acc += *reinterpret_cast<const f32x4*>(so[w] + r * PITCH + d);
-    const int t = (row0 + r) / a.group, h = kh * a.group + row0 + r - t * a.group;
+    int t, h;
+    b.of(row0 + r, t, h);
     if (last)
-      store4(static_cast<T*>(a.out) + (size_t)(q0 + t) * a.ldo + h * DH + d, acc[0], acc[1], acc[2], acc[3]);
+      store4(static_cast<T*>(a.out) + (size_t)(b.q0 + t) * a.ldo + h * DH + d, acc[0], acc[1], acc[2], acc[3]);
     else
-      *reinterpret_cast<f32x4*>(a.part + (((size_t)(q0 + t) * a.n_chunks + ch) * a.heads + h) * DH + d) = acc;
+      *reinterpret_cast<f32x4*>(a.part + b.partial(t, h) * DH + d) = acc;
   }
-  if (!last && wave == 0 && lh == 0 && here) {
-    const size_t at = ((size_t)(q0 + tok) * a.n_chunks + ch) * a.heads + head;
-    a.stat[2 * at] = any ? top : -INFINITY;
-    a.stat[2 * at + 1] = any ? all : kNoKey;
+  if (!last && wave == 0 && lh == 0 && row0 + l32 < rows)
+    b.state(tok, head, any ? top : -INFINITY, any ? all : kNoKey);
+}
+
+// 128 rows a workgroup, 32 a wave, which share the keys: tiles of 32, as codes, go from memory
+// straight into LDS, kStages - 1 tiles ahead, and every wave converts what it multiplies (an
+// LDS read of codes is half that of bf16, and a product hides four conversions).  Which blocks
+// those are, and their scales, stands in LDS for 128 tiles at a time, the next ones looked up
+// meanwhile.
+constexpr int kStages = 4;
+constexpr int kList = 256;  // blocks of a list: a thread each
+template <typename T, int DH>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void quant_walk_kernel(PartCall a) {
+  constexpr int SLABS = DH / 64, NK = DH / 16, ND = DH / 32;
+  constexpr int PARTS = sizeof(T) == 2 ? 1 : 3;
+  constexpr int BLOCK = kBlock * DH, STAGE = 4 * BLOCK;  // bytes: of a block, of two of keys and two of values
+  constexpr bool BY_SUM = sizeof(T) == 2 && DH <= 192;
+  constexpr int RING = kStages * STAGE > 4 * 8192 ? kStages * STAGE : 4 * 8192;
+  __shared__ __attribute__((aligned(1024))) unsigned char ring[RING];
+  __shared__ __attribute__((aligned(16))) u32x2 list[2][kList];  // block, scales (keys', values' from bit 8 on)
+  const PartRows<128> b(a);
+  if (!b.any() || b.idle()) return;
+  const int lane = b.lane, wave = b.wave, l32 = b.l32, lh = b.lh, rows = b.rows, k0 = b.k0, k1 = b.k1;
+  const int wrow = b.row0 + 32 * wave;
+  const int tiles = (k1 - k0 + 31) / 32;
+  const int whole = (min(b.limit(b.row0), k1) - k0) / 32;  // tiles that every row sees (negative: none)
+  int tok, head;
+  b.of(wrow + l32, tok, head);
+  const int lim = b.limit(wrow + l32);
+  const int end = wrow < rows ? b.limit(wrow + 31) : 0;
+
+  // the list of blocks from number n on
+  auto look_up = [&](int n) __attribute__((always_inline)) { return b.block_at(k0 + 16 * (n + (int)threadIdx.x)); };
+  auto scales_of = [&](int at) __attribute__((always_inline)) {
+    const size_t x = b.place(at);
+    return (uint32_t)(scale_exponent(a.k_scale[x]) + 127) | (uint32_t)(scale_exponent(a.v_scale[x]) + 127) << 8;
+  };
+  int ahead = look_up(0);
+  list[0][threadIdx.x] = u32x2{(uint32_t)ahead, scales_of(ahead)};
+
+  u32x4 qf[NK][PARTS];
+  {
+    const T* q = static_cast<const T*>(a.q) + (size_t)(b.q0 + tok) * a.ldq + head * DH;
+#pragma unroll
+    for (int p = 0; p < NK; ++p) query8(q + 64 * (p / 4) + 32 * (p / 2 % 2) + 16 * lh + 8 * (p % 2), qf[p]);
   }
+  f32x16 o[ND];
+#pragma unroll
+  for (int d = 0; d < ND; ++d) o[d] = zeros16();
+  float m = BY_SUM ? kNoRef : -INFINITY, l = 0.f;  // l over the lane half's keys only
+  bool seen = false;
+  uint32_t odd = 0;
+
+  // Wave w brings block w % 2 of a tile's keys (w < 2) or values.  A kilobyte of keys is 16
+  // positions of 64 bytes, of which piece c lies at c ^ position / 4: the 16 positions that a read
+  // touches at one piece then lie on different banks.
+  const int from = wave < 2 ? 64 * (lane >> 2) + 16 * ((lane & 3) ^ (lane >> 4)) : 16 * lane;
+  const unsigned char* pool = wave < 2 ? a.k : a.v;
+  auto issue = [&](int t) __attribute__((always_inline)) {
+    const int at = (int)list[t / (kList / 2) & 1][2 * t % kList + (wave & 1)][0];
+    const u32x4 src = dma_source(pool + b.place(at) * BLOCK);
+    unsigned char* to = ring + t % kStages * STAGE + wave * BLOCK;
+#pragma unroll
+    for (int x = 0; x < SLABS; ++x) dma16(src, to + 1024 * x, from + 1024 * x);
+  };
+  const int kaddr = (l32 >> 4) * BLOCK + 64 * (l32 & 15) + 16 * (lh ^ (l32 >> 2 & 3));
+  const int vaddr = 2 * BLOCK + 256 * lh + 16 * (l32 & 15) + 8 * (l32 >> 4);
+
+  // A tile's two blocks, the same in every lane.
+  struct Pair {
+    int block[2];
+    uint32_t scales[2];
+  };
+  // 32 keys.  EDGE: some row may not see them all, or they are not all there.
+  auto step = [&](auto at_edge, int t, const Pair& at) __attribute__((always_inline)) {
+    constexpr bool EDGE = decltype(at_edge)::value;
+    const int key0 = k0 + 32 * t;
+    const unsigned char* tile = ring + t % kStages * STAGE;
+    const float ks = __uint_as_float(((l32 < 16 ? at.scales[0] : at.scales[1]) & 255) << 23);
+    const float vs[2] = {__uint_as_float(at.scales[0] >> 8 << 23), __uint_as_float(at.scales[1] >> 8 << 23)};
+    int kb = kaddr, vb = vaddr;
+    asm volatile("" : "+v"(kb), "+v"(vb));  // not an address each kept over the loop
+    auto key = [&](int x) __attribute__((always_inline)) {  // slab x / 2, half x % 2
+      return *reinterpret_cast<const u32x4*>(tile + (x & 1 ? kb ^ 32 : kb) + 1024 * (x / 2));
+    };
+    auto value = [&](int x, int h) __attribute__((always_inline)) {  // slab x / 2, block x % 2
+      return *reinterpret_cast<const u32x2*>(tile + vb + x % 2 * BLOCK + 1024 * (x / 2) + 512 * h);
+    };
+    f32x16 sc = zeros16();
+    u32x4 raw[2] = {key(0), key(1)};
+    u32x4 op = to_bf16x8(raw[0][0], raw[0][1], ks);
+#pragma unroll
+    for (int p = 0; p < NK; ++p) {
+      u32x4 next = op;
+      if (p + 1 < NK) next = to_bf16x8(raw[(p + 1) / 2 % 2][2 * ((p + 1) % 2)], raw[(p + 1) / 2 % 2][2 * ((p + 1) % 2) + 1], ks);
+#pragma unroll
+      for (int x = 0; x < PARTS; ++x) sc = mma32(op, qf[p][x], sc, bf16_t{});
+      if (p % 2 == 0 && p / 2 + 2 < NK / 2) raw[p / 2 % 2] = key(p / 2 + 2);
+      __builtin_amdgcn_sched_barrier(0);
+      op = next;
+    }
+    u32x2 vr[2][2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) vr[x][h] = value(x, h);
+    __builtin_amdgcn_sched_barrier(0);
+    if (EDGE) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (at.block[r / 8] < 0) sc[r] = -INFINITY;
+      hide(sc, key0, lh, lim);
+      seen = seen || (at.block[0] >= 0 && key0 < lim) || (at.block[1] >= 0 && key0 + 16 < lim);
+    } else {
+      seen = true;
+    }
+    auto rescale = [&](float f) __attribute__((always_inline)) {
+#pragma unroll
+      for (int d = 0; d < ND; ++d) o[d] *= f;
+    };
+    u32x4 pf[2][PARTS];
+    if constexpr (BY_SUM) {
+      u32x4 one[2];
+      softmax_by_sum(sc, false, key0, lh, lim, a.scale, m, l, one, rescale);
+      pf[0][0] = one[0];
+      pf[1][0] = one[1];
+    } else {
+      u32x4 unused[2];
+      softmax<float>(sc, false, key0, lh, lim, a.scale, m, l, unused, rescale, [](int) {});
+      probabilities<PARTS>(sc, pf);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int x = 0; x < 2 * SLABS; ++x) {
+      const int c = x % 2;
+      u32x2 w[2] = {vr[c][0], vr[c][1]};
+      if (EDGE) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const uint32_t n = nans(w[h][e]);
+            odd |= n;
+            w[h][e] = without(w[h][e], n);
+          }
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const u32x4 v = u32x4{to_bf16<false>(w[0][e], vs[c]), to_bf16<true>(w[0][e], vs[c]),
+                              to_bf16<false>(w[1][e], vs[c]), to_bf16<true>(w[1][e], vs[c])};
+#pragma unroll
+        for (int y = 0; y < PARTS; ++y) o[x / 2 * 2 + e] = mma32(v, pf[c][y], o[x / 2 * 2 + e], bf16_t{});
+        if (e == 0 && x + 2 < 2 * SLABS) {
+          vr[c][0] = value(x + 2, 0);
+          vr[c][1] = value(x + 2, 1);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  };
+
+  __syncthreads();  // the list is there
+  for (int t = 0; t < kStages - 1 && t < tiles; ++t) issue(t);
+  uint32_t scales = 0;
+  // Waits for tile t, brings the next one, looks up the next list a step at a time.
+  auto begin = [&](int t) __attribute__((always_inline)) {
+    if (t + kStages - 1 <= tiles)
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kStages - 2) * SLABS) : "memory");
+    else
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();  // every wave's part is there, and tile t - 1 done with
+    asm volatile("" ::: "memory");
+    if (t + kStages - 1 < tiles) issue(t + kStages - 1);
+    const int n = t / (kList / 2) + 1, at = t % (kList / 2);
+    if (n * (kList / 2) < tiles) {
+      if (at == 8) ahead = look_up(n * kList);
+      if (at == 40) scales = scales_of(ahead);
+      if (at == 72) list[n & 1][threadIdx.x] = u32x2{(uint32_t)ahead, scales};
+    }
+    const u32x4 x = *reinterpret_cast<const u32x4*>(&list[t / (kList / 2) & 1][2 * t % kList]);
+    Pair p;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      p.block[i] = __builtin_amdgcn_readfirstlane((int)x[2 * i]);
+      p.scales[i] = (uint32_t)__builtin_amdgcn_readfirstlane((int)x[2 * i + 1]);
+    }
+    return p;
+  };
+  // From the first tile on that some row does not see whole, or that has a hole, values are sifted.
+  int t = 0;
+  Pair p = begin(0);
+  for (; t < whole && (p.block[0] | p.block[1]) >= 0; p = begin(t)) {
+    if (wrow < rows) step(std::false_type{}, t, p);
+    if (++t == tiles) break;
+  }
+  const int edge = t;
+  while (t < tiles) {
+    if (k0 + 32 * t < end) step(std::true_type{}, t, p);
+    if (++t < tiles) p = begin(t);
+  }
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();  // the ring is free
+  asm volatile("" ::: "memory");
+  if (wrow >= rows) return;
+
+  if (BY_SUM) m = m == kNoRef ? -INFINITY : -m;
+  l = other_half_sum(l);
+  const bool last = a.n_chunks == 1;
+  const bool unruly = __any(odd != 0);
+  // a row that sees no key: zeros; keys that all score -inf: 0/0, as the formula has it
+  const float f = last ? (seen ? 1.0f / l : 0.f) : 1.0f;
+  const size_t mine = last ? (size_t)(b.q0 + tok) * a.ldo + head * DH : b.partial(tok, head) * DH;
+  // rows go out in slabs, through LDS
+  float* so = reinterpret_cast<float*>(ring + 8192 * wave);
+  auto place_of = [&](int r, int d) __attribute__((always_inline)) { return 64 * r + (d ^ (r & 15) << 2); };
+#pragma unroll
+  for (int s = 0; s < SLABS; ++s) {
+#pragma unroll
+    for (int d = 2 * s; d < 2 * s + 2; ++d)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int at = 16 * (2 * (j >> 1) + d % 2) + 8 * (j & 1) + 4 * lh;
+        *reinterpret_cast<f32x4*>(so + place_of(l32, at)) =
+            f32x4{o[d][4 * j] * f, o[d][4 * j + 1] * f, o[d][4 * j + 2] * f, o[d][4 * j + 3] * f};
+      }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (unruly) {  // NaN among the values at the edge: of the rows that see them
+      for (int key = k0 + 32 * edge; key < min(end, k1); ++key) {
+        const int at = __builtin_amdgcn_readfirstlane(b.block_at(key & ~15));
+        if (at < 0) continue;
+        const bool odd = b.is_nan(b.place(at), key, 64 * s + lane, DH);
+        if (!__any(odd)) continue;
+        for (int r = 0; r < 32; ++r)
+          if (key < __shfl(lim, r) && odd) so[place_of(r, lane)] = __builtin_nanf("");
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+#pragma unroll
+    for (int u = lane; u < 32 * 16; u += 64) {
+      const int r = u / 16, d = 4 * (u % 16);
+      const size_t to = (size_t)__shfl((long long)mine, r) + 64 * s + d;
+      if (wrow + r < rows) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(so + place_of(r, d));
+        if (last)
+          store4(static_cast<T*>(a.out) + to, x[0], x[1], x[2], x[3]);
+        else
+          *reinterpret_cast<f32x4*>(a.part + to) = x;
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  }
+  if (!last && lh == 0 && wrow + l32 < rows) b.state(tok, head, seen ? m : -INFINITY, seen ? l : kNoKey);
 }
 
 template <typename T, int DH>
-void part_at(const PartCall& a, hipStream_t s) {
-  const int64_t blocks = (int64_t)a.n_slots * a.n_kv * a.n_chunks;
-  hipLaunchKernelGGL((quant_part_kernel<T, DH>), dim3((unsigned)blocks), dim3(64 * kPartWaves), 0, s, a);
+void part_at(const PartCall& a, int rows, hipStream_t s) {
+  const dim3 blocks((unsigned)((int64_t)a.n_slots * a.n_kv * a.n_chunks));
+  if (rows == 32)
+    hipLaunchKernelGGL((quant_part_kernel<T, DH>), blocks, dim3(64 * kPartWaves), 0, s, a);
+  else
+    hipLaunchKernelGGL((quant_walk_kernel<T, DH>), blocks, dim3(256), 0, s, a);
 }
 
 }  // namespace
@@ -260,7 +564,8 @@ void part_at(const PartCall& a, hipStream_t s) {
 PartPlan plan_part(const fv_part_args& x, const fv_quant_pages& c, int max_keys) {
   PartPlan p{};
   const int group = x.n_q_heads / c.n_kv_heads;
-  p.rows = 32;
+  // rows of an entry on average
+  p.rows = (int64_t)x.n_q * group / x.n_seqs > 64 ? 128 : 32;
   const int64_t cols = ((int64_t)x.n_q * group / p.rows + x.n_seqs) * c.n_kv_heads;
   const int least = kPartWaves * 64;
   int64_t chunk = ((int64_t)max_keys * cols + 1023) / 1024;
@@ -310,10 +615,10 @@ void launch_quant_part(const fv_part_args& x, const fv_quant_pages& c, const Par
   a.per_page = (uint32_t)(((1ull << 31) + c.page_len / 16 - 1) / (c.page_len / 16));
   a.scale = x.scale * kLog2e;
   switch (c.head_dim) {
-    case 64: part_at<T, 64>(a, s); break;
-    case 128: part_at<T, 128>(a, s); break;
-    case 192: part_at<T, 192>(a, s); break;
-    default: part_at<T, 256>(a, s);
+    case 64: part_at<T, 64>(a, p.rows, s); break;
+    case 128: part_at<T, 128>(a, p.rows, s); break;
+    case 192: part_at<T, 192>(a, p.rows, s); break;
+    default: part_at<T, 256>(a, p.rows, s);
   }
   if (p.n_chunks > 1) {
     PagedCall j{};
