@@ -31,13 +31,17 @@ __device__ __forceinline__ u32x4 dma_source(const void* base) {
   return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)p),
                (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(p >> 32)), 0x7fffffffu, 0x00020000u};
 }
-__device__ __forceinline__ void dma16(u32x4 src, const unsigned char* lds, int off) {
-  const uint32_t to = (uint32_t)reinterpret_cast<uintptr_t>(
-      (const __attribute__((address_space(3))) unsigned char*)lds);
+__device__ __forceinline__ uint32_t lds_address(const unsigned char* p) {
+  return (uint32_t)reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) unsigned char*)p);
+}
+__device__ __forceinline__ void dma16(u32x4 src, uint32_t lds, int off) {
   asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(
-                   __builtin_amdgcn_readfirstlane((int)to)),
+                   __builtin_amdgcn_readfirstlane((int)lds)),
                "v"(off), "s"(src)
                : "memory");
+}
+__device__ __forceinline__ void dma16(u32x4 src, const unsigned char* lds, int off) {
+  dma16(src, lds_address(lds), off);
 }
 
 // 32x32 products over two 16-byte pieces a row (one of each lane half).

@@ -62,6 +62,18 @@ __device__ __forceinline__ void query8(const float* p, u32x4 (&q)[3]) {
   for (int i = 0; i < 3; ++i) q[i] = __builtin_bit_cast(u32x4, w[i]);
 }
 
+// Eight elements, rounded once.
+__device__ __forceinline__ void store8(bf16_t* p, const float (&x)[8]) {
+  u16x8 v;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = f32_to_bf16(x[e]);
+  *reinterpret_cast<u16x8*>(p) = v;
+}
+__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
+  store4(p, x[0], x[1], x[2], x[3]);
+  store4(p + 4, x[4], x[5], x[6], x[7]);
+}
+
 // Sizes and bookkeeping as those of pages of the dtype, for what reads nothing else.
 inline fv_pages as_pages(const fv_quant_pages& c) {
   return fv_pages{c.dtype, c.n_layers, c.n_kv_heads, c.head_dim, c.page_len, c.n_pages, c.max_seqs,

@@ -30,16 +30,6 @@ __device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
     for (int e = 0; e < 4; ++e) x[4 * h + e] = v[e];
   }
 }
-__device__ __forceinline__ void store8(bf16_t* p, const float (&x)[8]) {
-  u16x8 v;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = f32_to_bf16(x[e]);
-  *reinterpret_cast<u16x8*>(p) = v;
-}
-__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
-  store4(p, x[0], x[1], x[2], x[3]);
-  store4(p + 4, x[4], x[5], x[6], x[7]);
-}
 // Eight pairs of a head, of which p holds the first halves.
 template <int HALF, typename T>
 __device__ __forceinline__ void turn8(const T* p, const float* cs, const float* sn, float (&x)[8], float (&y)[8]) {

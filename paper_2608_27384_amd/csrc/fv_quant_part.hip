@@ -42,6 +42,7 @@ template <int R> struct PartRows {
   int lane, wave, l32, lh, kh, ch, q0, nq, nk, rows, row0, k0, k1;
   bool named;  // the entry names a sequence
   const int* table;
+  int page0;   // of the keys from the chunk's 16 threadIdx.x on: on its way while the length is
 
   __device__ __forceinline__ explicit PartRows(const PartCall& call) : a(call) {
     lane = threadIdx.x & 63;
@@ -54,17 +55,29 @@ template <int R> struct PartRows {
     id /= a.n_chunks;
     kh = id % a.n_kv;
     const int slot = a.n_slots - 1 - id / a.n_kv;
-    int first;
-    const int entry = prompt_of<R>(a, slot, &first);
-    q0 = clamped(a.cu_q, entry, a.n_q);
-    nq = max(0, clamped(a.cu_q, entry + 1, a.n_q) - q0);
+    int first, entry, q1, s;
+    if (a.n_seqs < 64) {  // every offset and sequence in a lane
+      const int cu = min(max(a.cu_q[min(lane, a.n_seqs)], 0), a.n_q), seq = a.seqs[min(lane, a.n_seqs - 1)];
+      const int from = (int)((long long)cu * a.group / R) + lane;  // see prompt_of
+      entry = max(1, (int)__popcll(__ballot(lane < a.n_seqs && from <= slot))) - 1;
+      first = __builtin_amdgcn_readlane(from, entry);
+      q0 = __builtin_amdgcn_readlane(cu, entry);
+      q1 = __builtin_amdgcn_readlane(cu, entry + 1);
+      s = __builtin_amdgcn_readlane(seq, entry);
+    } else {
+      entry = prompt_of<R>(a, slot, &first);
+      q0 = clamped(a.cu_q, entry, a.n_q);
+      q1 = clamped(a.cu_q, entry + 1, a.n_q);
+      s = a.seqs[entry];
+    }
+    nq = max(0, q1 - q0);
     rows = nq * a.group;
     row0 = (slot - first) * R;
-    const int s = a.seqs[entry];
     named = s >= 0 && s < a.max_seqs;
-    nk = named ? min(max(a.len[s], 0), a.max_pages * a.page_len) : 0;
     table = a.table + (size_t)(named ? s : 0) * a.max_pages;
     k0 = ch * a.chunk;
+    page0 = page_at(k0 + 16 * threadIdx.x);
+    nk = named ? min(max(a.len[s], 0), a.max_pages * a.page_len) : 0;
     k1 = min(ch == a.n_chunks - 1 ? nk : min(nk, k0 + a.chunk), limit(row0 + R - 1));
   }
   // False: a spare slot, or one that no entry has (offsets that do not ascend from 0).
@@ -99,13 +112,17 @@ template <int R> struct PartRows {
         }
     return true;
   }
-  // The pool's block of the 16 keys from `key` on (page and its block), or -1.
-  __device__ __forceinline__ int block_at(int key) const {
-    if (key >= k1) return -1;
+  // The pool's block of the 16 keys from `key` on (page and its block), or -1.  In two steps: the
+  // table's entry can be on its way before the length is known.
+  __device__ __forceinline__ int page_at(int key) const {
     const int p = (int)__umulhi(key >> 3, a.per_page);
-    const int page = p < a.max_pages ? table[p] : -1;
-    return page < 0 || page >= a.n_pages ? -1 : page << 4 | (key - p * a.page_len) >> 4;
+    return p < a.max_pages ? table[p] : -1;
   }
+  __device__ __forceinline__ int block_at(int key, int page) const {
+    const int p = (int)__umulhi(key >> 3, a.per_page);
+    return key >= k1 || page < 0 || page >= a.n_pages ? -1 : page << 4 | (key - p * a.page_len) >> 4;
+  }
+  __device__ __forceinline__ int block_at(int key) const { return key < k1 ? block_at(key, page_at(key)) : -1; }
   __device__ __forceinline__ size_t place(int at) const {
     return block_of(max(at, 0) >> 4, a.n_kv, kh, a.page_len, max(at, 0) & 15);
   }
@@ -300,93 +317,145 @@ __global__ __launch_bounds__(64 * kPartWaves, 1) void quant_part_kernel(PartCall
     b.state(tok, head, any ? top : -INFINITY, any ? all : kNoKey);
 }
 
-// 128 rows a workgroup, 32 a wave, which share the keys: tiles of 32, as codes, go from memory
-// straight into LDS, kStages - 1 tiles ahead, and every wave converts what it multiplies (an
-// LDS read of codes is half that of bf16, and a product hides four conversions).  Which blocks
-// those are, and their scales, stands in LDS for 128 tiles at a time, the next ones looked up
-// meanwhile.
-constexpr int kStages = 4;
+// Four waves with 32 rows each share the keys: tiles of 32 KG, as codes, go from memory straight
+// into LDS, STAGES - 1 tiles ahead, and every wave converts what it multiplies (an LDS read of
+// codes is half that of bf16, and a product hides four conversions).  KG 1: 128 rows, every
+// wave takes every key.  KG 2: 64 rows, half of the waves take the first 32 keys of a tile and
+// half the others, and they join at the end, for where there are not enough row tiles to fill the
+// chip.  Which blocks a tile has, and their scales, stands in LDS for 256 blocks at a time, the
+// next ones looked up meanwhile.
 constexpr int kList = 256;  // blocks of a list: a thread each
-template <typename T, int DH>
+template <typename T, int DH, int KG>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void quant_walk_kernel(PartCall a) {
-  constexpr int SLABS = DH / 64, NK = DH / 16, ND = DH / 32;
+  constexpr int SLABS = DH / 64, NK = DH / 16, ND = DH / 32, RG = 4 / KG, KT = 32 * KG;
   constexpr int PARTS = sizeof(T) == 2 ? 1 : 3;
-  constexpr int BLOCK = kBlock * DH, STAGE = 4 * BLOCK;  // bytes: of a block, of two of keys and two of values
+  constexpr int BLOCK = kBlock * DH, HALF = 2 * KG * BLOCK, STAGE = 2 * HALF;  // bytes: of a block, a tile's keys, both
+  constexpr int STAGES = 65536 / STAGE > 4 ? 4 : 65536 / STAGE;
+  constexpr int LT = kList / (2 * KG);  // tiles of a list
   constexpr bool BY_SUM = sizeof(T) == 2 && DH <= 192;
-  constexpr int RING = kStages * STAGE > 4 * 8192 ? kStages * STAGE : 4 * 8192;
-  __shared__ __attribute__((aligned(1024))) unsigned char ring[RING];
-  __shared__ __attribute__((aligned(16))) u32x2 list[2][kList];  // block, scales (keys', values' from bit 8 on)
-  const PartRows<128> b(a);
+  constexpr int JOIN = KG == 2 ? 2 * 32 * DH * 4 : 0, OUT = 4 * 8192;
+  constexpr int RING = STAGES * STAGE > JOIN ? STAGES * STAGE : JOIN;
+  static_assert(STAGES >= 2, "a tile ahead");
+  __shared__ __attribute__((aligned(1024))) unsigned char ring[RING > OUT ? RING : OUT];
+  // Blocks: where they begin in either pool (64 bits), and their scales, of keys and, from bit 8 on,
+  // of values; bit 31: there is none.
+  __shared__ __attribute__((aligned(16))) u32x4 list[2][kList];
+  __shared__ float stats[KG == 2 ? 2 * 192 : 1];
+  __shared__ int found;  // NaN among the values that were sifted
+  const PartRows<32 * RG> b(a);
   if (!b.any() || b.idle()) return;
   const int lane = b.lane, wave = b.wave, l32 = b.l32, lh = b.lh, rows = b.rows, k0 = b.k0, k1 = b.k1;
-  const int wrow = b.row0 + 32 * wave;
-  const int tiles = (k1 - k0 + 31) / 32;
-  const int whole = (min(b.limit(b.row0), k1) - k0) / 32;  // tiles that every row sees (negative: none)
-  int tok, head;
-  b.of(wrow + l32, tok, head);
-  const int lim = b.limit(wrow + l32);
-  const int end = wrow < rows ? b.limit(wrow + 31) : 0;
-
-  // the list of blocks from number n on
-  auto look_up = [&](int n) __attribute__((always_inline)) { return b.block_at(k0 + 16 * (n + (int)threadIdx.x)); };
-  auto scales_of = [&](int at) __attribute__((always_inline)) {
-    const size_t x = b.place(at);
-    return (uint32_t)(scale_exponent(a.k_scale[x]) + 127) | (uint32_t)(scale_exponent(a.v_scale[x]) + 127) << 8;
+  const int rg = wave % RG, kg = wave / RG;
+  const int wrow = b.row0 + 32 * rg;
+  const int tiles = (k1 - k0 + KT - 1) / KT;
+  const int whole = (min(b.limit(b.row0), k1) - k0) / KT;  // tiles that every row sees (negative: none)
+  // The thread, anew wherever it is used, so that nothing made of it is kept over the loop.
+  auto self = [&]() __attribute__((always_inline)) {
+    int x = threadIdx.x;
+    asm volatile("" : "+v"(x));
+    return x;
   };
-  int ahead = look_up(0);
-  list[0][threadIdx.x] = u32x2{(uint32_t)ahead, scales_of(ahead)};
+  auto entry_of = [&](int at) __attribute__((always_inline)) {
+    const size_t x = b.place(at), from = x * BLOCK;
+    return u32x4{(uint32_t)from, (uint32_t)(from >> 32),
+                 (uint32_t)(scale_exponent(a.k_scale[x]) + 127) | (uint32_t)(scale_exponent(a.v_scale[x]) + 127) << 8 |
+                     (at < 0 ? 1u << 31 : 0u), 0};
+  };
+  auto look_up = [&](int n) __attribute__((always_inline)) {  // the list of blocks from number n on
+    const int x = self();
+    list[n / kList & 1][x] = entry_of(b.block_at(k0 + 16 * (n + x)));
+  };
 
   u32x4 qf[NK][PARTS];
   {
+    int tok, head;
+    b.of(wrow + l32, tok, head);
     const T* q = static_cast<const T*>(a.q) + (size_t)(b.q0 + tok) * a.ldq + head * DH;
 #pragma unroll
     for (int p = 0; p < NK; ++p) query8(q + 64 * (p / 4) + 32 * (p / 2 % 2) + 16 * lh + 8 * (p % 2), qf[p]);
   }
+  list[0][threadIdx.x] = entry_of(b.block_at(k0 + 16 * threadIdx.x, b.page0));
   f32x16 o[ND];
 #pragma unroll
   for (int d = 0; d < ND; ++d) o[d] = zeros16();
   float m = BY_SUM ? kNoRef : -INFINITY, l = 0.f;  // l over the lane half's keys only
   bool seen = false;
-  uint32_t odd = 0;
+  if (threadIdx.x == 0) found = 0;
 
-  // Wave w brings block w % 2 of a tile's keys (w < 2) or values.  A kilobyte of keys is 16
-  // positions of 64 bytes, of which piece c lies at c ^ position / 4: the 16 positions that a read
-  // touches at one piece then lie on different banks.
-  const int from = wave < 2 ? 64 * (lane >> 2) + 16 * ((lane & 3) ^ (lane >> 4)) : 16 * lane;
+  // Waves 0 and 1 bring half of a tile's keys each, 2 and 3 of its values: KG blocks.  A kilobyte
+  // of keys is 16 positions of 64 bytes, of which piece c lies at c ^ position / 4: the 16 positions
+  // that a read touches at one piece then lie on different banks.
+  int from = wave < 2 ? 64 * (lane >> 2) + 16 * ((lane & 3) ^ (lane >> 4)) : 16 * lane;
   const unsigned char* pool = wave < 2 ? a.k : a.v;
-  auto issue = [&](int t) __attribute__((always_inline)) {
-    const int at = (int)list[t / (kList / 2) & 1][2 * t % kList + (wave & 1)][0];
-    const u32x4 src = dma_source(pool + b.place(at) * BLOCK);
-    unsigned char* to = ring + t % kStages * STAGE + wave * BLOCK;
+  const uint32_t ring0 = lds_address(ring) + wave * KG * BLOCK;
+  auto issue = [&](int t, const uint64_t (&at)[KG]) __attribute__((always_inline)) {
+    const uint32_t to = ring0 + t % STAGES * STAGE;
 #pragma unroll
-    for (int x = 0; x < SLABS; ++x) dma16(src, to + 1024 * x, from + 1024 * x);
+    for (int i = 0; i < KG; ++i) {
+      const u32x4 src = dma_source(pool + at[i]);
+#pragma unroll
+      for (int x = 0; x < SLABS; ++x) dma16(src, to + i * BLOCK + 1024 * x, from + 1024 * x);
+    }
   };
-  const int kaddr = (l32 >> 4) * BLOCK + 64 * (l32 & 15) + 16 * (lh ^ (l32 >> 2 & 3));
-  const int vaddr = 2 * BLOCK + 256 * lh + 16 * (l32 & 15) + 8 * (l32 >> 4);
+  int kaddr = (2 * kg + (l32 >> 4)) * BLOCK + 64 * (l32 & 15) + 16 * (lh ^ (l32 >> 2 & 3));
+  int vaddr = HALF + 2 * kg * BLOCK + 256 * lh + 16 * (l32 & 15) + 8 * (l32 >> 4);
+  asm volatile("" : "+v"(kaddr), "+v"(vaddr), "+v"(from));  // three registers, not what they are made of
 
-  // A tile's two blocks, the same in every lane.
-  struct Pair {
-    int block[2];
+  // Of the list, the same in every lane: the scales of the wave's two blocks of a tile, and where the
+  // blocks begin that the wave brings for a later one.  Read during a softmax, used after it.
+  struct Entries {
     uint32_t scales[2];
+    uint64_t from[KG];
+    bool holes;  // a block of the tile is not there
+  };
+  uint32_t read_scales[2 * KG];  // the wave's two first
+  u32x2 read_from[KG];
+  auto read_bases = [&](int t) __attribute__((always_inline)) {
+    const u32x4* x = &list[t / LT & 1][2 * KG * t % kList + (wave & 1) * KG];
+#pragma unroll
+    for (int i = 0; i < KG; ++i) read_from[i] = *reinterpret_cast<const u32x2*>(x + i);
+  };
+  auto read = [&](int t) __attribute__((always_inline)) {  // of tile t, and of the one that it brings
+    const u32x4* x = &list[t / LT & 1][2 * KG * t % kList];
+#pragma unroll
+    for (int i = 0; i < 2 * KG; ++i) read_scales[i] = reinterpret_cast<const uint32_t*>(x + (i ^ 2 * kg))[2];
+    read_bases(t + STAGES - 1);
+  };
+  auto bases = [&](uint64_t (&from)[KG]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < KG; ++i)
+      from[i] = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)read_from[i][1]) << 32 |
+                (uint32_t)__builtin_amdgcn_readfirstlane((int)read_from[i][0]);
+  };
+  auto settled = [&]() __attribute__((always_inline)) {
+    Entries e;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) e.scales[i] = (uint32_t)__builtin_amdgcn_readfirstlane((int)read_scales[i]);
+    e.holes = (int)(e.scales[0] | e.scales[1]) < 0;
+    if (KG == 2)
+      e.holes = e.holes || __builtin_amdgcn_readfirstlane((int)(read_scales[2 * KG - 2] | read_scales[2 * KG - 1])) < 0;
+    bases(e.from);
+    return e;
   };
   // 32 keys.  EDGE: some row may not see them all, or they are not all there.
-  auto step = [&](auto at_edge, int t, const Pair& at) __attribute__((always_inline)) {
+  // Returns the entries of the next tile.
+  auto step = [&](auto at_edge, int t, const Entries& at, int lim) __attribute__((always_inline)) {
     constexpr bool EDGE = decltype(at_edge)::value;
-    const int key0 = k0 + 32 * t;
-    const unsigned char* tile = ring + t % kStages * STAGE;
+    const int key0 = k0 + KT * t + 32 * kg;
+    const unsigned char* tile = ring + t % STAGES * STAGE;
     const float ks = __uint_as_float(((l32 < 16 ? at.scales[0] : at.scales[1]) & 255) << 23);
-    const float vs[2] = {__uint_as_float(at.scales[0] >> 8 << 23), __uint_as_float(at.scales[1] >> 8 << 23)};
-    int kb = kaddr, vb = vaddr;
-    asm volatile("" : "+v"(kb), "+v"(vb));  // not an address each kept over the loop
+    const float vs[2] = {__uint_as_float((at.scales[0] >> 8 & 255) << 23), __uint_as_float((at.scales[1] >> 8 & 255) << 23)};
     auto key = [&](int x) __attribute__((always_inline)) {  // slab x / 2, half x % 2
-      return *reinterpret_cast<const u32x4*>(tile + (x & 1 ? kb ^ 32 : kb) + 1024 * (x / 2));
+      return *reinterpret_cast<const u32x4*>(tile + (x & 1 ? kaddr ^ 32 : kaddr) + 1024 * (x / 2));
     };
     auto value = [&](int x, int h) __attribute__((always_inline)) {  // slab x / 2, block x % 2
-      return *reinterpret_cast<const u32x2*>(tile + vb + x % 2 * BLOCK + 1024 * (x / 2) + 512 * h);
+      return *reinterpret_cast<const u32x2*>(tile + vaddr + x % 2 * BLOCK + 1024 * (x / 2) + 512 * h);
     };
     f32x16 sc = zeros16();
     u32x4 raw[2] = {key(0), key(1)};
     u32x4 op = to_bf16x8(raw[0][0], raw[0][1], ks);
+    __builtin_amdgcn_s_setprio(1);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int p = 0; p < NK; ++p) {
       u32x4 next = op;
@@ -397,6 +466,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void quant_walk_kernel
       __builtin_amdgcn_sched_barrier(0);
       op = next;
     }
+    __builtin_amdgcn_s_setprio(0);
     u32x2 vr[2][2];
 #pragma unroll
     for (int x = 0; x < 2; ++x)
@@ -406,9 +476,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void quant_walk_kernel
     if (EDGE) {
 #pragma unroll
       for (int r = 0; r < 16; ++r)
-        if (at.block[r / 8] < 0) sc[r] = -INFINITY;
+        if ((int)at.scales[r / 8] < 0) sc[r] = -INFINITY;
       hide(sc, key0, lh, lim);
-      seen = seen || (at.block[0] >= 0 && key0 < lim) || (at.block[1] >= 0 && key0 + 16 < lim);
+      seen = seen || ((int)at.scales[0] >= 0 && key0 < lim) || ((int)at.scales[1] >= 0 && key0 + 16 < lim);
     } else {
       seen = true;
     }
@@ -427,125 +497,195 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void quant_walk_kernel
       softmax<float>(sc, false, key0, lh, lim, a.scale, m, l, unused, rescale, [](int) {});
       probabilities<PARTS>(sc, pf);
     }
+    read(t + 1);
+    __builtin_amdgcn_s_setprio(1);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int x = 0; x < 2 * SLABS; ++x) {
       const int c = x % 2;
-      u32x2 w[2] = {vr[c][0], vr[c][1]};
-      if (EDGE) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const uint32_t n = nans(w[h][e]);
-            odd |= n;
-            w[h][e] = without(w[h][e], n);
-          }
-      }
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const u32x4 v = u32x4{to_bf16<false>(w[0][e], vs[c]), to_bf16<true>(w[0][e], vs[c]),
-                              to_bf16<false>(w[1][e], vs[c]), to_bf16<true>(w[1][e], vs[c])};
+        const u32x4 v = u32x4{to_bf16<false>(vr[c][0][e], vs[c]), to_bf16<true>(vr[c][0][e], vs[c]),
+                              to_bf16<false>(vr[c][1][e], vs[c]), to_bf16<true>(vr[c][1][e], vs[c])};
 #pragma unroll
         for (int y = 0; y < PARTS; ++y) o[x / 2 * 2 + e] = mma32(v, pf[c][y], o[x / 2 * 2 + e], bf16_t{});
-        if (e == 0 && x + 2 < 2 * SLABS) {
+        if (e == 1 && x + 2 < 2 * SLABS) {
           vr[c][0] = value(x + 2, 0);
           vr[c][1] = value(x + 2, 1);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
     }
+    __builtin_amdgcn_s_setprio(0);
+    return settled();
   };
 
   __syncthreads();  // the list is there
-  for (int t = 0; t < kStages - 1 && t < tiles; ++t) issue(t);
-  uint32_t scales = 0;
-  // Waits for tile t, brings the next one, looks up the next list a step at a time.
+  Entries now;
+  for (int t = 0; t < STAGES - 1 && t < tiles; ++t) {
+    read_bases(t);
+    bases(now.from);
+    issue(t, now.from);
+  }
+  read(0);
+  now = settled();
+  // Takes the NaN out of a tile's values: a weight of zero does not silence them.
+  auto sift = [&](int t) __attribute__((always_inline)) {
+    unsigned char* v = ring + t % STAGES * STAGE + HALF;
+    for (int x = 16 * self(); x < HALF; x += 16 * 256) {
+      u32x4 w = *reinterpret_cast<const u32x4*>(v + x);
+      uint32_t odd = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t n = nans(w[i]);
+        odd |= n;
+        w[i] = without(w[i], n);
+      }
+      if (odd) {
+        *reinterpret_cast<u32x4*>(v + x) = w;
+        found = 1;
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  // Waits for tile t, brings a later one, looks up the next list.
   auto begin = [&](int t) __attribute__((always_inline)) {
-    if (t + kStages - 1 <= tiles)
-      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kStages - 2) * SLABS) : "memory");
+    if (t + STAGES - 1 <= tiles)
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((STAGES - 2) * KG * SLABS) : "memory");
     else
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();  // every wave's part is there, and tile t - 1 done with
     asm volatile("" ::: "memory");
-    if (t + kStages - 1 < tiles) issue(t + kStages - 1);
-    const int n = t / (kList / 2) + 1, at = t % (kList / 2);
-    if (n * (kList / 2) < tiles) {
-      if (at == 8) ahead = look_up(n * kList);
-      if (at == 40) scales = scales_of(ahead);
-      if (at == 72) list[n & 1][threadIdx.x] = u32x2{(uint32_t)ahead, scales};
+    if (t + STAGES - 1 < tiles) issue(t + STAGES - 1, now.from);
+    const int n = t / LT + 1, at = t % LT;
+    if (n * LT < tiles) {
+      if (at == LT / 2) look_up(n * kList);
     }
-    const u32x4 x = *reinterpret_cast<const u32x4*>(&list[t / (kList / 2) & 1][2 * t % kList]);
-    Pair p;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      p.block[i] = __builtin_amdgcn_readfirstlane((int)x[2 * i]);
-      p.scales[i] = (uint32_t)__builtin_amdgcn_readfirstlane((int)x[2 * i + 1]);
-    }
-    return p;
   };
-  // From the first tile on that some row does not see whole, or that has a hole, values are sifted.
   int t = 0;
-  Pair p = begin(0);
-  for (; t < whole && (p.block[0] | p.block[1]) >= 0; p = begin(t)) {
-    if (wrow < rows) step(std::false_type{}, t, p);
-    if (++t == tiles) break;
+  // The queries are there: the compiler would wait for them at their use, in every turn of the
+  // loop, and with them for the tiles that are under way.
+#pragma unroll
+  for (int i = 0; i < NK; ++i)
+#pragma unroll
+    for (int x = 0; x < PARTS; ++x) asm volatile("" : "+v"(qf[i][x]));
+  // Whole tiles; from the first one on that some row does not see whole, or that has a hole, values
+  // are sifted.
+  if (wrow >= rows) {  // a wave without rows only does its part for the others
+    for (bool sifting = false; t < tiles; ++t) {
+      begin(t);
+      sifting = sifting || t >= whole || now.holes;
+      if (sifting) sift(t);
+      read(t + 1);
+      now = settled();
+    }
+  } else {
+    for (; t < tiles; ++t) {
+      begin(t);
+      if (t >= whole || now.holes) break;
+      now = step(std::false_type{}, t, now, 0);
+    }
   }
   const int edge = t;
+  // again from here on, so that nothing of it is kept over the whole tiles
+  int row = wrow + l32, tok, head;
+  asm volatile("" : "+v"(row));
+  b.of(row, tok, head);
+  const int lim = b.limit(row);
   while (t < tiles) {
-    if (k0 + 32 * t < end) step(std::true_type{}, t, p);
-    if (++t < tiles) p = begin(t);
+    sift(t);
+    now = step(std::true_type{}, t, now, lim);
+    if (++t < tiles) begin(t);
   }
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-  __builtin_amdgcn_s_barrier();  // the ring is free
-  asm volatile("" ::: "memory");
-  if (wrow >= rows) return;
-
+  // Every load has landed and every read is done: the ring is free.
+  auto meet = [] __device__() {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  meet();
   if (BY_SUM) m = m == kNoRef ? -INFINITY : -m;
   l = other_half_sum(l);
+  const bool unruly = found;
+  if constexpr (KG == 2) {
+    f32x4* so = reinterpret_cast<f32x4*>(ring) + rg * (4 * ND * 64) + lane;
+    float* st = stats + rg * 192 + lane;
+    if (kg) {
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          so[(4 * d + j) * 64] = f32x4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]};
+      st[0] = m;
+      st[64] = l;
+      st[128] = seen;
+    }
+    meet();
+    if (!kg) {
+      const float other = st[0], now = fmaxf(m, other), ref = now == -INFINITY ? 0.f : now;
+      const float f = __builtin_amdgcn_exp2f(m - ref), g = __builtin_amdgcn_exp2f(other - ref);
+      m = now;
+      l = l * f + st[64] * g;
+      seen = seen || st[128] != 0.f;
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const f32x4 x = so[(4 * d + j) * 64];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[d][4 * j + e] = o[d][4 * j + e] * f + x[e] * g;
+        }
+    }
+    meet();
+    if (kg) return;
+  }
+  if (wrow >= rows) return;
   const bool last = a.n_chunks == 1;
-  const bool unruly = __any(odd != 0);
   // a row that sees no key: zeros; keys that all score -inf: 0/0, as the formula has it
   const float f = last ? (seen ? 1.0f / l : 0.f) : 1.0f;
   const size_t mine = last ? (size_t)(b.q0 + tok) * a.ldo + head * DH : b.partial(tok, head) * DH;
-  // rows go out in slabs, through LDS
-  float* so = reinterpret_cast<float*>(ring + 8192 * wave);
-  auto place_of = [&](int r, int d) __attribute__((always_inline)) { return 64 * r + (d ^ (r & 15) << 2); };
+  // Lane halves exchange so that a lane has 8 elements of its row side by side.
+  if (row < rows) {
 #pragma unroll
-  for (int s = 0; s < SLABS; ++s) {
+    for (int d = 0; d < ND; ++d)
 #pragma unroll
-    for (int d = 2 * s; d < 2 * s + 2; ++d)
+      for (int j = 0; j < 2; ++j) {
+        const size_t to = mine + 64 * (d / 2) + 16 * (2 * j + d % 2) + 8 * lh;
+        float x[8];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int at = 16 * (2 * (j >> 1) + d % 2) + 8 * (j & 1) + 4 * lh;
-        *reinterpret_cast<f32x4*>(so + place_of(l32, at)) =
-            f32x4{o[d][4 * j] * f, o[d][4 * j + 1] * f, o[d][4 * j + 2] * f, o[d][4 * j + 3] * f};
+        for (int e = 0; e < 4; ++e) {
+          const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(o[d][8 * j + e] * f),
+                                                          __float_as_uint(o[d][8 * j + 4 + e] * f), false, false);
+          x[e] = __uint_as_float(y[0]);
+          x[4 + e] = __uint_as_float(y[1]);
+        }
+        if (last) {
+          store8(static_cast<T*>(a.out) + to, x);
+        } else {
+          store8(a.part + to, x);
+        }
       }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    if (unruly) {  // NaN among the values at the edge: of the rows that see them
-      for (int key = k0 + 32 * edge; key < min(end, k1); ++key) {
-        const int at = __builtin_amdgcn_readfirstlane(b.block_at(key & ~15));
-        if (at < 0) continue;
-        const bool odd = b.is_nan(b.place(at), key, 64 * s + lane, DH);
+  }
+  if (unruly) {  // NaN among the values at the edge: of the rows that see them
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    for (int key = k0 + KT * edge; key < min(b.limit(wrow + 31), k1); ++key) {
+      const int at = __builtin_amdgcn_readfirstlane(b.block_at(key & ~15));
+      if (at < 0) continue;
+      for (int d = lane; d < DH; d += 64) {
+        const bool odd = b.is_nan(b.place(at), key, d, DH);
         if (!__any(odd)) continue;
-        for (int r = 0; r < 32; ++r)
-          if (key < __shfl(lim, r) && odd) so[place_of(r, lane)] = __builtin_nanf("");
-      }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    }
-#pragma unroll
-    for (int u = lane; u < 32 * 16; u += 64) {
-      const int r = u / 16, d = 4 * (u % 16);
-      const size_t to = (size_t)__shfl((long long)mine, r) + 64 * s + d;
-      if (wrow + r < rows) {
-        const f32x4 x = *reinterpret_cast<const f32x4*>(so + place_of(r, d));
-        if (last)
-          store4(static_cast<T*>(a.out) + to, x[0], x[1], x[2], x[3]);
-        else
-          *reinterpret_cast<f32x4*>(a.part + to) = x;
+        for (int r = 0; r < 32; ++r) {
+          const size_t to = (size_t)__shfl((long long)mine, r) + d;
+          if (!(key < __shfl(lim, r)) || !odd || wrow + r >= rows) continue;
+          if (last)
+            static_cast<T*>(a.out)[to] = from_f32<T>(__builtin_nanf(""));
+          else
+            a.part[to] = __builtin_nanf("");
+        }
       }
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   }
   if (!last && lh == 0 && wrow + l32 < rows) b.state(tok, head, seen ? m : -INFINITY, seen ? l : kNoKey);
 }
@@ -555,26 +695,43 @@ void part_at(const PartCall& a, int rows, hipStream_t s) {
   const dim3 blocks((unsigned)((int64_t)a.n_slots * a.n_kv * a.n_chunks));
   if (rows == 32)
     hipLaunchKernelGGL((quant_part_kernel<T, DH>), blocks, dim3(64 * kPartWaves), 0, s, a);
+  else if (rows == 64)
+    hipLaunchKernelGGL((quant_walk_kernel<T, DH, 2>), blocks, dim3(256), 0, s, a);
   else
-    hipLaunchKernelGGL((quant_walk_kernel<T, DH>), blocks, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((quant_walk_kernel<T, DH, 1>), blocks, dim3(256), 0, s, a);
 }
 
 }  // namespace
 
+// us by rows a workgroup and, in brackets, chunks, of calls captured into a graph:
+//                                          32        64        128
+// 50 tokens on 866, heads 8/1 of 256       14.4 (8)  15.5 (8)  17.6 (12)
+// 8 by 16 on 2000, 8/1 of 256              19.6 (6)  20.5 (8)  24.4 (8)
+// 64 by 4 on 2000, 8/1 of 256              29.9 (2)  27.1 (4)  27.9 (6)
+// 64 by 1 to 61 on 300 to 866, 8/1 of 256  48.5 (1)  33.3 (1)  37.0 (1)
+// 500 on 8000, 8/1 of 256                  62.5 (2)  51.9 (8)  54.8 (8)
+// 4096 on 28672, 8/1 of 256                1311 (1)  809 (1)   800 (2)
+// 32 by 1 to 100 on 100 to 3000, 32/8/128  92.7 (1)  85.3 (1)  100 (3)
+// fp32: 5 of 33 to 301, 8/2 of 64          18.8 (1)  22.7 (4)  23.6 (4)
+// 4 by 200 on 1000, 8/1 of 256             49.5 (1)  44.9 (2)  44.0 (4)
+// One workgroup a CU is enough for short walks, two for long ones, whose workgroups wait for
+// their tiles; more chunks than that cost what the join reads.
 PartPlan plan_part(const fv_part_args& x, const fv_quant_pages& c, int max_keys) {
   PartPlan p{};
-  const int group = x.n_q_heads / c.n_kv_heads;
-  // rows of an entry on average
-  p.rows = (int64_t)x.n_q * group / x.n_seqs > 64 ? 128 : 32;
-  const int64_t cols = ((int64_t)x.n_q * group / p.rows + x.n_seqs) * c.n_kv_heads;
-  const int least = kPartWaves * 64;
-  int64_t chunk = ((int64_t)max_keys * cols + 1023) / 1024;
-  chunk = (chunk + 31) / 32 * 32;
-  if (chunk < least) chunk = least;
-  int64_t chunks = (max_keys + chunk - 1) / chunk;
+  const int64_t rows = (int64_t)x.n_q * (x.n_q_heads / c.n_kv_heads);
+  auto tiles = [&](int of) { return (rows / of + (x.n_seqs + 1) / 2) * c.n_kv_heads; };  // about
+  p.rows = rows / 32 * c.n_kv_heads <= (c.dtype == FV_FP32 && c.head_dim <= 128 ? 256 : 48) ? 32
+           : tiles(128) >= 256 && max_keys >= 8192                                          ? 128
+                                                                                            : 64;
+  const int64_t n = tiles(p.rows);
+  int64_t chunks = (p.rows == 32 ? 192 : 256 + n / 2) / n;
+  if (p.rows > 32 && max_keys > 1024 * (chunks > 1 ? chunks : 1)) chunks = (512 + n / 2) / n;
+  if (chunks > max_keys / 128) chunks = max_keys / 128;
+  if (chunks < 1) chunks = 1;
+  const int64_t chunk = ((max_keys + chunks - 1) / chunks + 31) / 32 * 32;
+  chunks = (max_keys + chunk - 1) / chunk;
   // the join's grid, one of more than 2^32 threads otherwise
-  if (chunks < 1 || (int64_t)x.n_q * x.n_q_heads > 1 << 22) chunks = 1;
-  while (chunks > 1 && chunks * cols > 1 << 23) chunks /= 2;  // the last one is longer then
+  if (chunks < 1 || (int64_t)x.n_q * x.n_q_heads > 1 << 22) chunks = 1;  // the last one is longer then
   p.chunk = (int)chunk;
   p.n_chunks = (int)chunks;
   if (chunks > 1) p.work_bytes = (size_t)x.n_q * chunks * x.n_q_heads * (c.head_dim + 2) * 4;
