@@ -30,16 +30,18 @@ template <bool STREAM, typename V> __device__ __forceinline__ void store_piece(V
     *p = x;
 }
 
-// The angles of a thread of kRopeThreads: pair i turns by pos * theta^(-2i/DH), taken in turns
+// The angles of a thread of the workgroup: pair i turns by pos * theta^(-2i/DH), taken in turns
 // (over 2 pi) in 64 bits, of which only the fraction is rounded to fp32.
 template <int DH> struct RopeAngles {
-  static constexpr int HALF = DH / 2, STEP = 256 / HALF;  // tokens a pass
+  static constexpr int HALF = DH / 2;
   const int* pos;  // of the pair's axis
   double turns;
-  int i, at;  // the pair, the first token of the thread
-  __device__ __forceinline__ RopeAngles(const fv_rope_args& a, double log2_theta) {
+  int i, at, step;  // the pair, the first token of the thread, tokens a pass
+  // threads: of the workgroup, at least HALF
+  __device__ __forceinline__ RopeAngles(const fv_rope_args& a, double log2_theta, int threads) {
+    step = threads / HALF;
     i = threadIdx.x % HALF;
-    at = threadIdx.x < STEP * HALF ? threadIdx.x / HALF : 1 << 30;
+    at = threadIdx.x < step * HALF ? threadIdx.x / HALF : 1 << 30;
     int axis = 0, end = a.sections[0];
     while (axis < a.n_axes - 1 && i >= end) end += a.sections[++axis];
     pos = a.pos + (size_t)axis * a.n;
@@ -47,7 +49,7 @@ template <int DH> struct RopeAngles {
   }
   // Of the tokens from `from` to `to` behind t0.
   __device__ __forceinline__ void form(int t0, int from, int to, float (*cs)[HALF], float (*sn)[HALF]) const {
-    for (int t = from + at; t < to; t += STEP) {
+    for (int t = from + at; t < to; t += step) {
       double x = (double)pos[t0 + t] * turns;
       x -= rint(x);
       float s, c;

@@ -46,7 +46,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_append_kernel(RopeCall r) {
     }
     slot[tid] = row;
   }
-  RopeAngles<DH>(a, r.log2_theta).form(t0, 0, nt, cs, sn);
+  RopeAngles<DH>(a, r.log2_theta, kRopeThreads).form(t0, 0, nt, cs, sn);
   __syncthreads();
 
   const int hk = a.n_q_heads, hv = hk + a.n_kv_heads;
