@@ -42,9 +42,9 @@ template <int R> struct PartRows {
   int lane, wave, l32, lh, kh, ch, q0, nq, nk, rows, row0, k0, k1;
   bool named;  // the entry names a sequence
   const int* table;
-  int page0;   // of the keys from the chunk's 16 threadIdx.x on: on its way while the length is
+  int page0;   // of the chunk's key `at`: on its way while the length is
 
-  __device__ __forceinline__ explicit PartRows(const PartCall& call) : a(call) {
+  __device__ __forceinline__ PartRows(const PartCall& call, int at) : a(call) {
     lane = threadIdx.x & 63;
     wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     l32 = lane & 31;
@@ -76,7 +76,7 @@ template <int R> struct PartRows {
     named = s >= 0 && s < a.max_seqs;
     table = a.table + (size_t)(named ? s : 0) * a.max_pages;
     k0 = ch * a.chunk;
-    page0 = page_at(k0 + 16 * threadIdx.x);
+    page0 = page_at(k0 + at);
     nk = named ? min(max(a.len[s], 0), a.max_pages * a.page_len) : 0;
     k1 = min(ch == a.n_chunks - 1 ? nk : min(nk, k0 + a.chunk), limit(row0 + R - 1));
   }
@@ -153,22 +153,67 @@ __device__ __forceinline__ void probabilities(const f32x16& p, u32x4 (&pf)[2][PA
 constexpr int kPartWaves = 4;
 
 // 32 rows a workgroup, whose waves share a chunk's keys out, straight from memory into registers,
-// and join in LDS.
+// the next step's codes under way in the one before, and join in LDS.  For where there are so few
+// rows that the time is the chain of trips to memory (offsets, the table with the length, scales
+// and codes, then the join's): 50 tokens on 866 keys, 8 query heads and 1 kv head of 256, bf16, are
+// 14.0 us with the join, of which two launches are 8; 1.5 us of it are products.
 template <typename T, int DH>
 __global__ __launch_bounds__(64 * kPartWaves, 1) void quant_part_kernel(PartCall a) {
   constexpr int SLABS = DH / 64, NK = DH / 16, ND = DH / 32, PITCH = DH + 4;
   constexpr int PARTS = sizeof(T) == 2 ? 1 : 3;
+  constexpr bool AHEAD = PARTS == 1 || DH <= 128;  // a step's codes are under way in the one before it
   __shared__ float sm[kPartWaves][32], sl[kPartWaves][32];
   __shared__ int seen_by[kPartWaves][32];
   __shared__ __attribute__((aligned(16))) float so[kPartWaves][32 * PITCH];
-  const PartRows<32> b(a);
+  // Lane l looks up the block of the wave's step l / 2, half l % 2; the wave's steps are
+  // kPartWaves apart, so this is 32 of them.
+  const int ahead = 32 * ((int)threadIdx.x >> 6) + 16 * ((int)threadIdx.x & 1) + 32 * kPartWaves * (((int)threadIdx.x & 63) >> 1);
+  const PartRows<32> b(a, ahead);
   if (!b.any() || b.idle()) return;
   const int lane = b.lane, wave = b.wave, l32 = b.l32, lh = b.lh, row0 = b.row0, rows = b.rows, k0 = b.k0, k1 = b.k1;
   const int steps = max(0, (k1 - k0 + 31) / 32);
+  int at = b.block_at(k0 + ahead, b.page0);
+  auto scales_at = [&](int at) __attribute__((always_inline)) {
+    const size_t x = b.place(at);
+    return (uint32_t)a.k_scale[x] | (uint32_t)a.v_scale[x] << 8;
+  };
+  uint32_t scales = scales_at(at);
   int tok, head;
   b.of(row0 + l32, tok, head);
   const int lim = b.limit(row0 + l32);
   const int whole = b.limit(row0);  // keys that every row of the tile sees
+  struct Tile {
+    int at[2];
+    uint32_t scales[2];
+    u32x4 k[2 * SLABS];
+    u32x2 v[SLABS][2][2];  // of block c, the positions from 4 lh + 8 h on
+  };
+  auto fetch = [&](int i, Tile& t) __attribute__((always_inline)) {
+    const int j = 2 * (i / kPartWaves % 32);
+    if (j == 0 && i >= kPartWaves) {
+      at = b.block_at(k0 + 32 * (i - wave) + ahead);
+      scales = scales_at(at);
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c) t.at[c] = __builtin_amdgcn_readlane(at, j + c);
+    const size_t p0 = b.place(t.at[0]), p1 = b.place(t.at[1]);
+    const unsigned char* kp = a.k + (l32 < 16 ? p0 : p1) * (16 * DH) + 64 * (l32 & 15) + 16 * lh;
+#pragma unroll
+    for (int x = 0; x < 2 * SLABS; ++x) t.k[x] = *reinterpret_cast<const u32x4*>(kp + 1024 * (x / 2) + 32 * (x % 2));
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const unsigned char* vp = a.v + (c ? p1 : p0) * (16 * DH) + 256 * lh + 16 * (l32 & 15) + 8 * (l32 >> 4);
+#pragma unroll
+      for (int x = 0; x < SLABS; ++x)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) t.v[x][c][h] = *reinterpret_cast<const u32x2*>(vp + 1024 * x + 512 * h);
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c) t.scales[c] = __builtin_amdgcn_readlane((int)scales, j + c);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  Tile now, next;
+  if (AHEAD && wave < steps) fetch(wave, next);
   u32x4 qf[NK][PARTS];
   {
     const T* q = static_cast<const T*>(a.q) + (size_t)(b.q0 + tok) * a.ldq + head * DH;
@@ -181,28 +226,19 @@ __global__ __launch_bounds__(64 * kPartWaves, 1) void quant_part_kernel(PartCall
   float m = -INFINITY, l = 0.f;  // l over the lane half's keys only
   bool unruly = false, seen = false;
   for (int i = wave; i < steps; i += kPartWaves) {
-    const int key0 = k0 + 32 * i;
-    const int at0 = __builtin_amdgcn_readfirstlane(b.block_at(key0));
-    const int at1 = __builtin_amdgcn_readfirstlane(b.block_at(key0 + 16));
-    const size_t p0 = b.place(at0), p1 = b.place(at1);
-    const bool edge = key0 + 32 > whole || key0 + 32 > k1 || at0 < 0 || at1 < 0;
-    const size_t mine = l32 < 16 ? p0 : p1;  // of the lane's key
-    const unsigned char* kp = a.k + mine * (16 * DH) + 64 * (l32 & 15) + 16 * lh;
-    const float ks = power_of(scale_exponent(a.k_scale[mine]));
-    const float vs[2] = {power_of(scale_exponent(a.v_scale[p0])), power_of(scale_exponent(a.v_scale[p1]))};
-    u32x4 kf[2 * SLABS];
-#pragma unroll
-    for (int x = 0; x < 2 * SLABS; ++x) kf[x] = *reinterpret_cast<const u32x4*>(kp + 1024 * (x / 2) + 32 * (x % 2));
-    // values: of block c, the positions from 4 lh + 8 h on
-    u32x2 vf[SLABS][2][2];
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const unsigned char* vp = a.v + (c ? p1 : p0) * (16 * DH) + 256 * lh + 16 * (l32 & 15) + 8 * (l32 >> 4);
-#pragma unroll
-      for (int x = 0; x < SLABS; ++x)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) vf[x][c][h] = *reinterpret_cast<const u32x2*>(vp + 1024 * x + 512 * h);
+    if (AHEAD) {
+      now = next;
+      if (i + kPartWaves < steps) fetch(i + kPartWaves, next);
+    } else {
+      fetch(i, now);
     }
+    const int key0 = k0 + 32 * i, at0 = now.at[0], at1 = now.at[1];
+    const bool edge = key0 + 32 > whole || key0 + 32 > k1 || at0 < 0 || at1 < 0;
+    const float ks = power_of(scale_exponent((uint8_t)(l32 < 16 ? now.scales[0] : now.scales[1])));
+    const float vs[2] = {power_of(scale_exponent((uint8_t)(now.scales[0] >> 8))),
+                         power_of(scale_exponent((uint8_t)(now.scales[1] >> 8)))};
+    auto& kf = now.k;
+    auto& vf = now.v;
     f32x16 sc = zeros16();
 #pragma unroll
     for (int p = 0; p < NK; ++p) {
@@ -300,18 +336,26 @@ __global__ __launch_bounds__(64 * kPartWaves, 1) void quant_part_kernel(PartCall
     }
   }
   __syncthreads();
-  for (int u = threadIdx.x; u < 32 * (DH / 4); u += 64 * kPartWaves) {
-    const int r = u / (DH / 4), d = 4 * (u % (DH / 4));
-    if (row0 + r >= rows) continue;
-    f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+  constexpr int OUT = 32 * (DH / 4) / (64 * kPartWaves);
+  f32x4 sum[OUT];
 #pragma unroll
-    for (int w = 0; w < kPartWaves; ++w) acc += *reinterpret_cast<const f32x4*>(so[w] + r * PITCH + d);
+  for (int j = 0; j < OUT; ++j) {
+    const int u = threadIdx.x + 64 * kPartWaves * j;
+    const float* x = so[0] + u / (DH / 4) * PITCH + 4 * (u % (DH / 4));
+    sum[j] = *reinterpret_cast<const f32x4*>(x);
+#pragma unroll
+    for (int w = 1; w < kPartWaves; ++w) sum[j] += *reinterpret_cast<const f32x4*>(x + w * 32 * PITCH);
+  }
+#pragma unroll
+  for (int j = 0; j < OUT; ++j) {
+    const int u = threadIdx.x + 64 * kPartWaves * j, r = u / (DH / 4), d = 4 * (u % (DH / 4));
+    if (row0 + r >= rows) continue;
     int t, h;
     b.of(row0 + r, t, h);
     if (last)
-      store4(static_cast<T*>(a.out) + (size_t)(b.q0 + t) * a.ldo + h * DH + d, acc[0], acc[1], acc[2], acc[3]);
+      store4(static_cast<T*>(a.out) + (size_t)(b.q0 + t) * a.ldo + h * DH + d, sum[j][0], sum[j][1], sum[j][2], sum[j][3]);
     else
-      *reinterpret_cast<f32x4*>(a.part + b.partial(t, h) * DH + d) = acc;
+      *reinterpret_cast<f32x4*>(a.part + b.partial(t, h) * DH + d) = sum[j];
   }
   if (!last && wave == 0 && lh == 0 && row0 + l32 < rows)
     b.state(tok, head, any ? top : -INFINITY, any ? all : kNoKey);
@@ -342,7 +386,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void quant_walk_kernel
   __shared__ __attribute__((aligned(16))) u32x4 list[2][kList];
   __shared__ float stats[KG == 2 ? 2 * 192 : 1];
   __shared__ int found;  // NaN among the values that were sifted
-  const PartRows<32 * RG> b(a);
+  const PartRows<32 * RG> b(a, 16 * threadIdx.x);
   if (!b.any() || b.idle()) return;
   const int lane = b.lane, wave = b.wave, l32 = b.l32, lh = b.lh, rows = b.rows, k0 = b.k0, k1 = b.k1;
   const int rg = wave % RG, kg = wave / RG;
@@ -705,15 +749,18 @@ void part_at(const PartCall& a, int rows, hipStream_t s) {
 
 // us by rows a workgroup and, in brackets, chunks, of calls captured into a graph:
 //                                          32        64        128
-// 50 tokens on 866, heads 8/1 of 256       14.4 (8)  15.5 (8)  17.6 (12)
-// 8 by 16 on 2000, 8/1 of 256              19.6 (6)  20.5 (8)  24.4 (8)
-// 64 by 4 on 2000, 8/1 of 256              29.9 (2)  27.1 (4)  27.9 (6)
-// 64 by 1 to 61 on 300 to 866, 8/1 of 256  48.5 (1)  33.3 (1)  37.0 (1)
-// 500 on 8000, 8/1 of 256                  62.5 (2)  51.9 (8)  54.8 (8)
+// 50 tokens on 866, heads 8/1 of 256       13.9 (7)  15.4 (7)  17.5 (7)
+// 50 on 4000, 8/1 of 256                   19.7 (11) 21.3 (16) 23.7 (32)
+// 8 by 16 on 2000, 8/1 of 256              20.3 (4)  20.5 (8)  24.7 (8)
+// 64 by 4 on 2000, 8/1 of 256              30.3 (2)  27.0 (4)  28.1 (6)
+// 64 by 1 to 61 on 300 to 866, 8/1 of 256  50.9 (1)  33.3 (1)  37.1 (1)
+// 500 on 8000, 8/1 of 256                  65.5 (2)  52.0 (8)  54.0 (16)
 // 4096 on 28672, 8/1 of 256                1311 (1)  809 (1)   800 (2)
-// 32 by 1 to 100 on 100 to 3000, 32/8/128  92.7 (1)  85.3 (1)  100 (3)
-// fp32: 5 of 33 to 301, 8/2 of 64          18.8 (1)  22.7 (4)  23.6 (4)
-// 4 by 200 on 1000, 8/1 of 256             49.5 (1)  44.9 (2)  44.0 (4)
+// 32 by 1 to 100 on 100 to 3000, 32/8/128  143 (1)   85.4 (1)  101 (3)
+// fp32: 5 of 33 to 301, 8/2 of 64          17.2 (1)  24.0 (4)  24.4 (4)
+// 50 on 900, 8/1 of 256                    20.1 (8)  22.5 (8)  26.8 (8)
+// 4 by 200 on 1000, 8/1 of 256             47.7 (1)  45.1 (2)  44.0 (4)
+// 2 by 200 on 4000, 8/1 of 256             86.7 (2)  58.4 (5)  57.4 (9)
 // One workgroup a CU is enough for short walks, two for long ones, whose workgroups wait for
 // their tiles; more chunks than that cost what the join reads.
 PartPlan plan_part(const fv_part_args& x, const fv_quant_pages& c, int max_keys) {
@@ -724,11 +771,13 @@ PartPlan plan_part(const fv_part_args& x, const fv_quant_pages& c, int max_keys)
            : tiles(128) >= 256 && max_keys >= 8192                                          ? 128
                                                                                             : 64;
   const int64_t n = tiles(p.rows);
-  int64_t chunks = (p.rows == 32 ? 192 : 256 + n / 2) / n;
-  if (p.rows > 32 && max_keys > 1024 * (chunks > 1 ? chunks : 1)) chunks = (512 + n / 2) / n;
-  if (chunks > max_keys / 128) chunks = max_keys / 128;
+  // the workgroups of fp32 have a CU each
+  int64_t chunks = p.rows == 32 ? 192 / n : c.dtype == FV_FP32 ? 256 / n : (256 + n / 2) / n;
+  if (p.rows > 32 && c.dtype == FV_BF16 && max_keys > 1024 * (chunks > 1 ? chunks : 1)) chunks = (512 + n / 2) / n;
+  if (chunks > (max_keys + 127) / 128) chunks = (max_keys + 127) / 128;
   if (chunks < 1) chunks = 1;
-  const int64_t chunk = ((max_keys + chunks - 1) / chunks + 31) / 32 * 32;
+  const int64_t step = p.rows == 32 ? 32 * kPartWaves : 32;  // each wave as many keys
+  const int64_t chunk = ((max_keys + chunks - 1) / chunks + step - 1) / step * step;
   chunks = (max_keys + chunk - 1) / chunk;
   // the join's grid, one of more than 2^32 threads otherwise
   if (chunks < 1 || (int64_t)x.n_q * x.n_q_heads > 1 << 22) chunks = 1;  // the last one is longer then
