@@ -377,14 +377,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void quant_walk_kernel
   constexpr int STAGES = 65536 / STAGE > 4 ? 4 : 65536 / STAGE;
   constexpr int LT = kList / (2 * KG);  // tiles of a list
   constexpr bool BY_SUM = sizeof(T) == 2 && DH <= 192;
-  constexpr int JOIN = KG == 2 ? 2 * 32 * DH * 4 : 0, OUT = 4 * 8192;
+  constexpr int JOIN = KG == 2 ? 2 * 32 * DH * 4 : 0;
   constexpr int RING = STAGES * STAGE > JOIN ? STAGES * STAGE : JOIN;
   static_assert(STAGES >= 2, "a tile ahead");
-  __shared__ __attribute__((aligned(1024))) unsigned char ring[RING > OUT ? RING : OUT];
+  __shared__ __attribute__((aligned(1024))) unsigned char ring[RING];
   // Blocks: where they begin in either pool (64 bits), and their scales, of keys and, from bit 8 on,
   // of values; bit 31: there is none.
   __shared__ __attribute__((aligned(16))) u32x4 list[2][kList];
-  __shared__ float stats[KG == 2 ? 2 * 192 : 1];
+  __shared__ float stats[KG == 2 ? 4 * 192 : 1];
   __shared__ int found;  // NaN among the values that were sifted
   const PartRows<32 * RG> b(a, 16 * threadIdx.x);
   if (!b.any() || b.idle()) return;
@@ -410,6 +410,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void quant_walk_kernel
     list[n / kList & 1][x] = entry_of(b.block_at(k0 + 16 * (n + x)));
   };
 
+  const u32x4 entry = entry_of(b.block_at(k0 + 16 * threadIdx.x, b.page0));
+  __builtin_amdgcn_sched_barrier(0);  // its loads before the queries'
   u32x4 qf[NK][PARTS];
   {
     int tok, head;
@@ -418,7 +420,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void quant_walk_kernel
 #pragma unroll
     for (int p = 0; p < NK; ++p) query8(q + 64 * (p / 4) + 32 * (p / 2 % 2) + 16 * lh + 8 * (p % 2), qf[p]);
   }
-  list[0][threadIdx.x] = entry_of(b.block_at(k0 + 16 * threadIdx.x, b.page0));
+  list[0][threadIdx.x] = entry;
   f32x16 o[ND];
 #pragma unroll
   for (int d = 0; d < ND; ++d) o[d] = zeros16();
@@ -653,37 +655,48 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void quant_walk_kernel
   if (BY_SUM) m = m == kNoRef ? -INFINITY : -m;
   l = other_half_sum(l);
   const bool unruly = found;
+  constexpr int OUT = ND / KG;  // of o, that the wave writes: from number kg OUT on, in front after this
   if constexpr (KG == 2) {
-    f32x4* so = reinterpret_cast<f32x4*>(ring) + rg * (4 * ND * 64) + lane;
-    float* st = stats + rg * 192 + lane;
-    if (kg) {
+    // the two waves of the rows give each other half of their sums
+    f32x4* so = reinterpret_cast<f32x4*>(ring) + lane;
+    float* st = stats + lane;
+    auto give = [&](int from) __attribute__((always_inline)) {
 #pragma unroll
-      for (int d = 0; d < ND; ++d)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          so[(4 * d + j) * 64] = f32x4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]};
-      st[0] = m;
-      st[64] = l;
-      st[128] = seen;
-    }
-    meet();
-    if (!kg) {
-      const float other = st[0], now = fmaxf(m, other), ref = now == -INFINITY ? 0.f : now;
-      const float f = __builtin_amdgcn_exp2f(m - ref), g = __builtin_amdgcn_exp2f(other - ref);
-      m = now;
-      l = l * f + st[64] * g;
-      seen = seen || st[128] != 0.f;
-#pragma unroll
-      for (int d = 0; d < ND; ++d)
+      for (int d = 0; d < OUT; ++d)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const f32x4 x = so[(4 * d + j) * 64];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[d][4 * j + e] = o[d][4 * j + e] * f + x[e] * g;
+          const f32x16& x = o[from + d];
+          so[((wave * OUT + d) * 4 + j) * 64] = f32x4{x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]};
         }
-    }
+    };
+    if (kg)
+      give(0);
+    else
+      give(OUT);
+    st[192 * wave] = m;
+    st[192 * wave + 64] = l;
+    st[192 * wave + 128] = seen;
     meet();
-    if (kg) return;
+    const int with = wave ^ RG;
+    const float other = st[192 * with], top = fmaxf(m, other), ref = top == -INFINITY ? 0.f : top;
+    const float f = __builtin_amdgcn_exp2f(m - ref), g = __builtin_amdgcn_exp2f(other - ref);
+    m = top;
+    l = l * f + st[192 * with + 64] * g;
+    seen = seen || st[192 * with + 128] != 0.f;
+    auto take = [&](int from) __attribute__((always_inline)) {
+#pragma unroll
+      for (int d = 0; d < OUT; ++d)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const f32x4 x = so[((with * OUT + d) * 4 + j) * 64];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[d][4 * j + e] = o[from + d][4 * j + e] * f + x[e] * g;
+        }
+    };
+    if (kg)
+      take(OUT);
+    else
+      take(0);
   }
   if (wrow >= rows) return;
   const bool last = a.n_chunks == 1;
@@ -693,10 +706,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void quant_walk_kernel
   // Lane halves exchange so that a lane has 8 elements of its row side by side.
   if (row < rows) {
 #pragma unroll
-    for (int d = 0; d < ND; ++d)
+    for (int d = 0; d < OUT; ++d)
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const size_t to = mine + 64 * (d / 2) + 16 * (2 * j + d % 2) + 8 * lh;
+        const int n = (KG == 2 ? kg * OUT : 0) + d;
+        const size_t to = mine + 64 * (n / 2) + 16 * (2 * j + n % 2) + 8 * lh;
         float x[8];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -718,7 +732,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void quant_walk_kernel
       const int at = __builtin_amdgcn_readfirstlane(b.block_at(key & ~15));
       if (at < 0) continue;
       for (int d = lane; d < DH; d += 64) {
-        const bool odd = b.is_nan(b.place(at), key, d, DH);
+        const bool odd = (KG == 1 || (2 * (d / 64) + d / 16 % 2) / OUT == kg) && b.is_nan(b.place(at), key, d, DH);
         if (!__any(odd)) continue;
         for (int r = 0; r < 32; ++r) {
           const size_t to = (size_t)__shfl((long long)mine, r) + d;
@@ -731,7 +745,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void quant_walk_kernel
       }
     }
   }
-  if (!last && lh == 0 && wrow + l32 < rows) b.state(tok, head, seen ? m : -INFINITY, seen ? l : kNoKey);
+  if (!last && kg == 0 && lh == 0 && wrow + l32 < rows) b.state(tok, head, seen ? m : -INFINITY, seen ? l : kNoKey);
 }
 
 template <typename T, int DH>
