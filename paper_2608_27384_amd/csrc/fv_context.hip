@@ -260,7 +260,8 @@ int keys_planned(int max_len, const fv_quant_pages& c) {
   return max_len > 0 && max_len < holds ? max_len : holds;
 }
 PagedPlan quant_plan(const fv_paged_args& a, const fv_quant_pages& c) {
-  return plan_quant(a.n, a.n_q_heads, c.n_kv_heads, c.head_dim, keys_planned(a.max_len, c));
+  return plan_quant(a.n, a.n_q_heads, c.n_kv_heads, c.head_dim, keys_planned(a.max_len, c),
+                    c.dtype == FV_BF16);
 }
 
 // Whether there is work.

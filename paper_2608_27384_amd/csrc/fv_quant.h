@@ -91,7 +91,7 @@ int quant_tokens(int n);  // tokens of a workgroup of the append
 template <typename T>
 void launch_quant_gather(const fv_quant_pages& c, const int* seqs, int n, int ld, void* k_out, void* v_out,
                          hipStream_t s);
-PagedPlan plan_quant(int n, int n_q_heads, int n_kv_heads, int head_dim, int max_keys);
+PagedPlan plan_quant(int n, int n_q_heads, int n_kv_heads, int head_dim, int max_keys, bool bf16);
 template <typename T>
 void launch_quant_paged(const fv_paged_args& a, const fv_quant_pages& c, const PagedPlan& p, hipStream_t s);
 

@@ -239,8 +239,30 @@ void quant_paged_at(const PagedCall& a, size_t bytes, hipStream_t s) {
 
 }  // namespace
 
-PagedPlan plan_quant(int n, int n_q_heads, int n_kv_heads, int head_dim, int max_keys) {
-  return plan_paged(n, n_q_heads, n_kv_heads, head_dim, max_keys, true);
+// Chunks' join is a launch of its own, and their workgroups more than the chip takes at once where
+// there are many sequences.  One chunk where that costs more than the walk does; us of chunks and
+// of one, bf16, lengths from a third of the longest on:
+//   cols                  keys   440         700         1000         2040
+//      1, 8/1 heads of 256     8.3 / 8.2   8.5 / 10.4   8.5 / 12.5   10.6 / 20.3
+//      8, 32/8 of 128          7.4 / 6.3   7.8 / 7.9    7.7 / 9.3    10.3 / 15.1
+//     64, 8/1 of 256           9.3 / 8.5  11.3 / 10.6  12.2 / 13.1   21.0 / 22.5
+//    128, 8/2 of 64            8.0 / 5.7   8.6 / 7.0   9.5 / 8.1     14.6 / 13.2
+//    256, 8/1 of 256          19.0 / 11.1 23.7 / 15.4  30.6 / 19.6   40.9 / 32.5
+//   2048, 32/8 of 128         28.6 / 28.1 41.3 / 41.0  73.0 / 69.0  129   / 119
+// and fp32, whose walk costs three times the products:
+//      1, 8/1 of 256          10.3 / 12.0 10.3 / 15.7  10.5 / 18.6   12.6 / 31.3
+//     64, 8/1 of 256          11.5 / 12.5 14.1 / 16.0  15.8 / 20.4   28.0 / 36.5
+//    256, 8/1 of 256          25.7 / 16.0 32.2 / 20.3  42.8 / 24.6   56.3 / 40.7
+//      2, 8/2 of 64            7.2 / 6.0   7.4 / 7.3    7.5 / 8.6     9.6 / 13.7
+PagedPlan plan_quant(int n, int n_q_heads, int n_kv_heads, int head_dim, int max_keys, bool bf16) {
+  PagedPlan p = plan_paged(n, n_q_heads, n_kv_heads, head_dim, max_keys, true);
+  const int64_t cols = (int64_t)n * n_kv_heads * ((n_q_heads / n_kv_heads + 15) / 16);
+  const int64_t few = bf16 ? 12 * cols : 0, least = bf16 || head_dim <= 128 ? 448 : 256;
+  if (max_keys <= (cols >= 128 ? 2048 : few > least ? few : least)) {
+    p.n_chunks = 1;
+    p.work_bytes = 0;
+  }
+  return p;
 }
 
 template <typename T>
