@@ -304,6 +304,20 @@ def test_every_key_counts_once(shape, max_len):
         assert bool(((out.double() * n[:, None, None] - want).abs() <= want * (cu.EPS[dtype] + 2.0 ** -16)).all())
 
 
+@pytest.mark.parametrize("shape,n,keys", [(("bf16", 8, 1, 256), 1, 448), (("fp32", 2, 1, 256), 1, 256),
+                                          (("bf16", 8, 1, 256), 64, 768), (("bf16", 4, 4, 64), 32, 2048),
+                                          (("fp32", 4, 4, 64), 32, 2048)])
+def test_one_chunk_and_several(shape, n, keys):
+    """The longest sequences that one workgroup walks, and the next longer ones."""
+    torch = cu.torch_mod()
+    for top in (keys, keys + 1):
+        lens = [top - 37 * b % top for b in range(n)]
+        cache, q, table = qu.make(shape, lens, layers=1)
+        out = torch.full_like(q, 7.0)
+        cache.attend(0, q, cu.ints(range(n)), out, max_len=top)
+        check(shape, cache, table, lens, q, out, 0)
+
+
 # ------------------------------------------------------------------ several tokens a sequence
 
 def entries(parts, cut=()):
@@ -383,6 +397,53 @@ def test_every_key_that_is_seen_counts_once(shape, rows):
         see = torch.arange(n - rows + 1, n + 1, device="cuda")
         want = counts(see, D, H, G)
         assert bool(((out.double() * see[:, None, None] - want).abs() <= want * (cu.EPS[dtype] + 2.0 ** -16)).all())
+
+
+@pytest.mark.parametrize("holes", [False, True])
+@pytest.mark.parametrize("rows", ["few", "some", "many"])
+@pytest.mark.parametrize("shape", MANY, **IDS)
+def test_long_walks(shape, rows, holes):
+    """More keys than a workgroup looks up blocks for at once, in one chunk: of 32 rows a workgroup,
+    64, and 128.  All probabilities are one, see test_every_key_counts_once: here up to 9013 keys by
+    at most 141 steps of 64 of them, a lane's 16 after another, so sums are off by 2^-24 for each of at
+    most 2^8 + 16 additions."""
+    torch = cu.torch_mod()
+    dtype, H, G, D = shape
+    n, page_len = 9013, 48
+    m = {"few": 3, "some": 1100 if H < 32 else 500, "many": 33000 // H}[rows]
+    cache, _, table = one_hot(shape, [n], page_len)
+    there = torch.ones(n, dtype=torch.bool, device="cuda")
+    if holes:
+        for i, col in enumerate((0, 7, 87, 88, 90, 120, 187)):
+            cache.table[0, col] = (-1, cache.c.n_pages)[i % 2]
+            there[col * page_len:(col + 1) * page_len] = False
+    q = torch.zeros(m, H, D, dtype=cu.ttype(dtype), device="cuda")
+    out = torch.full_like(q, 7.0)
+    cache.attend_part(0, q, cu.ints([0, m]), cu.ints([0]), out, max_len=9013 if rows == "many" else 100)
+    limits = torch.arange(n - m + 1, n + 1, device="cuda")
+    see = torch.cat([there.new_zeros(1, dtype=torch.long), there.long().cumsum(0)])[limits]
+    for g in range(G):
+        hot = torch.nn.functional.one_hot((torch.arange(n, device="cuda") + g) % D, D) * there[:, None]
+        want = torch.cat([hot.new_zeros(1, D), hot.cumsum(0)])[limits][:, None].double()
+        got = out[:, g * H // G:(g + 1) * H // G].double()
+        assert bool(((got * see[:, None, None] - want).abs() <= want * (cu.EPS[dtype] + 2.0 ** -15)).all())
+
+
+@pytest.mark.parametrize("n", [62, 63, 64, 65, 300])
+@pytest.mark.parametrize("shape", [SHAPES[0], SHAPES[5]], **IDS)
+def test_many_entries(shape, n):
+    """Entries of no row to 40, of which neighbours share a workgroup's slots."""
+    torch = cu.torch_mod()
+    dtype, H, G, D = shape
+    lens = [1 + 53 * b % 200 for b in range(20)]
+    rows = [b * b % 41 if b % 7 else 0 for b in range(n)]
+    seqs = [b * 3 % 21 - (b % 11 == 0) for b in range(n)]
+    cache, _, table = qu.make(shape, lens, 16)
+    cum = entries(rows)
+    q = cu.randn(dtype, n, int(cum[-1]), H, D)
+    out = torch.full_like(q, 7.0)
+    cache.attend_part(1, q, cu.ints(cum), cu.ints(seqs), out)
+    check_parts(shape, cache, table, lens, seqs, cum, q, out, 1, True)
 
 
 @pytest.mark.parametrize("max_len", [0, 1300])

@@ -230,3 +230,43 @@ def test_every_part_is_a_launch(heads, kv, D, dtype):
                     assert p.work_bytes >= n_q * heads * p.n_chunks * (D + 2) * 4
                 else:
                     assert p.work_bytes == 0
+
+
+@pytest.mark.parametrize("n_q,n_seqs,heads,kv,D,keys,dtype,rows,chunk,chunks", [
+    (50, 1, 8, 1, 256, 866, fvb.FV_BF16, 32, 128, 7),       # every wave of a chunk has one step
+    (200, 1, 8, 1, 256, 866, fvb.FV_BF16, 64, 128, 7),      # 50 row tiles of 32
+    (4096, 1, 8, 1, 256, 8191, fvb.FV_BF16, 64, 8192, 1),
+    (4096, 1, 8, 1, 256, 8192, fvb.FV_BF16, 128, 4096, 2),  # two workgroups a CU
+    (4064, 1, 8, 1, 256, 28672, fvb.FV_BF16, 64, 28672, 1),
+    (800, 4, 8, 2, 64, 1301, fvb.FV_FP32, 32, 1408, 1),
+    (2100, 4, 8, 2, 64, 1301, fvb.FV_FP32, 64, 1312, 1),
+    (800, 4, 8, 1, 256, 1000, fvb.FV_FP32, 64, 512, 2)])    # one workgroup a CU
+def test_parts_are_shared_out(n_q, n_seqs, heads, kv, D, keys, dtype, rows, chunk, chunks):
+    p = part_plan(n_q, n_seqs, heads, kv, D, keys, dtype)
+    assert (p.rows, p.chunk, p.n_chunks) == (rows, chunk, chunks)
+
+
+def token_plan(n, heads, kv, D, keys, bf16):
+    class Plan(ctypes.Structure):
+        _fields_ = [("keys", ctypes.c_int32), ("chunk", ctypes.c_int32), ("n_chunks", ctypes.c_int32),
+                    ("work_bytes", ctypes.c_size_t)]
+    f = fvb.lib()._ZN2fv10plan_quantEiiiiib
+    f.restype, f.argtypes = Plan, [ctypes.c_int] * 5 + [ctypes.c_bool]
+    return f(n, heads, kv, D, keys, bf16)
+
+
+def test_tokens_are_shared_out():
+    """One chunk up to a length that grows with the workgroups of one chunk."""
+    for n, heads, kv, D, bf16, most in ((1, 8, 1, 256, True, 448), (1, 8, 1, 256, False, 256), (2, 4, 2, 128, False, 448),
+                                        (64, 8, 1, 256, True, 768), (64, 8, 1, 256, False, 256), (127, 8, 1, 64, True, 1524),
+                                        (128, 8, 1, 256, True, 2048), (32, 32, 4, 128, False, 2048), (1, 128, 1, 64, True, 448),
+                                        (16, 128, 1, 64, True, 2048), (4096, 8, 8, 64, True, 2048)):
+        p, more = token_plan(n, heads, kv, D, most, bf16), token_plan(n, heads, kv, D, most + 1, bf16)
+        assert p.n_chunks == 1 and p.work_bytes == 0
+        assert more.n_chunks > 1 and more.work_bytes == n * more.n_chunks * heads * (D + 2) * 4
+
+
+def test_tokens_of_an_append_are_shared_out():
+    f = fvb.lib()._ZN2fv12quant_tokensEi
+    f.restype, f.argtypes = ctypes.c_int, [ctypes.c_int]
+    assert [f(n) for n in (1, 511, 512, 4095, 4096, 1 << 26)] == [1, 1, 4, 4, 8, 8]
