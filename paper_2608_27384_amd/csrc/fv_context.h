@@ -47,13 +47,31 @@ template <int DH> struct RopeAngles {
     pos = a.pos + (size_t)axis * a.n;
     turns = exp2(-log2_theta * (2.0 * i / DH)) * 0.15915494309189535;
   }
+  // Cosine and sine of x turns, |x| <= 1/2, as 64 bits give them: off by no more than fp32's own
+  // rounding, where the fp32 function of the rounded angle is off by several times that.  What is
+  // quantised lands on the other side of a tie that much less often.  Their series within an eighth
+  // of a turn, whose first terms left out are below 2^-33.
+  static __device__ __forceinline__ void fine(double x, float& c, float& s) {
+    const double quarter = rint(4 * x), t = (x - 0.25 * quarter) * 6.283185307179586, z = t * t;
+    const float a = (float)(t * (1 + z * (-1. / 6 + z * (1. / 120 + z * (-1. / 5040 + z * (1. / 362880 + z * (-1. / 39916800)))))));
+    const float b = (float)(1 + z * (-1. / 2 + z * (1. / 24 + z * (-1. / 720 + z * (1. / 40320 + z * (-1. / 3628800))))));
+    const int n = (int)quarter;
+    c = n & 1 ? a : b;
+    s = n & 1 ? b : a;
+    if ((n + 1) & 2) c = -c;
+    if (n & 2) s = -s;
+  }
   // Of the tokens from `from` to `to` behind t0.
+  template <bool FINE = false>
   __device__ __forceinline__ void form(int t0, int from, int to, float (*cs)[HALF], float (*sn)[HALF]) const {
     for (int t = from + at; t < to; t += step) {
       double x = (double)pos[t0 + t] * turns;
       x -= rint(x);
       float s, c;
-      sincospif(2.0f * (float)x, &s, &c);
+      if (FINE)
+        fine(x, c, s);
+      else
+        sincospif(2.0f * (float)x, &s, &c);
       cs[t][i] = c;
       sn[t][i] = s;
     }

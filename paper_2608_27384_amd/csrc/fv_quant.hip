@@ -148,13 +148,13 @@ __global__ __launch_bounds__(256) void quant_append_kernel(QuantAppend r) {
   }
   const RopeAngles<DH> angles(a, r.log2_theta, 256);
   if (TT == 1) {
-    angles.form(t0, 0, 1, cs, sn);
+    angles.template form<true>(t0, 0, 1, cs, sn);
     __syncthreads();
     if (!n_runs) return;
   }
   const int first = run_tok[0], end = run_tok[n_runs - 1] + __popc(run_rows[n_runs - 1]);
   if (TT > 1 || end > 1) {
-    angles.form(t0, TT == 1 ? 1 : first, end, cs, sn);
+    angles.template form<true>(t0, TT == 1 ? 1 : first, end, cs, sn);
     __syncthreads();
   }
 

@@ -150,6 +150,25 @@ def test_rotated_and_quantised(shape, n):
     assert bool(((got - want).abs() <= tol).all()), float(((got - want).abs() - tol).max())
 
 
+@pytest.mark.parametrize("D", [64, 128, 192, 256])
+def test_turned_as_64_bits_turn(D):
+    """Cosines and sines are off by half a step of fp32 at one (2^-25) and 2^-33, products and the sum
+    by another 2^-24 each of a result of |a| + |b| at most; the positions' turns in 64 bits by
+    2^-50 of them.  Every eighth of a turn is among the angles."""
+    torch = cu.torch_mod()
+    n = 4096
+    cache, _ = fresh(4, 1, 1, 16, heads=1, D=D, dtype="fp32")
+    q, k = cu.randn("fp32", D, n, 2, D), cu.randn("fp32", D + 1, n, 1, D)
+    pos = np.concatenate([np.arange(-1024, 1024), np.random.default_rng(D).integers(-1 << 20, 1 << 20, 2048)])[None]
+    for theta in (1e4, 2.0 * np.pi):
+        qo, ko = torch.empty_like(q), torch.empty_like(k)
+        append(cache, 0, q, k, k, np.full(n, -1), np.zeros(n), pos, theta=theta, q_out=qo, k_out=ko)
+        for got, x in ((qo, q), (ko, k)):
+            want, _, whole = cu.rotate(x, pos, (D // 2,), theta)
+            tol = (2.5 * 2.0 ** -24 + 2.0 ** -33 + (1 << 20) * 2.0 ** -50) * (1 + 2.0 ** -20)
+            assert bool(((got.double() - want).abs() <= tol * whole).all()), float(((got.double() - want).abs() / whole).max())
+
+
 def test_a_block_starts_anew_and_goes_on():
     """From its first position on: zeros behind the new ones and a scale of theirs alone.  From
     another: the scale does not fall, the rows on both sides stay, gaps are left as they are."""
