@@ -330,7 +330,9 @@ __global__ __launch_bounds__(256) void quant_append_kernel(QuantAppend r) {
 
 // Reading back.  Block (b, entry, layer): the positions 16 b .. 16 b + 15 of a sequence, one
 // wave the keys, one the values.  Rows go out whole, 128 bytes or more side by side; a
-// lane's four positions of values are turned over in LDS.
+// lane's four positions of values are turned over in LDS.  Bounded by HBM: 64 sequences of 300 to
+// 816 tokens in 18 layers, 1 kv head of 256, to bf16: 179 us for 995 MB, 5.5 TB/s; one of 560 5.1
+// us, the trip to the table, the length and the codes.
 template <typename T, int DH, bool STREAM>
 __global__ __launch_bounds__(128) void quant_gather_kernel(fv_quant_pages c, const int* seqs, int n, int ld,
                                                            T* k_out, T* v_out) {

@@ -3,7 +3,10 @@
 // Built as the attention over pages of the dtype is (fv_paged.hip): a sequence's keys in
 // chunks, one workgroup each (per kv head and tile of 16 query heads), whose four waves walk
 // their own tiles of 32 keys from memory straight into registers and join in LDS; a second
-// kernel joins the chunks.  Memory bounds it.
+// kernel joins the chunks.  Memory bounds it: 192 sequences of 1 to 8191 keys, 32 query and 8 kv heads
+// of 128, bf16, pages of 64: 272 us for 1.63 GB, 6.0 TB/s, as a plain read goes (6.2).  Small calls
+// are a chain of trips to memory (sequence, table with the length, codes) and the join's launch:
+// one sequence of 816 keys, 8 query heads and 1 kv head of 256, 8.5 us, 64 of 300 to 816 11.6.
 //
 // A lane's 16 bytes of a block are its matrix operands after a conversion to bf16, which is
 // exact, the block's scale included: two codes an instruction, 4 cycles a wave.  Values lie in
