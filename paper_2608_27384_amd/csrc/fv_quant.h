@@ -87,7 +87,11 @@ inline Scales scales_of(const fv_quant_pages& c) {
 // The launches take validated arguments.
 template <typename T>
 void launch_quant_append(const fv_rope_args& a, const fv_quant_pages& c, hipStream_t s);
-int quant_tokens(int n);  // tokens of a workgroup of the append
+// Tokens of a workgroup of the append, and workgroups that share the same ones.
+struct QuantShare {
+  int tokens, parts;
+};
+QuantShare quant_share(int n, int n_kv_heads);
 template <typename T>
 void launch_quant_gather(const fv_quant_pages& c, const int* seqs, int n, int ld, void* k_out, void* v_out,
                          hipStream_t s);

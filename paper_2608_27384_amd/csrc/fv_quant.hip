@@ -85,11 +85,13 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t w, float f) {
 // or values of one head: it finds the largest size, which gives the scale, in registers, lays
 // the block out in LDS over what it held, and stores it, whole or the pieces that changed.  So no
 // two waves write one block, nothing is read twice, and the result does not depend on the order
-// of anything.  The queries of the runs go, a few pieces at a time, to the waves that are free.
+// of anything.  Of the workgroups that have the same tokens (blockIdx.z) each takes its share of
+// the runs' keys and values and of their queries, which go, a few pieces at a time, to the waves
+// that are free.
 // A workgroup's time is a chain of trips to memory (token, table, block's scale and codes), so
 // all loads of a piece of work are issued before the first is used.  64 prompts of 300 to 816
 // tokens, 8 query heads and 1 kv head of 256, bf16: 83 us for 368 MB, 4.4 TB/s, as large copies go
-// (5.1); queries in a launch of their own beside it took 97 us.  64 single tokens: 6.0 us.
+// (5.1); queries in a launch of their own beside it took 97 us.  64 single tokens: 6.3 us.
 template <typename T, int DH, int TT>
 __global__ __launch_bounds__(256) void quant_append_kernel(QuantAppend r) {
   constexpr int HALF = DH / 2, SLABS = DH / 64, ANG = TT + kBlock - 1, WAVES = 4;
@@ -160,8 +162,10 @@ __global__ __launch_bounds__(256) void quant_append_kernel(QuantAppend r) {
 
   const size_t layer = (size_t)a.layer * block_of(c.n_pages, c.n_kv_heads, 0, c.page_len, 0);
   unsigned char* mine = reinterpret_cast<unsigned char*>(image[wave]);
-  const int items = n_runs * 2 * c.n_kv_heads;
-  for (int item = wave; item < items; item += WAVES) {
+  // the workgroup's share of the keys and values, and further down of the queries
+  const int part = blockIdx.z, parts = gridDim.z;
+  const int all_items = n_runs * 2 * c.n_kv_heads, items = (part + 1) * all_items / parts;
+  for (int item = part * all_items / parts + wave; item < items; item += WAVES) {
     const bool values = item & 1;
     const int g = (item >> 1) % c.n_kv_heads, run = (item >> 1) / c.n_kv_heads;
     const int tok = run_tok[run], rows = __builtin_amdgcn_readfirstlane(run_rows[run]), len = __popc(rows);
@@ -298,10 +302,11 @@ __global__ __launch_bounds__(256) void quant_append_kernel(QuantAppend r) {
 
   // N pieces a lane, 16 N 64 elements a wave, at a time
   constexpr int PIECES = DH / 16, N = 2;
-  const int all = (end - first) * a.n_q_heads * PIECES;
+  const int pieces = (end - first) * a.n_q_heads * PIECES;
+  const int from0 = part * pieces / parts, all = (part + 1) * pieces / parts;
   while (true) {
     int u0 = 0;
-    if (lane == 0) u0 = atomicAdd(&taken, 64 * N);
+    if (lane == 0) u0 = from0 + atomicAdd(&taken, 64 * N);
     u0 = __builtin_amdgcn_readfirstlane(u0);
     if (u0 >= all) break;
     float x[N][8], y[N][8];
@@ -408,16 +413,17 @@ __global__ __launch_bounds__(128) void quant_gather_kernel(fv_quant_pages c, con
 }
 
 template <typename T, int DH, int TT>
-void append_runs(const QuantAppend& r, hipStream_t s) {
+void append_runs(const QuantAppend& r, int parts, hipStream_t s) {
   const unsigned n = (r.a.n + TT - 1) / TT, wide = n < 1 << 20 ? n : 1 << 20;
-  hipLaunchKernelGGL((quant_append_kernel<T, DH, TT>), dim3(wide, (n + wide - 1) / wide), dim3(256), 0, s, r);
+  hipLaunchKernelGGL((quant_append_kernel<T, DH, TT>), dim3(wide, (n + wide - 1) / wide, parts), dim3(256), 0, s, r);
 }
 template <typename T, int DH>
 void append_at(const QuantAppend& r, hipStream_t s) {
-  switch (quant_tokens(r.a.n)) {
-    case 1: return append_runs<T, DH, 1>(r, s);
-    case 4: return append_runs<T, DH, 4>(r, s);
-    default: return append_runs<T, DH, 8>(r, s);
+  const QuantShare x = quant_share(r.a.n, r.c.n_kv_heads);
+  switch (x.tokens) {
+    case 1: return append_runs<T, DH, 1>(r, x.parts, s);
+    case 4: return append_runs<T, DH, 4>(r, x.parts, s);
+    default: return append_runs<T, DH, 8>(r, x.parts, s);
   }
 }
 
@@ -434,13 +440,30 @@ void gather_at(const fv_quant_pages& c, const int* seqs, int n, int ld, void* k_
 
 }  // namespace
 
-// Few tokens are as a rule one a sequence, each a run: a workgroup for each, since one that has
-// several takes their blocks one after another.  Many are prompts, of up to 16 tokens a run:
-// workgroups of few tokens are then mostly ones that find no run of their own.  Microseconds at
-// 1, 4 and 8 tokens, bf16: 192 sequences of one token and 8 kv heads 11.2, 31, 58, of 1 kv head
-// 6.3, 9.1, 14; a prompt of 816, 1 kv head of 256, 21.7, 11.2, 10.1, 8 of 128 35, 21.8, 20.8;
-// 2500 sequences of a token, 1 kv head 22.3, 15.6, 20.1; 64 prompts of 300 to 816 186, 92.8, 83.
-int quant_tokens(int n) { return n < 512 ? 1 : n < 4096 ? 4 : 8; }
+// A list of many tokens is as a rule prompts, whose runs are up to 16 long: workgroups of few tokens
+// are then mostly ones that find no run of their own.  One of few is as a rule a token a sequence,
+// each a run.  Where the tokens do not fill the chip, several workgroups have the same ones and
+// share their blocks and queries out, or a workgroup's waves take many blocks one after another.
+// us by parts, bf16 (in brackets: what is taken):
+//                                         1 token          4 tokens               8 tokens
+//   parts                                 1    4    8      1    2    4    8       1    2    4    8
+//   64 single tokens, 8/1 heads of 256   (6.3)             9.0  6.7  6.6
+//   64 single tokens, 32/8 of 128       10.9  5.7 (5.9)   31.1 17.9 10.9  7.5
+//   500 single tokens, 32/8 of 128      13.8 14.5 20.6    33.3 19.8 13.8 (12.3)
+//   a prompt of 400, 8/1 of 256         12.9              10.1  9.0 (9.2)
+//   a prompt of 816, 8/1 of 256         21.5              11.3 (10.4) 14.1
+//   2 prompts of 816, 32/8 of 128       58.3 68.9 91.0    27.0 24.6 25.1 27.9    22.3 17.2 (16.4) 17.3
+//   4 prompts of 816, 8/1 of 256        55.7              25.1 26.2 35.1         (14.3) 17.6 21.1 29.9
+//   8 prompts of 816, 32/8 of 128                         73.1 72.7 76.1 95.6    (42.4) 41.5 43.0 51.4
+QuantShare quant_share(int n, int n_kv_heads) {
+  QuantShare x;
+  x.tokens = n < 128 ? 1 : n < 1024 ? 4 : 8;
+  const int fill = n_kv_heads < 3 ? 256 * (n_kv_heads + 1) : 1024, most = n_kv_heads * x.tokens;
+  x.parts = fill / ((n + x.tokens - 1) / x.tokens);
+  if (x.parts > most) x.parts = most;
+  if (x.parts < 1) x.parts = 1;
+  return x;
+}
 
 template <typename T>
 void launch_quant_append(const fv_rope_args& a, const fv_quant_pages& c, hipStream_t s) {

@@ -105,12 +105,13 @@ def test_appended_part_by_part(shape, page_len):
         assert x[0].equal(y[0])
 
 
-@pytest.mark.parametrize("n", [1, 17, 511, 512, 2053, 4095, 4096, 8197])
+@pytest.mark.parametrize("n", [1, 17, 127, 128, 1023, 1024, 4099, 8197])
 @pytest.mark.parametrize("shape", SHAPES[:6], **IDS)
 def test_rotated_and_quantised(shape, n):
     """Keys are off by half a step of e4m3 and the rotation's own error; scales are those of the
     largest, queries and kept keys the rotary operator's.  Runs of tokens lie in both sequences, from
-    position 5 on, and cross what workgroups share out, 1, 4 or 8 tokens of the list."""
+    position 5 on, and cross what workgroups share out, 1, 4 or 8 tokens of the list,
+    and the shares of workgroups that have the same tokens."""
     torch = cu.torch_mod()
     dtype, H, G, D = shape
     rng = np.random.default_rng(n)

@@ -267,6 +267,15 @@ def test_tokens_are_shared_out():
 
 
 def test_tokens_of_an_append_are_shared_out():
-    f = fvb.lib()._ZN2fv12quant_tokensEi
-    f.restype, f.argtypes = ctypes.c_int, [ctypes.c_int]
-    assert [f(n) for n in (1, 511, 512, 4095, 4096, 1 << 26)] == [1, 1, 4, 4, 8, 8]
+    class Share(ctypes.Structure):
+        _fields_ = [("tokens", ctypes.c_int32), ("parts", ctypes.c_int32)]
+    f = fvb.lib()._ZN2fv11quant_shareEii
+    f.restype, f.argtypes = Share, [ctypes.c_int] * 2
+    for n, kv, tokens, parts in ((1, 1, 1, 1), (127, 1, 1, 1), (128, 1, 4, 4), (1023, 1, 4, 2), (1024, 1, 8, 4), (4096, 1, 8, 1),
+                                 (1, 8, 1, 8), (127, 8, 1, 8), (128, 8, 4, 32), (1023, 8, 4, 4), (1024, 8, 8, 8),
+                                 (4096, 8, 8, 2), (4104, 8, 8, 1), (512, 2, 4, 6), (1 << 26, 1024, 8, 1)):
+        s = f(n, kv)
+        assert (s.tokens, s.parts) == (tokens, parts), n
+        wide = min(-(-n // tokens), 1 << 20)
+        assert wide * 256 < 1 << 32 and -(-n // tokens // wide) < 1 << 16
+    assert max(f(n, 1024).parts for n in range(1, 2000)) < 1 << 16
