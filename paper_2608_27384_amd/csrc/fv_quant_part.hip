@@ -771,43 +771,78 @@ void part_at(const PartCall& a, int rows, hipStream_t s) {
 
 }  // namespace
 
-// us by rows a workgroup and, in brackets, chunks, of calls captured into a graph:
-//                                          32        64        128
-// 50 tokens on 866, heads 8/1 of 256       13.9 (7)  15.4 (7)  17.5 (7)
-// 50 on 4000, 8/1 of 256                   19.7 (11) 21.3 (16) 23.7 (32)
-// 8 by 16 on 2000, 8/1 of 256              20.3 (4)  20.5 (8)  24.7 (8)
-// 64 by 4 on 2000, 8/1 of 256              30.3 (2)  27.0 (4)  28.1 (6)
-// 64 by 1 to 61 on 300 to 866, 8/1 of 256  50.9 (1)  33.3 (1)  37.1 (1)
-// 500 on 8000, 8/1 of 256                  65.5 (2)  52.0 (8)  54.0 (16)
-// 4096 on 28672, 8/1 of 256                1311 (1)  809 (1)   800 (2)
-// 32 by 1 to 100 on 100 to 3000, 32/8/128  143 (1)   85.4 (1)  101 (3)
-// fp32: 5 of 33 to 301, 8/2 of 64          17.2 (1)  24.0 (4)  24.4 (4)
-// 50 on 900, 8/1 of 256                    20.1 (8)  22.5 (8)  26.8 (8)
-// 4 by 200 on 1000, 8/1 of 256             47.7 (1)  45.1 (2)  44.0 (4)
-// 2 by 200 on 4000, 8/1 of 256             86.7 (2)  58.4 (5)  57.4 (9)
-// One workgroup a CU is enough for short walks, two for long ones, whose workgroups wait for
-// their tiles; more chunks than that cost what the join reads.
+namespace {
+// About the us of a call that shares its rows out to `tiles` row tiles and its keys to `chunks` chunks
+// of `chunk`: a launch, and between the time of one workgroup and that of all of them on the chip, a
+// little more than the longer; where there are chunks, the join and what it reads.  Either
+// time is a fixed part and one for each 32 keys, with a part of each that grows with the head.
+// The workgroups of fp32 have a CU each, so that what is over a full round counts half a round.
+// Fitted to 11370 timings of 1086 calls of 1 to 512 sequences, 1 to 4096 new tokens, 1 to 30000
+// keys, heads 8/1 of 256, 32/8 of 128, 8/2 of 64 and 4/2 of 192 (14 % off each).  What it
+// chooses took 3 % longer than the best of all in the mean and 10 % at the ninetieth hundredth,
+// where limits on the number of row tiles and of keys took over 10 % in the mean.
+double part_time(bool fp32, int kind, double head, double tiles, double chunk, int chunks, double moved) {
+  static const double of[2][3][8] = {
+      {{0.836, 4.174, 0.136, 0.259, 0.051, 6.612, 0.102, 0.302},
+       {1.194, 4.239, 0.196, 0.36, 1.317, 1.957, 0.082, 0.341},
+       {0.934, 3.331, 0.396, 0.594, 0.81, 1.039, 0.091, 0.633}},
+      {{0, 6.914, 0, 0.665, 0, 10.39, 0, 0.71},
+       {0.188, 6.218, 0.25, 0.669, 0, 11.671, 0.041, 1.223},
+       {0, 4.994, 0.381, 1.474, 0, 10.213, 0.127, 2.314}}};
+  static const double join[2][2] = {{3.543, 0.173}, {2.818, 0.157}};  // us, us a MB
+  const double* x = of[fp32][kind];
+  const double w = head / 256, steps = chunk / 32;
+  double n = tiles * chunks;
+  if (fp32) {
+    const double round = head < 128 ? 512 : 256;
+    n = 0.5 * (n + round * ceil(n / round));
+  }
+  const double one = x[0] + x[1] * w + steps * (x[2] + x[3] * w);
+  const double all = n / 256 * (x[4] + x[5] * w + steps * (x[6] + x[7] * w));
+  return 3 + sqrt(one * one + all * all) + (chunks > 1 ? join[fp32][0] + join[fp32][1] * 1e-6 * moved * chunks : 0);
+}
+}  // namespace
+
+// The rows of a workgroup and the chunks that part_time says are the fastest.  us by rows and, in
+// brackets, chunks, the best of each, of calls captured into a graph, and what is taken:
+//                                          32        64        128       taken
+// 50 tokens on 866, heads 8/1 of 256       14.3 (7)  15.5 (7)  17.9 (7)  32 (7)
+// 4 by 50 on 866, 8/1 of 256               18.1 (4)  19.7 (3)  22.7 (7)  64 (4): 20
+// 64 by 1 to 61 on 300 to 866, 8/1 of 256  52.2 (1)  34.5 (1)  37.4 (1)  64 (1)
+// 128 by 50 on 300 to 866, 8/1 of 256      125 (1)   64.9 (1)  54.1 (1)  128 (1)
+// 500 on 8000, 8/1 of 256                  66.7 (2)  53.1 (8)  55.6 (8)  64 (6): 56.6
+// 4096 on 28672, 8/1 of 256                1390 (1)  824 (1)   808 (2)   128 (2)
+// 32 by 1 to 100 on 100 to 3000, 32/8/128  143 (1)   87.6 (1)  103 (3)   64 (1)
+// 8 by 500 on 2000, 32/8 of 128            295 (1)   161 (1)   132 (1)   128 (1)
+// fp32: 5 by 33 to 301 on 60 to 1301, 8/2/64 17.2 (1)  23.4 (4)  24.7 (4)  32 (1)
+// fp32: 50 on 900, 8/1 of 256              20.7 (8)  21.7 (8)  27.1 (8)  32 (8)
+// fp32: 4 by 200 on 1000, 8/1 of 256       48.9 (1)  43.8 (2)  44.6 (4)  32 (1)
+// fp32: 64 by 50 on 866, 8/1 of 256        170 (1)   100 (1)   83.7 (1)  64 (1)
 PartPlan plan_part(const fv_part_args& x, const fv_quant_pages& c, int max_keys) {
+  static const int counts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
   PartPlan p{};
   const int64_t rows = (int64_t)x.n_q * (x.n_q_heads / c.n_kv_heads);
-  auto tiles = [&](int of) { return (rows / of + (x.n_seqs + 1) / 2) * c.n_kv_heads; };  // about
-  p.rows = rows / 32 * c.n_kv_heads <= (c.dtype == FV_FP32 && c.head_dim <= 128 ? 256 : 48) ? 32
-           : tiles(128) >= 256 && max_keys >= 8192                                          ? 128
-                                                                                            : 64;
-  const int64_t n = tiles(p.rows);
-  // the workgroups of fp32 have a CU each
-  int64_t chunks = p.rows == 32 ? 192 / n : c.dtype == FV_FP32 ? 256 / n : (256 + n / 2) / n;
-  if (p.rows > 32 && c.dtype == FV_BF16 && max_keys > 1024 * (chunks > 1 ? chunks : 1)) chunks = (512 + n / 2) / n;
-  if (chunks > (max_keys + 127) / 128) chunks = (max_keys + 127) / 128;
-  if (chunks < 1) chunks = 1;
-  const int64_t step = p.rows == 32 ? 32 * kPartWaves : 32;  // each wave as many keys
-  const int64_t chunk = ((max_keys + chunks - 1) / chunks + step - 1) / step * step;
-  chunks = (max_keys + chunk - 1) / chunk;
-  // the join's grid, one of more than 2^32 threads otherwise
-  if (chunks < 1 || (int64_t)x.n_q * x.n_q_heads > 1 << 22) chunks = 1;  // the last one is longer then
-  p.chunk = (int)chunk;
-  p.n_chunks = (int)chunks;
-  if (chunks > 1) p.work_bytes = (size_t)x.n_q * chunks * x.n_q_heads * (c.head_dim + 2) * 4;
+  double best = 0;
+  for (int kind = 0; kind < 3; ++kind) {
+    const int of = 32 << kind;
+    const double shared = (double)rows / of + 0.5 * x.n_seqs;  // entries begin inside tiles
+    const double tiles = (shared > x.n_seqs ? shared : x.n_seqs) * c.n_kv_heads;
+    for (int count : counts) {
+      const int64_t step = kind ? 32 : 32 * kPartWaves;  // with 32 rows, each wave as many keys
+      const int64_t chunk = ((max_keys + count - 1) / count + step - 1) / step * step;
+      const int64_t chunks = (max_keys + chunk - 1) / chunk;
+      // not where the chip is full without, nor where the join's grid would have 2^32 threads
+      if (count > 1 && (chunk < 128 || tiles * count > 768 || (int64_t)x.n_q * x.n_q_heads > 1 << 22)) break;
+      const double us = part_time(c.dtype == FV_FP32, kind, c.head_dim, tiles, chunk < max_keys ? chunk : max_keys,
+                                  (int)chunks, 8. * rows * c.n_kv_heads * c.head_dim);
+      if (p.rows && us >= best) continue;
+      best = us;
+      p.rows = of;
+      p.chunk = (int)chunk;
+      p.n_chunks = (int)chunks;
+    }
+  }
+  if (p.n_chunks > 1) p.work_bytes = (size_t)x.n_q * p.n_chunks * x.n_q_heads * (c.head_dim + 2) * 4;
   return p;
 }
 

@@ -7,6 +7,7 @@ import pytest
 
 import context_util as cu
 import quant_util as qu
+from test_quant_refusals import part_plan
 
 pytestmark = pytest.mark.gpu
 
@@ -399,18 +400,29 @@ def test_every_key_that_is_seen_counts_once(shape, rows):
         assert bool(((out.double() * see[:, None, None] - want).abs() <= want * (cu.EPS[dtype] + 2.0 ** -16)).all())
 
 
+def in_one_chunk(shape, rows):
+    """New tokens of one sequence, and a bound of its length, that make one chunk of row tiles of `rows`."""
+    dtype, H, G, D = shape
+    from paper_2608_27384_amd import flashvla as fvb
+    for m in (3, 500, 600, 1100, 2500, 4000, 60000 // H, 120000 // H):
+        for top in (100, 9013):
+            p = part_plan(m, 1, H, G, D, top, fvb.FV_BF16 if dtype == "bf16" else fvb.FV_FP32)
+            if (p.rows, p.n_chunks) == (rows, 1):
+                return m, top
+
+
 @pytest.mark.parametrize("holes", [False, True])
-@pytest.mark.parametrize("rows", ["few", "some", "many"])
+@pytest.mark.parametrize("rows", [32, 64, 128])
 @pytest.mark.parametrize("shape", MANY, **IDS)
 def test_long_walks(shape, rows, holes):
-    """More keys than a workgroup looks up blocks for at once, in one chunk: of 32 rows a workgroup,
-    64, and 128.  All probabilities are one, see test_every_key_counts_once: here up to 9013 keys by
-    at most 141 steps of 64 of them, a lane's 16 after another, so sums are off by 2^-24 for each of at
-    most 2^8 + 16 additions."""
+    """More keys than a workgroup looks up blocks for at once, in one chunk, by each of the kernels.
+    All probabilities are one, see test_every_key_counts_once: here up to 9013 keys by at most 141
+    steps of 64 of them, a lane's 16 after another, so sums are off by 2^-24 for each of at most 2^8 +
+    16 additions."""
     torch = cu.torch_mod()
     dtype, H, G, D = shape
     n, page_len = 9013, 48
-    m = {"few": 3, "some": 1100 if H < 32 else 500, "many": 33000 // H}[rows]
+    m, max_len = in_one_chunk(shape, rows)
     cache, _, table = one_hot(shape, [n], page_len)
     there = torch.ones(n, dtype=torch.bool, device="cuda")
     if holes:
@@ -419,8 +431,8 @@ def test_long_walks(shape, rows, holes):
             there[col * page_len:(col + 1) * page_len] = False
     q = torch.zeros(m, H, D, dtype=cu.ttype(dtype), device="cuda")
     out = torch.full_like(q, 7.0)
-    cache.attend_part(0, q, cu.ints([0, m]), cu.ints([0]), out, max_len=9013 if rows == "many" else 100)
-    limits = torch.arange(n - m + 1, n + 1, device="cuda")
+    cache.attend_part(0, q, cu.ints([0, m]), cu.ints([0]), out, max_len=max_len)
+    limits = torch.arange(n - m + 1, n + 1, device="cuda").clamp(min=0)
     see = torch.cat([there.new_zeros(1, dtype=torch.long), there.long().cumsum(0)])[limits]
     for g in range(G):
         hot = torch.nn.functional.one_hot((torch.arange(n, device="cuda") + g) % D, D) * there[:, None]

@@ -234,13 +234,15 @@ def test_every_part_is_a_launch(heads, kv, D, dtype):
 
 @pytest.mark.parametrize("n_q,n_seqs,heads,kv,D,keys,dtype,rows,chunk,chunks", [
     (50, 1, 8, 1, 256, 866, fvb.FV_BF16, 32, 128, 7),       # every wave of a chunk has one step
-    (200, 1, 8, 1, 256, 866, fvb.FV_BF16, 64, 128, 7),      # 50 row tiles of 32
-    (4096, 1, 8, 1, 256, 8191, fvb.FV_BF16, 64, 8192, 1),
-    (4096, 1, 8, 1, 256, 8192, fvb.FV_BF16, 128, 4096, 2),  # two workgroups a CU
-    (4064, 1, 8, 1, 256, 28672, fvb.FV_BF16, 64, 28672, 1),
-    (800, 4, 8, 2, 64, 1301, fvb.FV_FP32, 32, 1408, 1),
-    (2100, 4, 8, 2, 64, 1301, fvb.FV_FP32, 64, 1312, 1),
-    (800, 4, 8, 1, 256, 1000, fvb.FV_FP32, 64, 512, 2)])    # one workgroup a CU
+    (1982, 64, 8, 1, 256, 866, fvb.FV_BF16, 64, 896, 1),
+    (6400, 128, 8, 1, 256, 866, fvb.FV_BF16, 128, 896, 1),
+    (500, 1, 8, 1, 256, 8000, fvb.FV_BF16, 64, 1344, 6),
+    (4096, 1, 8, 1, 256, 28672, fvb.FV_BF16, 128, 14336, 2),  # two workgroups a CU
+    (4000, 8, 32, 8, 128, 2000, fvb.FV_BF16, 128, 2016, 1),
+    (800, 5, 8, 2, 64, 1301, fvb.FV_FP32, 32, 1408, 1),
+    (50, 1, 8, 1, 256, 900, fvb.FV_FP32, 32, 128, 8),
+    (12800, 256, 8, 1, 256, 866, fvb.FV_FP32, 128, 896, 1),
+    (1, 1, 8, 1, 256, 1 << 24, fvb.FV_BF16, 32, 1 << 19, 32)])
 def test_parts_are_shared_out(n_q, n_seqs, heads, kv, D, keys, dtype, rows, chunk, chunks):
     p = part_plan(n_q, n_seqs, heads, kv, D, keys, dtype)
     assert (p.rows, p.chunk, p.n_chunks) == (rows, chunk, chunks)
