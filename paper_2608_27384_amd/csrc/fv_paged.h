@@ -45,7 +45,6 @@ __device__ __forceinline__ int length_of(const PagedCall& a, int s) {
   return min(max(a.len[s], 0), a.max_pages * a.page_len);
 }
 
-
 // The call of validated arguments, without its pools.
 PagedCall paged_call(const fv_paged_args& x, const fv_pages& c, const PagedPlan& p);
 // The kernel that joins a call's chunks, if it has several.

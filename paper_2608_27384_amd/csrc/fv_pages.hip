@@ -21,7 +21,8 @@ struct RopeCall {
 
 // A workgroup first forms the cosines and sines of its tokens, once for all
 // heads (RopeAngles).  Then each thread takes 16 bytes of a head's first half and
-// the 16 that they are paired with.  Memory bounds it: 38 thousand tokens, heads 8/1 of 256, 78 us (388 MB, 4.9 TB/s, as a copy has);
+// the 16 that they are paired with.  Memory bounds it: 38 thousand tokens, heads 8/1 of 256,
+// 78 us (388 MB, 4.9 TB/s, as a copy has);
 // 64 tokens 3.8 us, a launch and one trip to memory.
 template <typename T, int DH>
 __global__ __launch_bounds__(kRopeThreads) void rope_append_kernel(RopeCall r) {
