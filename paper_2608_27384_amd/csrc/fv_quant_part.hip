@@ -165,10 +165,13 @@ template <typename T, int DH>
 __global__ __launch_bounds__(64 * kPartWaves, 1) void quant_part_kernel(PartCall a) {
   constexpr int SLABS = DH / 64, NK = DH / 16, ND = DH / 32, PITCH = DH + 4;
   constexpr int PARTS = sizeof(T) == 2 ? 1 : 3;
-  constexpr bool AHEAD = PARTS == 1 || DH <= 128;  // a step's codes are under way in the one before it
+  // fp32 queries of long heads are 144 or 192 registers in parts: they stay in LDS, where `so` comes
+  // later.  50 tokens on 866 keys, 8/1 heads of 256, 16.5 us, in registers 20.0; 4/2 of 192 13.3, 14.2.
+  constexpr bool PUT = PARTS == 3 && DH >= 192;
   __shared__ float sm[kPartWaves][32], sl[kPartWaves][32];
   __shared__ int seen_by[kPartWaves][32];
   __shared__ __attribute__((aligned(16))) float so[kPartWaves][32 * PITCH];
+  u32x4* const put = reinterpret_cast<u32x4*>(&so[0][0]);
   // Lane l looks up the block of the wave's step l / 2, half l % 2; the wave's steps are
   // kPartWaves apart, so this is 32 of them.
   const int ahead = 32 * ((int)threadIdx.x >> 6) + 16 * ((int)threadIdx.x & 1) + 32 * kPartWaves * (((int)threadIdx.x & 63) >> 1);
@@ -217,12 +220,19 @@ __global__ __launch_bounds__(64 * kPartWaves, 1) void quant_part_kernel(PartCall
     __builtin_amdgcn_sched_barrier(0);
   };
   Tile now, next;
-  if (AHEAD && wave < steps) fetch(wave, next);
+  if (wave < steps) fetch(wave, next);
   u32x4 qf[NK][PARTS];
   {
     const T* q = static_cast<const T*>(a.q) + (size_t)(b.q0 + tok) * a.ldq + head * DH;
 #pragma unroll
-    for (int p = 0; p < NK; ++p) query8(q + 64 * (p / 4) + 32 * (p / 2 % 2) + 16 * lh + 8 * (p % 2), qf[p]);
+    for (int p = 0; p < NK; ++p) {
+      if (PUT && p % kPartWaves != wave) continue;
+      query8(q + 64 * (p / 4) + 32 * (p / 2 % 2) + 16 * lh + 8 * (p % 2), qf[p]);
+      if (PUT)
+#pragma unroll
+        for (int x = 0; x < PARTS; ++x) put[(p * PARTS + x) * 64 + lane] = qf[p][x];
+    }
+    if (PUT) __syncthreads();
   }
   f32x16 o[ND];
 #pragma unroll
@@ -230,12 +240,8 @@ __global__ __launch_bounds__(64 * kPartWaves, 1) void quant_part_kernel(PartCall
   float m = -INFINITY, l = 0.f;  // l over the lane half's keys only
   bool unruly = false, seen = false;
   for (int i = wave; i < steps; i += kPartWaves) {
-    if (AHEAD) {
-      now = next;
-      if (i + kPartWaves < steps) fetch(i + kPartWaves, next);
-    } else {
-      fetch(i, now);
-    }
+    now = next;
+    if (i + kPartWaves < steps) fetch(i + kPartWaves, next);
     const int key0 = k0 + 32 * i, at0 = now.at[0], at1 = now.at[1];
     const bool edge = key0 + 32 > whole || key0 + 32 > k1 || at0 < 0 || at1 < 0;
     const float ks = power_of(scale_exponent((uint8_t)(l32 < 16 ? now.scales[0] : now.scales[1])));
@@ -248,7 +254,7 @@ __global__ __launch_bounds__(64 * kPartWaves, 1) void quant_part_kernel(PartCall
     for (int p = 0; p < NK; ++p) {
       const u32x4 k = to_bf16x8(kf[p / 2][2 * (p % 2)], kf[p / 2][2 * (p % 2) + 1], ks);
 #pragma unroll
-      for (int x = 0; x < PARTS; ++x) sc = mma32(k, qf[p][x], sc, bf16_t{});
+      for (int x = 0; x < PARTS; ++x) sc = mma32(k, PUT ? put[(p * PARTS + x) * 64 + lane] : qf[p][x], sc, bf16_t{});
     }
     if (edge) {
       uint32_t odd = 0;
