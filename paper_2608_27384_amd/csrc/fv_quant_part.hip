@@ -785,7 +785,8 @@ namespace {
 // The workgroups of fp32 have a CU each, so that what is over a full round counts half a round.
 // Fitted to 11370 timings of 1086 calls of 1 to 512 sequences, 1 to 4096 new tokens, 1 to 30000
 // keys, heads 8/1 of 256, 32/8 of 128, 8/2 of 64 and 4/2 of 192 (14 % off each).  What it
-// chooses took 3 % longer than the best of all in the mean and 10 % at the ninetieth hundredth,
+// chooses took 3 % longer than the best of all in the mean and 10 % at the ninetieth hundredth
+// (2 and 7 % in fp32, on 284 other calls, since the queries of long heads are in LDS),
 // where limits on the number of row tiles and of keys took over 10 % in the mean.
 double part_time(bool fp32, int kind, double head, double tiles, double chunk, int chunks, double moved) {
   static const double of[2][3][8] = {
@@ -820,10 +821,10 @@ double part_time(bool fp32, int kind, double head, double tiles, double chunk, i
 // 4096 on 28672, 8/1 of 256                1390 (1)  824 (1)   808 (2)   128 (2)
 // 32 by 1 to 100 on 100 to 3000, 32/8/128  143 (1)   87.6 (1)  103 (3)   64 (1)
 // 8 by 500 on 2000, 32/8 of 128            295 (1)   161 (1)   132 (1)   128 (1)
-// fp32: 5 by 33 to 301 on 60 to 1301, 8/2/64 17.2 (1)  23.4 (4)  24.7 (4)  32 (1)
-// fp32: 50 on 900, 8/1 of 256              20.7 (8)  21.7 (8)  27.1 (8)  32 (8)
-// fp32: 4 by 200 on 1000, 8/1 of 256       48.9 (1)  43.8 (2)  44.6 (4)  32 (1)
-// fp32: 64 by 50 on 866, 8/1 of 256        170 (1)   100 (1)   83.7 (1)  64 (1)
+// fp32: 5 by 33 to 301 on 60 to 1301, 8/2/64 17.8 (1)  23.4 (4)  24.6 (4)  32 (1)
+// fp32: 50 on 900, 8/1 of 256              16.8 (8)  21.6 (8)  27.3 (8)  32 (8)
+// fp32: 4 by 200 on 1000, 8/1 of 256       35.9 (1)  43.8 (2)  44.4 (4)  32 (1)
+// fp32: 64 by 50 on 866, 8/1 of 256        126 (1)   97.7 (1)  83.6 (1)  64 (1)
 PartPlan plan_part(const fv_part_args& x, const fv_quant_pages& c, int max_keys) {
   static const int counts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
   PartPlan p{};
