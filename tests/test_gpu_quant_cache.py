@@ -7,6 +7,7 @@ import pytest
 
 import context_util as cu
 import quant_util as qu
+from test_quant_refusals import part_plan
 
 pytestmark = pytest.mark.gpu
 
@@ -39,7 +40,7 @@ def scattered(cache, lens, seed=0):
 
 
 SHAPES = [("bf16", 8, 1, 256), ("bf16", 4, 2, 64), ("fp32", 3, 1, 192), ("bf16", 8, 8, 128),
-          ("fp32", 4, 2, 128), ("bf16", 6, 2, 192), ("fp32", 2, 2, 64), ("fp32", 2, 1, 256)]
+          ("fp32", 4, 2, 128), ("bf16", 6, 2, 192), ("fp32", 2, 2, 64), ("fp32", 2, 1, 256), ("bf16", 40, 40, 64)]
 IDS = dict(ids=lambda s: "x".join(map(str, s)))
 
 
@@ -366,6 +367,13 @@ def test_offsets_past_32_bits():
     cu.check_attention_wide(out, ref, "bf16")
     cache.attend_part(1, q[-1:], cu.ints([0, 1]), cu.ints([0]), out)
     cu.check_attention(out, ref, "bf16")
+    ref = qu.attention(q, kd[1, 0].double(), vd[1, 0].double(), range(1, n + 1), "bf16")
+    for times, rows in ((3, 64), (20, 128)):  # of the whole sequence
+        assert part_plan(times * n, times, 8, 1, D, 3 * pl).rows == rows
+        out = torch.empty(times * n, 8, D, dtype=torch.bfloat16, device="cuda")
+        cache.attend_part(1, q.repeat(times, 1, 1), cu.ints(n * np.arange(times + 1)), cu.ints([0] * times), out)
+        for i in range(times):
+            cu.check_attention(out[n * i:n * (i + 1)], ref, "bf16")
 
 
 # ------------------------------------------------------------------ reading back
