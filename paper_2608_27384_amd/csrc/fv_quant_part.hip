@@ -378,8 +378,8 @@ __global__ __launch_bounds__(64 * kPartWaves, 1) void quant_part_kernel(PartCall
 // half the others, and they join at the end, for where there are not enough row tiles to fill the
 // chip.  Which blocks a tile has, and their scales, stands in LDS for 256 blocks at a time, the
 // next ones looked up meanwhile.
-// 4096 tokens on 28672 keys, 8 query heads and 1 kv head of 256, causal, bf16 (KG 1, two chunks): 784 us,
-// 1.14 PFLOP/s, where a library product of 8192^3 reaches 1.21: bounded by the matrix unit, which
+// 4096 tokens on 28672 keys, 8 query heads and 1 kv head of 256, causal, bf16 (KG 1, two chunks): 779 us,
+// 1.15 PFLOP/s, where a library product of 8192^3 reaches 1.21: bounded by the matrix unit, which
 // the conversions (4 cycles each, four beside a product of 32) and the softmax of the other
 // wave of a SIMD leave busy.  64 parts of 1 to 61 tokens on 300 to 866 keys (KG 2): 33 us, of which
 // 10 to 13 steps of 64 keys are 16 to 20; the rest is the lookup, the queries, the first tile and the
@@ -392,7 +392,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void quant_walk_kernel
   constexpr int BLOCK = kBlock * DH, HALF = 2 * KG * BLOCK, STAGE = 2 * HALF;  // bytes: of a block, a tile's keys, both
   constexpr int STAGES = 65536 / STAGE > 4 ? 4 : 65536 / STAGE;
   constexpr int LT = kList / (2 * KG);  // tiles of a list
-  constexpr bool BY_SUM = sizeof(T) == 2 && DH <= 192;
+  constexpr bool BY_SUM = sizeof(T) == 2;  // no maximum in the loop: 789 us where 803 with it
   constexpr int JOIN = KG == 2 ? 2 * 32 * DH * 4 : 0;
   constexpr int RING = STAGES * STAGE > JOIN ? STAGES * STAGE : JOIN;
   static_assert(STAGES >= 2, "a tile ahead");
