@@ -536,6 +536,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void quant_walk_kernel
       for (int h = 0; h < 2; ++h) vr[x][h] = value(x, h);
     __builtin_amdgcn_sched_barrier(0);
     if (EDGE) {
+      // What is seen is a branch ahead of the scores, and the compiler, where a long and a short path
+      // lead from a product to its use, counts its wait along the long one: here it is in full.
+      asm volatile("s_nop 11");
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int r = 0; r < 16; ++r)
         if ((int)at.scales[r / 8] < 0) sc[r] = -INFINITY;

@@ -441,6 +441,31 @@ def test_long_walks(shape, rows, holes):
         assert bool(((got * see[:, None, None] - want).abs() <= want * (cu.EPS[dtype] + 2.0 ** -15)).all())
 
 
+@pytest.mark.parametrize("rows", [32, 64, 128])
+@pytest.mark.parametrize("shape", MANY, **IDS)
+def test_a_part_repeats_itself(shape, rows):
+    """Several workgroups on every CU, a missing page and the last keys inside a tile: the same bits
+    from every call, whatever runs beside it."""
+    torch = cu.torch_mod()
+    dtype, H, G, D = shape
+    from paper_2608_27384_amd import flashvla as fvb
+    t = fvb.FV_BF16 if dtype == "bf16" else fvb.FV_FP32
+    plans = {top: m for top in (0, 100, 1500) for m in (40, 300, 1000, 2000, 4000, 8000, 16000, 32000)
+             if part_plan(m, 1, H, G, D, top or 1504, t).rows == rows}
+    cache, _, table = qu.make(shape, [1500], 16, layers=1)
+    cache.table[0, 30] = -1
+    assert plans
+    for top, m in plans.items():
+        q = cu.randn(dtype, 5, m, H, D)
+        calls = []
+        for _ in range(4):
+            out = torch.full_like(q, 7.0)
+            cache.attend_part(0, q, cu.ints([0, m]), cu.ints([0]), out, causal=False, max_len=top)
+            calls.append(out)
+        for out in calls:
+            assert out.isfinite().all() and out.equal(calls[0])
+
+
 @pytest.mark.parametrize("n", [62, 63, 64, 65, 300])
 @pytest.mark.parametrize("shape", [SHAPES[0], SHAPES[5]], **IDS)
 def test_many_entries(shape, n):
