@@ -327,3 +327,19 @@ def test_longest_row_of_a_table(max_len):
     again = torch.full_like(q, 7.0)
     cache.attend(0, q, cu.ints([0]), again, max_len=max_len)
     cu.check_attention_wide(again, (want, size, soft + size * 2.0 ** -8), "bf16")
+
+
+@pytest.mark.parametrize("max_len", [0, 700, 40])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_calls_repeat_themselves(shape, max_len):
+    """More workgroups than CUs, in chunks and in one: the same bits from every call."""
+    torch = cu.torch_mod()
+    lens = [1 + 37 * b % 700 for b in range(300)]
+    cache, q, _ = make(shape, lens, layers=1)
+    seqs, calls = cu.ints(range(len(lens))), []
+    for _ in range(4):
+        out = torch.full_like(q, 7.0)
+        cache.attend(0, q, seqs, out, max_len=max_len)
+        calls.append(out)
+    for out in calls:
+        assert out.isfinite().all() and out.equal(calls[0])

@@ -124,6 +124,5 @@ def test_every_product_is_waited_for(tmp_path):
     products = 0
     for name, ins, at in code(tmp_path):
         products += sum(op.startswith("v_mfma") for op, _, _ in ins)
-        if "quant_" in name:
-            assert not [(ins[i][:2], ins[j][:2], "%#x" % at[j], short) for i, j, short in early(ins, at)], name
+        assert not [(ins[i][:2], ins[j][:2], "%#x" % at[j], short) for i, j, short in early(ins, at)], name
     assert products > 10000
