@@ -195,6 +195,10 @@ __global__ __launch_bounds__(64 * kPartWaves, 1) void quant_part_kernel(PartCall
     u32x4 k[2 * SLABS];
     u32x2 v[SLABS][2][2];  // of block c, the positions from 4 lh + 8 h on
   };
+  // A step that some row does not see whole, or whose keys are not all there: its values are sifted.
+  auto is_edge = [&](int key0, int at0, int at1) __attribute__((always_inline)) {
+    return key0 + 32 > whole || key0 + 32 > k1 || at0 < 0 || at1 < 0;
+  };
   auto fetch = [&](int i, Tile& t) __attribute__((always_inline)) {
     const int j = 2 * (i / kPartWaves % 32);
     if (j == 0 && i >= kPartWaves) {
@@ -243,7 +247,7 @@ __global__ __launch_bounds__(64 * kPartWaves, 1) void quant_part_kernel(PartCall
     now = next;
     if (i + kPartWaves < steps) fetch(i + kPartWaves, next);
     const int key0 = k0 + 32 * i, at0 = now.at[0], at1 = now.at[1];
-    const bool edge = key0 + 32 > whole || key0 + 32 > k1 || at0 < 0 || at1 < 0;
+    const bool edge = is_edge(key0, at0, at1);
     const float ks = power_of(scale_exponent((uint8_t)(l32 < 16 ? now.scales[0] : now.scales[1])));
     const float vs[2] = {power_of(scale_exponent((uint8_t)(now.scales[0] >> 8))),
                          power_of(scale_exponent((uint8_t)(now.scales[1] >> 8)))};
@@ -329,13 +333,16 @@ __global__ __launch_bounds__(64 * kPartWaves, 1) void quant_part_kernel(PartCall
       *reinterpret_cast<f32x4*>(mine + l32 * PITCH + at) =
           f32x4{o[d][4 * j] * f, o[d][4 * j + 1] * f, o[d][4 * j + 2] * f, o[d][4 * j + 3] * f};
     }
-  if (unruly) {  // NaN among the values at the edge: of the rows that see them
+  if (unruly) {  // NaN among the values that were sifted: of the rows that see them
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     for (int i = wave; i < steps; i += kPartWaves) {
       const int from = k0 + 32 * i;
+      const int at0 = __builtin_amdgcn_readfirstlane(b.block_at(from));
+      const int at1 = __builtin_amdgcn_readfirstlane(b.block_at(from + 16));
+      if (!is_edge(from, at0, at1)) continue;
       for (int key = from; key < min(from + 32, k1); ++key) {
-        const int at = __builtin_amdgcn_readfirstlane(b.block_at(key & ~15));
-        if (at < 0 || (from + 32 <= whole && from + 32 <= k1)) continue;
+        const int at = key < from + 16 ? at0 : at1;
+        if (at < 0) continue;
         for (int d = lane; d < DH; d += 64) {
           const bool odd = b.is_nan(b.place(at), key, d, DH);
           if (!__any(odd)) continue;

@@ -466,6 +466,81 @@ def test_a_part_repeats_itself(shape, rows):
             assert out.isfinite().all() and out.equal(calls[0])
 
 
+HOLES = [(16, [5, 10, 30]), (48, [3, 4, 9])]  # page_len, table columns that are no page
+
+
+def nan_values(shape, cache, table, n, page_len, cols):
+    """NaN in values beside missing blocks, in the same 32 keys and behind: {position: element}."""
+    gone = {p // 16 for c in cols for p in range(c * page_len, (c + 1) * page_len, 16)}
+    at = {}
+    for b in sorted({x ^ 1 for x in gone} | {0, n // 32 * 2 - 4}):
+        if b in gone or 16 * b + 16 > n:
+            continue
+        p, d = 16 * b + (7 * b + 3) % 16, (11 * b + 5) % shape[3]
+        at[p] = d
+
+        def put(x, d=d):
+            x[:, d] = 255
+            return x
+        codes_at(cache, cache.v, True, 0, table[0, p // page_len], p % page_len, put)
+    return at
+
+
+@pytest.mark.parametrize("page_len,cols", HOLES, ids=lambda x: str(x) if isinstance(x, int) else None)
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("rows", [32, 64, 128, "chunks"])
+@pytest.mark.parametrize("shape", MANY, **IDS)
+def test_values_that_are_not_numbers_beside_missing_pages(shape, rows, causal, page_len, cols):
+    """In each kernel: NaN in the element of a value, in the rows that see it and no others, where the
+    other 16 of its 32 keys have no page; every other element keeps its bits."""
+    torch = cu.torch_mod()
+    dtype, H, G, D = shape
+    m, max_len = (40, 0) if rows == "chunks" else in_one_chunk(shape, rows)
+    n = 1500
+    cache, _, table = qu.make(shape, [n], page_len, layers=1)
+    for c in cols:
+        cache.table[0, c] = -1
+    q = cu.randn(dtype, 8, m, H, D)
+
+    def run():
+        out = torch.full_like(q, 7.0)
+        cache.attend_part(0, q, cu.ints([0, m]), cu.ints([0]), out, causal=causal, max_len=max_len)
+        return out
+
+    clean = run()
+    assert clean.isfinite().all()
+    at = nan_values(shape, cache, table, n, page_len, cols)
+    assert len(at) >= 4
+    got = run()
+    limits = torch.arange(n - m + 1, n + 1, device="cuda").clamp(min=0) if causal else torch.full((m,), n, device="cuda")
+    want = torch.zeros(m, 1, D, dtype=torch.bool, device="cuda")
+    for p, d in at.items():
+        want[:, 0, d] |= limits > p
+    assert got.isnan().equal(want.expand(m, H, D))
+    assert got[~got.isnan()].equal(clean[~got.isnan()])
+
+
+@pytest.mark.parametrize("max_len", [0, 100])
+@pytest.mark.parametrize("page_len,cols", HOLES, ids=lambda x: str(x) if isinstance(x, int) else None)
+@pytest.mark.parametrize("shape", SHAPES, **IDS)
+def test_a_token_sees_values_that_are_not_numbers_beside_missing_pages(shape, page_len, cols, max_len):
+    torch = cu.torch_mod()
+    dtype, H, G, D = shape
+    n = 1500
+    cache, q, table = qu.make(shape, [n], page_len, layers=1)
+    for c in cols:
+        cache.table[0, c] = -1
+    clean, got = torch.full_like(q, 7.0), torch.full_like(q, 7.0)
+    cache.attend(0, q, cu.ints([0]), clean, max_len=max_len)
+    assert clean.isfinite().all()
+    at = nan_values(shape, cache, table, n, page_len, cols)
+    cache.attend(0, q, cu.ints([0]), got, max_len=max_len)
+    want = torch.zeros(D, dtype=torch.bool, device="cuda")
+    want[list(at.values())] = True
+    assert got.isnan().equal(want.expand(1, H, D))
+    assert got[..., ~want].equal(clean[..., ~want])
+
+
 @pytest.mark.parametrize("n", [62, 63, 64, 65, 300])
 @pytest.mark.parametrize("shape", [SHAPES[0], SHAPES[5]], **IDS)
 def test_many_entries(shape, n):
