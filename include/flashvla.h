@@ -685,9 +685,10 @@ fv_status fv_quant_attention(const fv_paged_args *args, const fv_quant_pages *ca
  *  work     fv_quant_part_workspace bytes, overwritten (calls that may run at the same
  *           time need one each); NULL where that is 0
  * Rows past cu_q[n_seqs] are left as they were.  Scores, softmax and sums are fp32; in
- * bf16 the probabilities are rounded to bf16 before they meet the values, in fp32 they
- * keep 24 bits; sums may leave the range of fp32 as in fv_prompt_attention.  out must
- * not overlap q, work none of the other operands, and neither the layer's pages.
+ * bf16 the probabilities keep 16 bits where there are few rows and are rounded to bf16 (8
+ * bits) where there are many before they meet the values, in fp32 they keep 24 bits; sums
+ * may leave the range of fp32 as in fv_prompt_attention.  out must not overlap q, work
+ * none of the other operands, and neither the layer's pages.
  * Errors: FV_ERR_INVALID_ARG (a size below 0, n_seqs > 65536, n_q * n_q_heads > 2^28,
  * n_seqs * n_kv_heads > 2^22, strides, pointers), FV_ERR_HIP.
  */

@@ -9,11 +9,14 @@
 // Per 32 keys: S^T = K Q^T by 32x32 MFMA, so a lane holds 16 scores of one query; the
 // probabilities are, without data movement, the operand of O^T += V^T P^T.  Codes become bf16
 // operands by an exact conversion that applies the block's scale.  fp32 queries and
-// probabilities go in as three parts of bf16 each, 24 bits.  In bf16 the queries are exact and a
-// probability is one bf16 number, off by half a step, 2^-9 to 2^-8 of it: nothing would hide the
-// products of a second part, and the error is that of rounding the result.  (The unit's products
-// of codes as they are, at twice the rate, are not used: their inner sums are off by 2^-12 of the
-// largest term, which scores of large keys cannot bear, and queries would need several parts.)
+// probabilities go in as three parts of bf16 each, 24 bits.  In bf16 the queries are exact.  A
+// probability is two parts, 16 bits, where there are few rows (50 tokens on 866 keys, heads 8/1
+// of 256: 14.3 us, with one part 14.0).  In the kernels of 64 and 128 rows nothing would hide the
+// products of a second part, and it is one bf16 number, off by up to 2^-8 of it: us with one and
+// with two, the same heads, 64 parts of 1 to 61 tokens on 300 to 866 keys 32.4 and 45.5, 500 tokens
+// on 8000 keys 54 and 67, 4096 on 28672 785 and 1087.  (The unit's products of codes as they are, at
+// twice the rate, are not used: their inner sums are off by 2^-12 of the largest term, which scores
+// of large keys cannot bear, and queries would need several parts.)
 #include "fv_paged.h"
 #include "fv_prompt.h"
 #include "fv_quant.h"
@@ -164,7 +167,7 @@ constexpr int kPartWaves = 4;
 template <typename T, int DH>
 __global__ __launch_bounds__(64 * kPartWaves, 1) void quant_part_kernel(PartCall a) {
   constexpr int SLABS = DH / 64, NK = DH / 16, ND = DH / 32, PITCH = DH + 4;
-  constexpr int PARTS = sizeof(T) == 2 ? 1 : 3;
+  constexpr int PARTS = sizeof(T) == 2 ? 1 : 3, PP = sizeof(T) == 2 ? 2 : 3;  // of queries, of probabilities
   // fp32 queries of long heads are 144 or 192 registers in parts: they stay in LDS, where `so` comes
   // later.  50 tokens on 866 keys, 8/1 heads of 256, 16.5 us, in registers 20.0; 4/2 of 192 13.3, 14.2.
   constexpr bool PUT = PARTS == 3 && DH >= 192;
@@ -288,8 +291,8 @@ __global__ __launch_bounds__(64 * kPartWaves, 1) void quant_part_kernel(PartCall
                      for (int d = 0; d < ND; ++d) o[d] *= f;
                    },
                    [](int) {});
-    u32x4 pf[2][PARTS];
-    probabilities<PARTS>(sc, pf);
+    u32x4 pf[2][PP];
+    probabilities<PP>(sc, pf);
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
@@ -298,7 +301,7 @@ __global__ __launch_bounds__(64 * kPartWaves, 1) void quant_part_kernel(PartCall
         const u32x4 v = u32x4{to_bf16<false>(lo, vs[c]), to_bf16<true>(lo, vs[c]), to_bf16<false>(hi, vs[c]),
                               to_bf16<true>(hi, vs[c])};
 #pragma unroll
-        for (int x = 0; x < PARTS; ++x) o[d] = mma32(v, pf[c][x], o[d], bf16_t{});
+        for (int x = 0; x < PP; ++x) o[d] = mma32(v, pf[c][x], o[d], bf16_t{});
       }
   }
 

@@ -541,6 +541,21 @@ def test_a_token_sees_values_that_are_not_numbers_beside_missing_pages(shape, pa
     assert got[..., ~want].equal(clean[..., ~want])
 
 
+@pytest.mark.parametrize("m,n,max_len", [(1, 300, 0), (17, 866, 0), (50, 866, 866), (40, 1500, 100)])
+@pytest.mark.parametrize("shape", [("bf16", 8, 1, 256), ("bf16", 8, 2, 64), ("bf16", 4, 2, 192), ("bf16", 8, 4, 128)], **IDS)
+def test_few_rows_keep_16_bits_of_their_probabilities(shape, m, n, max_len):
+    """The kernel of 32 rows, in chunks and in one, to what two parts of a probability leave."""
+    torch = cu.torch_mod()
+    dtype, H, G, D = shape
+    assert part_plan(m, 1, H, G, D, max_len or -(-n // 16) * 16).rows == 32
+    cache, _, table = qu.make(shape, [n], layers=1)
+    q = cu.randn(dtype, 12, m, H, D)
+    out = torch.full_like(q, 7.0)
+    cache.attend_part(0, q, cu.ints([0, m]), cu.ints([0]), out, max_len=max_len)
+    k, v = qu.context(cache, table, 0, n, 0)
+    cu.check_attention_wide(out, qu.attention(q, k, v, [n - m + 1 + j for j in range(m)], dtype), dtype)
+
+
 @pytest.mark.parametrize("n", [62, 63, 64, 65, 300])
 @pytest.mark.parametrize("shape", [SHAPES[0], SHAPES[5]], **IDS)
 def test_many_entries(shape, n):
