@@ -166,9 +166,9 @@ void check_list(const fv_pages* c, const void* p, int n, const char* what) {
   if (n) aligned(p, 4, what);
 }
 
-// The rotary append into c (or none), which holds `held` for the layer; whether there is work.
+// The rotary append into c (or none), a checked cache whose layer (checked too) holds `held`;
+// whether there is work.
 bool check_rope(const fv_rope_args* a, const fv_pages* c, const Span* held, int n_held) {
-  need(a, "args");
   const size_t e = type_size(a->dtype);
   check_heads(a->n_q_heads, a->n_kv_heads, a->head_dim);
   if (a->n < 0 || a->n > 1 << 26) bad("n must be 0 to 2^26");
@@ -180,12 +180,8 @@ bool check_rope(const fv_rope_args* a, const fv_pages* c, const Span* held, int 
   }
   if (pairs != a->head_dim / 2) bad("sections must add up to head_dim/2");
   if (!(a->theta > 0.f) || !std::isfinite(a->theta)) bad("theta must be positive and finite");
-  if (c) {
-    check_cache(c);
-    if (c->dtype != a->dtype || c->head_dim != a->head_dim || c->n_kv_heads != a->n_kv_heads)
-      bad("the cache has another dtype, head_dim or n_kv_heads");
-    if (a->layer < 0 || a->layer >= c->n_layers) bad("layer out of range");
-  }
+  if (c && (c->dtype != a->dtype || c->head_dim != a->head_dim || c->n_kv_heads != a->n_kv_heads))
+    bad("the cache has another dtype, head_dim or n_kv_heads");
   if (a->n == 0) return false;
   const int rq = a->n_q_heads * a->head_dim, rk = a->n_kv_heads * a->head_dim;
   const Span q = operand(a->q, a->n, a->ldq, rq, e, "q");
