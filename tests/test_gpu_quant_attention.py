@@ -631,6 +631,35 @@ def test_offsets_that_do_not_ascend(shape):
         cu.check_attention(out[lo:lo + 20], ref, dtype)
 
 
+@pytest.mark.parametrize("rows,max_len", [(64, 0), (64, 100), (2000, 100)])
+@pytest.mark.parametrize("entries", [2, 70])
+@pytest.mark.parametrize("shape", [SHAPES[0], SHAPES[5], ("bf16", 32, 8, 128)], **IDS)
+def test_wrong_offsets_write_no_other_rows(shape, entries, rows, max_len):
+    """Between guard rows, which offsets outside the rows or descending leave as they were; so they do
+    all rows where no entry has any."""
+    torch = cu.torch_mod()
+    dtype, H, G, D = shape
+    lens = [60, 200]
+    cache, _, table = qu.make(shape, lens)
+    q = cu.randn(dtype, 3, rows, H, D)
+    full = torch.full((rows + 512, H, D), 7.0, dtype=q.dtype, device="cuda")
+    out = full[256:256 + rows]
+    big, mid = 1 << 30, rows // 3
+    for first, last in ((rows, rows), (big, big), (5, 1), (rows, 0), (-9, -9), (-big, -1), (rows + 1, big),  # no rows
+                        (0, rows + 6), (-7, rows), (-big, big), (mid, big)):
+        for middle in (first, last, (first + last) // 2):
+            cum = [first] + [middle] * (entries - 1) + [last]
+            cache.attend_part(0, q, cu.ints(cum), cu.ints([i % 2 for i in range(entries)]), out, max_len=max_len)
+            assert (full[:256] == 7).all() and (full[256 + rows:] == 7).all()
+            begin, end = (min(max(x, 0), rows) for x in (first, last))
+            assert (out[:begin] == 7).all()
+            if begin >= end:
+                assert (out == 7).all()
+            else:
+                assert (out[begin:end] != 7).any(-1).all() and out.isfinite().all()
+            out.fill_(7.0)
+
+
 def test_nothing_to_attend():
     torch = cu.torch_mod()
     cache, q, _ = qu.make(SHAPES[2], [10, 20])
