@@ -650,6 +650,10 @@ typedef struct {
  *    (which changes only what falls below 2^-6 of it).
  * Elements are rounded to the nearest code, ties to even, and saturate at 448 times
  * the scale; what is infinite or NaN becomes NaN and has no part in a.
+ * A block's scale does not fall while the block goes on: tokens that are taken back (a
+ * shorter length) may have had the ones before them in their block rounded again, which
+ * stays.  Tokens that may be taken back go to a child (fv_quant_fork), whose part-filled
+ * page is its own.
  * A block whose tokens stand in several places of the list holds codes of either
  * and a scale of either: the caller appends them by several calls.
  * Errors: FV_ERR_INVALID_ARG, FV_ERR_HIP.

@@ -532,6 +532,35 @@ def test_written_tensors_move_their_versions():
     moved(lambda: cache.free(cu.ints([0]), st), books)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_tokens_that_are_taken_back(dtype):
+    """Large tokens appended behind five of a block, then left out by a shorter length: the five are
+    rounded at the grown scale and stay so.  Appended to a fork they change nothing of the parent's."""
+    torch = cu.torch_mod()
+    cache, _ = fresh(20, 4, 4, layers=1, dtype=dtype)
+    G, D = cache.c.n_kv_heads, cache.c.head_dim
+
+    def append(seq, at, size):
+        n = len(at)
+        q, k, v = (cu.randn(dtype, 7 + i, n, h, D, std=size) for i, h in enumerate((2 * G, G, G)))
+        assert int(cache.grow(cu.ints([seq]), cu.ints([n]))) == 0
+        cache.append(0, q, k, v, cu.ints([at]), cu.ints([seq] * n), cu.ints(at), (D // 2,))
+
+    def held(seq):
+        kd, vd = (torch.zeros(1, 1, 21, G, D, dtype=cu.ttype(dtype), device="cuda") for _ in range(2))
+        cache.gather(cu.ints([seq]), kd, vd)
+        return kd, vd
+
+    append(0, range(21), 1.0)
+    first = held(0)
+    assert int(cache.fork(cu.ints([0]), cu.ints([1]))) == 0
+    append(1, range(21, 24), 1e4)
+    cache.length[1] = 21
+    for seq, same in ((0, True), (1, False)):
+        for a, b in zip(held(seq), first):
+            assert a[:, :, :16].equal(b[:, :, :16]) and a[:, :, 16:].equal(b[:, :, 16:]) == same
+
+
 # ------------------------------------------------------------------ together
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
