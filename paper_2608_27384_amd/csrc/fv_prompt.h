@@ -185,11 +185,10 @@ __device__ __forceinline__ void softmax(f32x16& sc, bool edge, int key0, int lh,
 // either half's keys) is past kLimit, or none, takes its maximum as the reference and
 // everything again.  `minus`: minus the reference, kNoRef for a row without one,
 // against which any visible score is infinite and a hidden one still nothing.
-// Leaves the scores as they are, which takes 16 more registers: for head dims up to
-// 192.  At 128 the vector unit is busy 58 % of the time and the matrix unit 62 %, and a
-// wave uses one after the other: 16 maxima less, and the kept load offsets, brought eight
-// prompts of 2000 tokens, every key seen, heads 32/8 of 128, from 519 to 485 us (1.08
-// PFLOP/s).
+// Leaves the scores as they are, which takes 16 more registers.  With heads of 128 the
+// vector unit is busy 58 % of the time and the matrix unit 62 %, and a wave uses one after
+// the other: 16 maxima less, and the kept load offsets, brought eight prompts of 2000
+// tokens, every key seen, heads 32/8 of 128, from 519 to 485 us (1.08 PFLOP/s).
 constexpr float kLimit = 1024.0f;  // sums stay within 2^10 of the largest value's size
 constexpr float kNoRef = 3.402823466e38f;
 template <typename Rescale>

@@ -266,6 +266,7 @@ struct Walk : Rows<T, DH, 128> {
     const int lim = limit(wrow + l32);
     meet();  // the ring is the tiles' from here on
     const int end = wrow < rows ? limit(wrow + 31) : 0;
+    // heads of 256 leave no 16 registers for it here
     constexpr bool BY_SUM = E == 2 && DH <= 192;
     f32x16 o[ND];
     float m = BY_SUM ? kNoRef : -INFINITY, l = 0.f;  // l over the lane half's keys only

@@ -163,7 +163,7 @@ constexpr int kPartWaves = 4;
 // the next step's codes under way in the one before, and join in LDS.  For where there are so few
 // rows that the time is the chain of trips to memory (offsets, the table with the length, scales
 // and codes, then the join's): 50 tokens on 866 keys, 8 query heads and 1 kv head of 256, bf16, are
-// 14.0 us with the join, of which two launches are 8; 1.5 us of it are products.
+// 14.3 us with the join, of which two launches are 8; under 2 us of it are products.
 template <typename T, int DH>
 __global__ __launch_bounds__(64 * kPartWaves, 1) void quant_part_kernel(PartCall a) {
   constexpr int SLABS = DH / 64, NK = DH / 16, ND = DH / 32, PITCH = DH + 4;
@@ -797,11 +797,12 @@ namespace {
 // little more than the longer; where there are chunks, the join and what it reads.  Either
 // time is a fixed part and one for each 32 keys, with a part of each that grows with the head.
 // The workgroups of fp32 have a CU each, so that what is over a full round counts half a round.
-// Fitted to 11370 timings of 1086 calls of 1 to 512 sequences, 1 to 4096 new tokens, 1 to 30000
-// keys, heads 8/1 of 256, 32/8 of 128, 8/2 of 64 and 4/2 of 192 (14 % off each).  What it
-// chooses took 3 % longer than the best of all in the mean and 10 % at the ninetieth hundredth
-// (2 and 7 % in fp32, on 284 other calls, since the queries of long heads are in LDS),
-// where limits on the number of row tiles and of keys took over 10 % in the mean.
+// Fitted, by least squares of the logarithms, to 11370 timings of 1086 calls of 1 to 512 sequences, 1
+// to 4096 new tokens, 1 to 30000 keys, heads 8/1 of 256, 32/8 of 128, 8/2 of 64 and 4/2 of 192 (14 %
+// off each), when the probabilities of few rows had one part in bf16.  With the present kernels what
+// it chooses takes 4 % longer than the best of all in the mean and 14 % at the ninetieth hundredth, over
+// the 3738 timings of 296 calls in profiles/quant_part_timings.txt; limits on the number of row tiles
+// and of keys took over 10 % in the mean.
 double part_time(bool fp32, int kind, double head, double tiles, double chunk, int chunks, double moved) {
   static const double of[2][3][8] = {
       {{0.836, 4.174, 0.136, 0.259, 0.051, 6.612, 0.102, 0.302},
@@ -827,17 +828,17 @@ double part_time(bool fp32, int kind, double head, double tiles, double chunk, i
 // The rows of a workgroup and the chunks that part_time says are the fastest.  us by rows and, in
 // brackets, chunks, the best of each, of calls captured into a graph, and what is taken:
 //                                          32        64        128       taken
-// 50 tokens on 866, heads 8/1 of 256       14.3 (7)  15.5 (7)  17.9 (7)  32 (7)
-// 4 by 50 on 866, 8/1 of 256               18.1 (4)  19.7 (3)  22.7 (7)  64 (4): 20
-// 64 by 1 to 61 on 300 to 866, 8/1 of 256  52.2 (1)  34.5 (1)  37.4 (1)  64 (1)
-// 128 by 50 on 300 to 866, 8/1 of 256      125 (1)   64.9 (1)  54.1 (1)  128 (1)
-// 500 on 8000, 8/1 of 256                  66.7 (2)  53.1 (8)  55.6 (8)  64 (6): 56.6
-// 4096 on 28672, 8/1 of 256                1390 (1)  824 (1)   808 (2)   128 (2)
-// 32 by 1 to 100 on 100 to 3000, 32/8/128  143 (1)   87.6 (1)  103 (3)   64 (1)
-// 8 by 500 on 2000, 32/8 of 128            295 (1)   161 (1)   132 (1)   128 (1)
-// fp32: 5 by 33 to 301 on 60 to 1301, 8/2/64 17.8 (1)  23.4 (4)  24.6 (4)  32 (1)
-// fp32: 50 on 900, 8/1 of 256              16.8 (8)  21.6 (8)  27.3 (8)  32 (8)
-// fp32: 4 by 200 on 1000, 8/1 of 256       35.9 (1)  43.8 (2)  44.4 (4)  32 (1)
+// 50 tokens on 866, heads 8/1 of 256       14.6 (7)  15.4 (7)  17.6 (7)  32 (7)
+// 4 by 50 on 866, 8/1 of 256               18.7 (4)  20.1 (4)  22.5 (4)  64 (4)
+// 64 by 1 to 61 on 300 to 866, 8/1 of 256  55.2 (1)  33.5 (1)  36.1 (1)  64 (1)
+// 128 by 50 on 300 to 866, 8/1 of 256      134 (1)   62.9 (1)  52.6 (1)  128 (1)
+// 500 on 8000, 8/1 of 256                  74.6 (2)  53.3 (8)  54.0 (8)  64 (6): 55.5
+// 4096 on 28672, 8/1 of 256                1570 (1)  806 (1)   809 (2)   128 (2)
+// 32 by 1 to 100 on 100 to 3000, 32/8/128  156 (1)   87.2 (1)  103 (3)   64 (1)
+// 8 by 500 on 2000, 32/8 of 128            323 (1)   156 (1)   131 (1)   128 (1)
+// fp32: 5 by 33 to 301 on 60 to 1301, 8/2/64 17.6 (1)  23.3 (4)  24.8 (4)  32 (1)
+// fp32: 50 on 900, 8/1 of 256              16.8 (8)  21.7 (8)  27.3 (8)  32 (8)
+// fp32: 4 by 200 on 1000, 8/1 of 256       36.7 (1)  44.8 (2)  45.3 (4)  32 (1)
 // fp32: 64 by 50 on 866, 8/1 of 256        126 (1)   97.7 (1)  83.6 (1)  64 (1)
 PartPlan plan_part(const fv_part_args& x, const fv_quant_pages& c, int max_keys) {
   static const int counts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
