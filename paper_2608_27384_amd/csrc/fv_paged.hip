@@ -203,11 +203,10 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_kernel(PagedCall a)
         for (int b = 0; b < KB; ++b) sc[h] = mma64(kf[h][b], qf[b], sc[h], T{});
       }
       __builtin_amdgcn_sched_barrier(0);
-      if (it + 1 < here) load_keys(it + 1);  // while the softmax and the values are at work
-      // Ahead of the next branch: the compiler, where a long and a short path lead from a product to its
-      // use, counts its wait along the long one.
-#pragma unroll
-      for (int h = 0; h < NH; ++h) sc[h] *= a.scale;
+      if (it + 1 < here)
+        load_keys(it + 1);  // while the softmax and the values are at work
+      else
+        asm volatile("s_nop 9");  // the compiler counts the products' wait along the loads' path only
       bool whole = true;
 #pragma unroll
       for (int h = 0; h < NH; ++h) {
@@ -228,7 +227,10 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_kernel(PagedCall a)
 #pragma unroll
       for (int h = 0; h < NH; ++h)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) top = fmaxf(top, sc[h][r]);
+        for (int r = 0; r < 4; ++r) {
+          sc[h][r] *= a.scale;
+          top = fmaxf(top, sc[h][r]);
+        }
       top = max_xor16_32(top);
       if (__any(top > m)) {
         const float now = fmaxf(m, top);
